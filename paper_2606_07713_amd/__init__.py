@@ -9,6 +9,10 @@ The Python names mirror the C entry points (``moa_attn_fwd``,
 computation runs in the library's HIP kernels.  ``attn_fwd`` is a convenience
 wrapper for torch tensors (torch supplies device memory and the stream).
 
+What stands around the attention of a model has modules of its own, with their
+names here as well: ``rope`` (``include/moa_rope.h``: norms of queries and keys
+for each head with the rotation by position, and the gradients).
+
 There is no fallback: if the HIP library has not been built, importing this
 package raises ``ImportError``.
 """
@@ -26,6 +30,8 @@ __all__ = [
     "moa_attn_fwd_strided", "moa_attn_bwd", "moa_attn_bwd_workspace_bytes", "attn_bwd", "LIB_PATH",
     "lib", "moa_attn_fwd_proj", "moa_attn_proj_workspace_bytes", "attn_fwd_proj",
     "moa_attn_fwd_noalloc", "MOA_ERR_SCRATCH", "MOA_NOALLOC_SCRATCH_BYTES", "moa_attn_fwd_onf",
+    "moa_qk_norm_rope", "moa_qk_norm_rope_bwd", "moa_qk_norm_rope_bwd_workspace_bytes",
+    "qk_norm_rope", "qk_norm_rope_bwd",
 ]
 
 MOA_OK, MOA_ERR_INVALID_ARG, MOA_ERR_UNSUPPORTED, MOA_ERR_WORKSPACE, MOA_ERR_HIP = 0, 1, 2, 3, 4
@@ -364,3 +370,8 @@ def attn_fwd_proj(x, wq, wk, wv, heads, scale=None, causal=False, out_dtype=None
         res.append(tuple(raw[i * sz: i * sz + B * heads * N * d * 2].view(torch.bfloat16)
                          .view(B, heads, N, d) for i in range(3)))
     return res[0] if len(res) == 1 else tuple(res)
+
+
+from .rope import (  # noqa: E402
+    moa_qk_norm_rope, moa_qk_norm_rope_bwd, moa_qk_norm_rope_bwd_workspace_bytes, qk_norm_rope,
+    qk_norm_rope_bwd)

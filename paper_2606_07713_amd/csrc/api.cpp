@@ -6,10 +6,13 @@
 #include <limits>
 
 #include "../../include/moa_attn.h"
+#include "api_checks.h"
 #include "launch.h"
 #include "proj.h"
 
 namespace {
+
+using namespace moa;   // the checks of api_checks.h
 
 constexpr int kMaxSplits = 256;
 // Keys a decode workgroup should stream at least, and the workgroup count the
@@ -55,8 +58,6 @@ int pick_splits(int64_t bh, int64_t Nk, int requested) {
     if (s < 1) s = 1;
     return (int)s;
 }
-
-size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 size_t prefill_ws_bytes(int64_t bh, int64_t Nq, int64_t d, int splits) {
     return align256((size_t)bh * (size_t)Nq * (size_t)splits * (size_t)(d + 2) * sizeof(float));
@@ -186,21 +187,6 @@ size_t decode_ws_bytes(int64_t bh, int64_t d, int splits) {
     return align256((size_t)bh * (size_t)splits * (size_t)(d + 2) * sizeof(float));
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-bool overlaps(const void* a, size_t an, const void* b, size_t bn) {
-    if (an == 0 || bn == 0) return false;
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-    return a0 < b0 + bn && b0 < a0 + an;
-}
-
-// Element strides of one tensor over (batch, head, row); d is contiguous.
-struct Strides {
-    int64_t b, h, r;
-};
-
-Strides contiguous(int64_t H, int64_t N, int64_t d) { return {H * N * d, N * d, d}; }
-
 // Checks of one tensor's strides: non-negative, every row 16-byte aligned,
 // rows of d elements that do not overlap, and in-head byte offsets that fit
 // the kernels' 32-bit descriptors.  0 = fine, else a status code.
@@ -213,29 +199,6 @@ int check_strides(const Strides& s, int64_t N, int64_t d, size_t es) {
     if (s.r > lim / (int64_t)es) return MOA_ERR_UNSUPPORTED;
     if (N > 0 && ((N - 1) * s.r + d) > lim / (int64_t)es) return MOA_ERR_UNSUPPORTED;
     return 0;
-}
-
-// Bytes from a tensor's base pointer to the end of its last element.
-size_t extent_bytes(const Strides& s, int64_t B, int64_t H, int64_t N, int64_t d, size_t es) {
-    if (B == 0 || H == 0 || N == 0 || d == 0) return 0;
-    return (size_t)((B - 1) * s.b + (H - 1) * s.h + (N - 1) * s.r + d) * es;
-}
-
-// True if no two (batch, head, row, element) positions share an address:
-// the dimensions of size > 1, by increasing stride, nest without overlap.
-bool injective(const Strides& s, int64_t B, int64_t H, int64_t N, int64_t d) {
-    if (B == 0 || H == 0 || N == 0) return true;   // nothing is written
-    struct Dim { int64_t stride, count; } dims[3] = {{s.b, B}, {s.h, H}, {s.r, N}};
-    for (int i = 0; i < 3; ++i)
-        for (int j = i + 1; j < 3; ++j)
-            if (dims[j].stride < dims[i].stride) { Dim t = dims[i]; dims[i] = dims[j]; dims[j] = t; }
-    int64_t span = d;   // elements covered by the inner dimensions so far
-    for (int i = 0; i < 3; ++i) {
-        if (dims[i].count <= 1) continue;
-        if (dims[i].stride < span) return false;
-        span = dims[i].stride * dims[i].count;
-    }
-    return true;
 }
 
 // Element strides of one tensor over (batch, head, row, head element), for
@@ -270,6 +233,12 @@ bool injective4(const Strides4& t, int64_t B, int64_t H, int64_t N, int64_t d) {
 }
 
 }  // namespace
+
+int moa::hip_status(hipError_t e) {
+    if (e == hipSuccess) return MOA_OK;
+    g_last_hip_error = hipGetErrorName(e);
+    return MOA_ERR_HIP;
+}
 
 extern "C" {
 

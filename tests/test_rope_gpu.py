@@ -1,0 +1,233 @@
+"""Head norms with rotation on the GPU against the formulas in fp64.
+
+Tolerances, per element.  Forward: y = r (x A + x' B); the sum of squares (tree of 128 terms), the
+reciprocal square root, the sine, the cosine and the products are each off by a few 2^-24, below
+16 of them together, relative to r (|x w| + |x' w'|); bf16 outputs add half a step, 2^-8 |y|.
+Backward: two such sums and their products, below 64 units of 2^-24 relative to the magnitudes that
+are added; a weight's gradient adds one unit per row that its fp32 sum takes.
+"""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def _say(*a):
+    print(*a, flush=True)
+
+
+def _angles(pos, freq, sections, B, N):
+    """fp64 angles [B, 1, N, pairs]."""
+    import torch
+    pairs = freq.numel()
+    if pairs == 0:
+        return torch.zeros((B, 1, N, 0), dtype=torch.float64)
+    if pos is None:
+        pos = torch.arange(N).expand(B, N)
+    pos = pos.cpu().double().reshape(-1, B, N)
+    axis = [a for a, n in enumerate(sections or [pairs]) for _ in range(n)]
+    f = freq.cpu().double()
+    return torch.stack([pos[axis[i]] * f[i] for i in range(pairs)], -1)[:, None]
+
+
+def _rotate(t, ang, il, sign=1.0):
+    """(rotated, partner magnitudes |t'|) of fp64 rows t."""
+    import torch
+    r = 2 * ang.shape[-1]
+    y, mag = t.clone(), torch.zeros_like(t)
+    ia, ib = (slice(0, r, 2), slice(1, r, 2)) if il else (slice(0, r // 2), slice(r // 2, r))
+    a, b, c, s = t[..., ia], t[..., ib], ang.cos(), sign * ang.sin()
+    y[..., ia], y[..., ib] = a * c - b * s, b * c + a * s
+    mag[..., ia], mag[..., ib] = b.abs(), a.abs()
+    return y, mag
+
+
+def _reference(x, w, ang, il, eps, dy=None):
+    import torch
+    x = x.detach().cpu().double()
+    d = x.shape[-1]
+    r = 1 / torch.sqrt(x.square().mean(-1, keepdim=True) + eps) if w is not None else torch.ones(())
+    wd = w.cpu().double() if w is not None else torch.ones(d, dtype=torch.float64)
+    n = x * r
+    y, other = _rotate(n * wd, ang, il)
+    tol = 16 * U * ((n * wd).abs() + other)
+    if dy is None:
+        return y, tol
+    g, other = _rotate(dy.cpu().double(), ang, il, -1.0)
+    gmag = dy.cpu().double().abs() + other
+    if w is None:
+        return y, tol, g, 16 * U * gmag, None, None
+    gw = g * wd
+    dx = r * (gw - n * (gw * n).mean(-1, keepdim=True))
+    xmag = r * (gmag * wd.abs() + n.abs() * (gmag * wd.abs() * n.abs()).mean(-1, keepdim=True))
+    dw = (g * n).sum((0, 1, 2))
+    rows = x[..., 0].numel()
+    return y, tol, dx, 64 * U * xmag, dw, (64 + rows) * U * (gmag * n.abs()).sum((0, 1, 2))
+
+
+def _near(name, got, want, tol):
+    import torch
+    half = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}[got.dtype]
+    err = (got.cpu().double() - want).abs()
+    lim = tol + half * want.abs()
+    worst = (err / lim.clamp(min=1e-300)).max().item() if err.numel() else 0.0
+    _say(f"  {name}: worst {worst:.2f} of the bound")
+    assert not torch.isnan(got).any() and worst <= 1.0, name
+
+
+def _inputs(B, Hq, Hk, N, d, dtype, rot, axes, norm, packed, far, seed=1):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    dt = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    dev = lambda t: t.to("cuda")  # noqa: E731
+    if packed:
+        x = dev(torch.randn((B, N, Hq + 2 * Hk, d), generator=g).to(dt))
+        q, k = x[:, :, :Hq].transpose(1, 2), x[:, :, Hq:Hq + Hk].transpose(1, 2)
+    else:
+        q, k = (dev((2 * torch.randn((B, h, N, d), generator=g)).to(dt)) for h in (Hq, Hk))
+    w = [dev((1 + 0.3 * torch.randn(d, generator=g)).to(dt)) if n else None for n in norm]
+    freq = dev(torch.tensor([10000.0 ** (-2 * i / rot) for i in range(rot // 2)], dtype=torch.float32)) if rot else None
+    pos = dev(far + torch.randint(0, 5000, (axes, B, N), generator=g))
+    sections = None
+    if axes > 1:
+        sections = [rot // 2 - (axes - 1) * (rot // 2 // axes)] + [rot // 2 // axes] * (axes - 1)
+    else:
+        pos = pos[0]
+    return q, k, w, freq, pos, sections
+
+
+# B, Hq, Hk, N, d, dtype, rot, axes, interleaved, norm of (q, k), packed, far
+CASES = [
+    (1, 32, 8, 1, 128, "bf16", 128, 1, False, (True, True), False, 1000000),
+    (1, 1, 1, 1, 64, "f32", 64, 1, False, (True, True), False, 0),
+    (2, 3, 5, 33, 128, "bf16", 128, 1, False, (True, True), True, 100),
+    (2, 4, 2, 67, 64, "bf16", 64, 1, True, (True, False), True, 7),
+    (3, 2, 7, 41, 128, "f32", 96, 3, False, (True, True), False, 50000),
+    (1, 5, 1, 130, 64, "f32", 16, 2, True, (False, False), False, 3),
+    (2, 12, 12, 100, 64, "bf16", 32, 4, False, (False, True), False, 11),
+    (1, 3, 2, 19, 128, "bf16", 0, 1, False, (True, True), False, 0),
+    (4, 16, 4, 1100, 128, "bf16", 128, 1, False, (True, True), True, 0),
+]
+IDS = lambda c: "x".join(map(str, c[:5])) + f"_{c[5]}_r{c[6]}_a{c[7]}" + ("_il" if c[8] else "")  # noqa: E731
+
+
+@pytest.mark.parametrize("case", CASES, ids=IDS)
+def test_forward_and_gradients(case):
+    import torch
+    import paper_2606_07713_amd as moa
+    B, Hq, Hk, N, d, dtype, rot, axes, il, norm, packed, far = case
+    _say(f"rope {case}")
+    q, k, w, freq, pos, sections = _inputs(B, Hq, Hk, N, d, dtype, rot, axes, norm, packed, far)
+    how = dict(positions=pos, inv_freq=freq, q_weight=w[0], k_weight=w[1], eps=1e-5, interleaved=il, sections=sections)
+    g = torch.Generator().manual_seed(9)
+    gy = [torch.randn(x.shape, generator=g).to(x.dtype).to("cuda") for x in (q, k)]
+    y = moa.qk_norm_rope(q, k, **how)
+    dq, dk, dwq, dwk = moa.qk_norm_rope_bwd(q, k, *gy, **how)
+    torch.cuda.synchronize()
+    ang = _angles(pos, freq if freq is not None else torch.zeros(0), sections, B, N)
+    for name, x, yy, dx, dw, wt, dy in (("q", q, y[0], dq, dwq, w[0], gy[0]), ("k", k, y[1], dk, dwk, w[1], gy[1])):
+        ref = _reference(x, wt, ang, il, 1e-5, dy)
+        _near(name, yy, *ref[:2])
+        _near("d" + name, dx, *ref[2:4])
+        assert (dw is None) == (wt is None)
+        if wt is not None:
+            _near("dw " + name, dw, *ref[4:])
+
+
+def test_gradients_against_differences():
+    # d/dx and d/dw of sum(y * g) by central differences of the fp64 formula
+    import torch
+    import paper_2606_07713_amd as moa
+    q, k, w, freq, pos, sections = _inputs(1, 2, 1, 3, 64, "f32", 64, 2, (True, True), False, 5)
+    how = dict(positions=pos, inv_freq=freq, q_weight=w[0], k_weight=w[1], sections=sections)
+    gy = [torch.randn(x.shape, generator=torch.Generator().manual_seed(3)).to("cuda") for x in (q, k)]
+    dq, _, dwq, _ = moa.qk_norm_rope_bwd(q, k, *gy, **how)
+    ang = _angles(pos, freq, sections, 1, 3)
+
+    def loss(x, wt):
+        return (_reference(x, wt, ang, False, 1e-6)[0] * gy[0].cpu().double()).sum().item()
+
+    x0, w0, h = q.cpu().double(), w[0].cpu().double(), 2.0 ** -12
+    # error of a central difference: h^2 |f'''| / 6 < 1e-6 here; the kernel's below 1e-5
+    for i in (0, 17, 63):
+        for base, grad, at in ((x0, dq, (0, 1, 2, i)), (w0, dwq, (i,))):
+            up, down = base.clone(), base.clone()
+            up[at] += h
+            down[at] -= h
+            diff = (loss(up, w0) - loss(down, w0)) if base is x0 else (loss(x0, up) - loss(x0, down))
+            assert abs(diff / (2 * h) - grad[at].item()) < 2e-5
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_in_place_and_strided_outputs(packed):
+    import torch
+    import paper_2606_07713_amd as moa
+    q, k, w, freq, pos, sections = _inputs(2, 6, 2, 45, 128, "bf16", 128, 1, (True, True), packed, 9)
+    how = dict(positions=pos, inv_freq=freq, q_weight=w[0], k_weight=w[1])
+    want = moa.qk_norm_rope(q, k, **how)
+    out = torch.zeros((2, 45, 10, 128), dtype=torch.bfloat16, device="cuda")
+    views = out[:, :, :6].transpose(1, 2), out[:, :, 6:8].transpose(1, 2)
+    moa.qk_norm_rope(q, k, q_out=views[0], k_out=views[1], **how)
+    assert torch.equal(views[0], want[0]) and torch.equal(views[1], want[1]) and not out[:, :, 8:].any()
+    gy = [torch.randn(x.shape, device="cuda").to(torch.bfloat16) for x in (q, k)]
+    grads = moa.qk_norm_rope_bwd(q, k, *gy, **how)
+    inplace = [t.clone() for t in gy]
+    again = moa.qk_norm_rope_bwd(q, k, *inplace, dq=inplace[0], dk=inplace[1], **how)
+    for a, b in zip(grads, again):
+        assert torch.equal(a, b)
+    moa.qk_norm_rope(q, k, q_out=q, k_out=k, **how)
+    torch.cuda.synchronize()
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
+def test_queries_alone_default_positions_and_no_rows():
+    import torch
+    import paper_2606_07713_amd as moa
+    q, k, w, freq, pos, _ = _inputs(2, 3, 1, 37, 64, "bf16", 64, 1, (True, True), False, 0)
+    a, none = moa.qk_norm_rope(q, inv_freq=freq, q_weight=w[0])
+    b, _ = moa.qk_norm_rope(q, positions=torch.arange(37, device="cuda").expand(2, 37).contiguous(), inv_freq=freq,
+                            q_weight=w[0])
+    assert none is None and torch.equal(a, b)
+    e = q[:0]
+    y, _ = moa.qk_norm_rope(e, inv_freq=freq, q_weight=w[0])
+    dq, _, dw, _ = moa.qk_norm_rope_bwd(e, None, e, None, inv_freq=freq, q_weight=w[0])
+    torch.cuda.synchronize()
+    assert y.shape == e.shape and dq.shape == e.shape and not dw.any()
+
+
+def test_infinity_outside_the_rotated_elements_stays_there():
+    import torch
+    import paper_2606_07713_amd as moa
+    q, _, _, freq, pos, _ = _inputs(1, 1, 1, 4, 64, "f32", 32, 1, (False, False), False, 3)
+    want = moa.qk_norm_rope(q, positions=pos, inv_freq=freq)[0].clone()
+    q[0, 0, 1, 40] = math.inf
+    got = moa.qk_norm_rope(q, positions=pos, inv_freq=freq)[0]
+    want[0, 0, 1, 40] = math.inf
+    assert torch.equal(got, want)
+
+
+def test_captured_call_replays():
+    import torch
+    import paper_2606_07713_amd as moa
+    q, k, w, freq, pos, _ = _inputs(2, 4, 2, 50, 128, "bf16", 128, 1, (True, True), False, 3)
+    gy = [torch.randn(x.shape, device="cuda").to(torch.bfloat16) for x in (q, k)]
+    how = dict(positions=pos, inv_freq=freq, q_weight=w[0], k_weight=w[1])
+
+    def call():
+        return (*moa.qk_norm_rope(q, k, **how), *moa.qk_norm_rope_bwd(q, k, *gy, **how))
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for rep in range(3):
+        q.copy_(torch.randn(q.shape, generator=torch.Generator().manual_seed(rep)).to(q))
+        want = call()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b), f"replay {rep}"
