@@ -11,7 +11,9 @@ wrapper for torch tensors (torch supplies device memory and the stream).
 
 What stands around the attention of a model has modules of its own, with their
 names here as well: ``rope`` (``include/moa_rope.h``: norms of queries and keys
-for each head with the rotation by position, and the gradients).
+for each head with the rotation by position, and the gradients) and ``kv4``
+(``include/moa_kv4.h``: a key/value cache held in four bits and the attention
+over it).
 
 There is no fallback: if the HIP library has not been built, importing this
 package raises ``ImportError``.
@@ -32,6 +34,9 @@ __all__ = [
     "moa_attn_fwd_noalloc", "MOA_ERR_SCRATCH", "MOA_NOALLOC_SCRATCH_BYTES", "moa_attn_fwd_onf",
     "moa_qk_norm_rope", "moa_qk_norm_rope_bwd", "moa_qk_norm_rope_bwd_workspace_bytes",
     "qk_norm_rope", "qk_norm_rope_bwd",
+    "moa_kv4_page_bytes", "moa_kv4_write", "moa_kv4_read", "moa_kv4_attn_fwd",
+    "moa_kv4_attn_num_splits", "moa_kv4_attn_workspace_bytes",
+    "kv4_cache", "kv4_write", "kv4_read", "kv4_attn_fwd",
 ]
 
 MOA_OK, MOA_ERR_INVALID_ARG, MOA_ERR_UNSUPPORTED, MOA_ERR_WORKSPACE, MOA_ERR_HIP = 0, 1, 2, 3, 4
@@ -375,3 +380,6 @@ def attn_fwd_proj(x, wq, wk, wv, heads, scale=None, causal=False, out_dtype=None
 from .rope import (  # noqa: E402
     moa_qk_norm_rope, moa_qk_norm_rope_bwd, moa_qk_norm_rope_bwd_workspace_bytes, qk_norm_rope,
     qk_norm_rope_bwd)
+from .kv4 import (  # noqa: E402
+    kv4_attn_fwd, kv4_cache, kv4_read, kv4_write, moa_kv4_attn_fwd, moa_kv4_attn_num_splits,
+    moa_kv4_attn_workspace_bytes, moa_kv4_page_bytes, moa_kv4_read, moa_kv4_write)

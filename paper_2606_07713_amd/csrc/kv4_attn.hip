@@ -1,0 +1,473 @@
+// Attention over the four-bit cache (moa_kv4.h).
+//
+// A workgroup takes RT tiles of 16 rows of one key/value head -- a row is a
+// query and one of the G = Hq/Hk heads that share the stored head, query by
+// query -- over a range of keys; its four waves take the range's 64-key tiles
+// in turn, each with a softmax state of its own, and join them at the end.
+//
+// The codes go from memory to registers in the order in which the matrix
+// instruction takes them, without LDS: for S^T = K Q^T a lane holds 32 (16 at
+// d = 64) successive elements of a key, its part of a wave-wide read of whole
+// rows; for O^T += V^T P^T it holds, of every four keys, the elements d/16 c ..
+// of its column c.  One v_cvt_scalef32_pk_bf16_fp4 makes two bf16 of a byte and
+// their power of two, exactly.  The S^T accumulators leave a lane with the four
+// keys 16 t + 4 g .. of row n = lane % 16 -- and since the order of the keys
+// in a product is free, two such accumulators, packed to bf16, are the B
+// operand of the second product as they are.
+//
+// Softmax: running reference m per row (raised only when a tile's maximum is
+// more than 8 log2 units above it, for the whole wave at once), fp32 sums of
+// the unrounded weights per lane, joined over the lanes once at the end.
+#include <limits>
+
+#include "kv4_common.h"
+#include "prefill_bf16_common.h"
+
+namespace moa {
+namespace {
+
+using namespace kv4;
+
+constexpr int WAVES = 4;
+constexpr float kLift = 8.0f;   // log2 units that weights may grow above the reference
+
+// Max over the four lanes with the same lane % 16.
+__device__ __forceinline__ float column_max(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return half_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float column_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const bf16x2 t = {(__bf16)lo, (__bf16)hi};
+    return __builtin_bit_cast(uint32_t, t);
+}
+
+template <int B>
+__device__ __forceinline__ uint32_t values2(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B));
+}
+
+// Eight successive elements of a key.
+__device__ __forceinline__ bf16x8 key8(uint32_t w, float scale) {
+    const uint4 r = make_uint4(values2<0>(w, scale), values2<1>(w, scale), values2<2>(w, scale), values2<3>(w, scale));
+    return __builtin_bit_cast(bf16x8, r);
+}
+
+// Four bytes per scale, in the order of the keys.
+template <int I>
+__device__ __forceinline__ float scale_byte(uint32_t w) { return scale_of((w >> (8 * I)) & 255u); }
+
+// One 64-key tile's codes and scales of one lane.
+template <int D>
+struct Tile {
+    uint32_t k[4][D / 32], v[4][D / 32];   // [16-key group][dwords]
+    uint32_t ks, vs[4];
+
+    __device__ __forceinline__ void load(const unsigned char* head, int page, int in, int lane) {
+        const int r = lane & 15, g = lane >> 4;
+        const unsigned char* kc = head + in * 32 * D;
+        const unsigned char* vc = head + val_codes(page, D) + in * 32 * D;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            read(kc + (16 * t + r) * (D / 2) + g * (D / 8), k[t]);
+            read(vc + (4 * t + g) * 2 * D + r * (D / 8), v[t]);
+        }
+        // key scales: of this lane's 32 (16) elements; value scales: of its column
+        constexpr int LANES_PER_BLOCK = D == 128 ? 1 : 2, COLS_PER_BLOCK = D == 128 ? 4 : 8;
+        ks = *reinterpret_cast<const uint32_t*>(head + key_scales(page, D) + in * 2 * D + (g / LANES_PER_BLOCK) * 64 + r * 4);
+        const uint4 s = *reinterpret_cast<const uint4*>(head + val_scales(page, D) + in * 2 * D + (r / COLS_PER_BLOCK) * 64 + g * 16);
+        vs[0] = s.x; vs[1] = s.y; vs[2] = s.z; vs[3] = s.w;
+    }
+    static __device__ __forceinline__ void read(const unsigned char* p, uint32_t (&w)[D / 32]) {
+        if constexpr (D == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(p);
+            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(p);
+            w[0] = x.x; w[1] = x.y;
+        }
+    }
+    // S^T of 16-key group t: 4 keys 16 t + 4 g .. of row lane % 16.
+    template <int T>
+    __device__ __forceinline__ void keys(bf16x8 (&a)[D / 32]) const {
+        const float s = scale_byte<T>(ks);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) a[i] = key8(k[T][i], s);
+    }
+    // V^T operands of the 32 keys of groups 2 U and 2 U + 1 for the column's
+    // D/16 elements.
+    template <int U>
+    __device__ __forceinline__ void values(bf16x8 (&a)[D / 16]) const {
+        uint32_t r[D / 16][4];
+        quad<0>(v[2 * U], vs[2 * U], r);
+        quad<1>(v[2 * U + 1], vs[2 * U + 1], r);
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) a[e] = __builtin_bit_cast(bf16x8, make_uint4(r[e][0], r[e][1], r[e][2], r[e][3]));
+    }
+    template <int H>
+    static __device__ __forceinline__ void quad(const uint32_t (&w)[D / 32], uint32_t s, uint32_t (&r)[D / 16][4]) {
+        const float s0 = scale_byte<0>(s), s1 = scale_byte<1>(s), s2 = scale_byte<2>(s), s3 = scale_byte<3>(s);
+#pragma unroll
+        for (int f = 0; f < D / 64; ++f) {   // four elements: dword 2 f has keys 0, 1, dword 2 f + 1 keys 2, 3
+            pair(w[2 * f], s0, s1, r[4 * f][2 * H], r[4 * f + 1][2 * H], r[4 * f + 2][2 * H], r[4 * f + 3][2 * H]);
+            pair(w[2 * f + 1], s2, s3, r[4 * f][2 * H + 1], r[4 * f + 1][2 * H + 1], r[4 * f + 2][2 * H + 1], r[4 * f + 3][2 * H + 1]);
+        }
+    }
+    static __device__ __forceinline__ void pair(uint32_t w, float sa, float sb, uint32_t& e0, uint32_t& e1, uint32_t& e2, uint32_t& e3) {
+        const uint32_t a01 = values2<0>(w, sa), a23 = values2<1>(w, sa), b01 = values2<2>(w, sb), b23 = values2<3>(w, sb);
+        e0 = __builtin_amdgcn_perm(b01, a01, 0x05040100);
+        e1 = __builtin_amdgcn_perm(b01, a01, 0x07060302);
+        e2 = __builtin_amdgcn_perm(b23, a23, 0x05040100);
+        e3 = __builtin_amdgcn_perm(b23, a23, 0x07060302);
+    }
+    // Value scales that no written block has (255: the block held a NaN; unset
+    // memory) become 2^-127, a finite factor for keys that a row does not see.
+    // Returns those bytes, one bit per key of the lane: bit 4 t + j.
+    __device__ __forceinline__ uint32_t tame() {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (((vs[t] >> (8 * j)) & 255u) > 252u) {
+                    bad |= 1u << (4 * t + j);
+                    vs[t] &= ~(255u << (8 * j));
+                }
+        return bad;
+    }
+};
+
+template <int D, int RT>
+__global__ __launch_bounds__(WAVES * 64) void kv4_attn_kernel(Kv4Attn p, float c, bool flip, int row_tiles) {
+    constexpr int E = D / 16, ROWS = 16 * RT, LD = D + 4;
+    __shared__ __attribute__((aligned(16))) float part[WAVES][ROWS][LD];
+    __shared__ float part_m[WAVES][ROWS], part_l[WAVES][ROWS];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, g = lane >> 4;
+    const Kv4Cache& kc = p.c;
+    const int G = p.hq / kc.hk;
+    int blk = blockIdx.x;
+    const int sp = blk % p.splits; blk /= p.splits;
+    const int rt = blk % row_tiles; blk /= row_tiles;
+    const int h = blk % kc.hk, b = blk / kc.hk;
+
+    const int count = new_tokens(kc, b), rows = count * G, row0 = rt * ROWS;
+    if (row0 >= rows) return;
+    const long long len = kc.seq_lens[b], cap = (long long)kc.max_pages * kc.page;
+    const long long first = len - count;   // position of query 0
+    // A row sees keys 0 .. sees(row) - 1; rows behind the last one are computed
+    // as it is, with queries of zero, and not stored.
+    const auto sees = [&](int row) -> int {
+        const long long s = p.causal ? first + row / G + 1 : len;
+        return (int)max(0ll, min(s, cap));
+    };
+    int seen[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) seen[i] = sees(min(row0 + 16 * i + n, rows - 1));
+    const int most = __builtin_amdgcn_readfirstlane(sees(min(row0 + ROWS, rows) - 1));
+    const int whole = __builtin_amdgcn_readfirstlane(sees(row0)) >> 6;   // tiles below it need no mask
+    const int tiles = (most + 63) >> 6, per = (tiles + p.splits - 1) / p.splits;
+    const int begin = sp * per, end = min(tiles, begin + per);
+
+    bf16x8 q[RT][D / 32];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int row = row0 + 16 * i + n;
+        const bool in = row < rows;
+        const int qi = in ? row / G : 0, hh = h * G + (in ? row - qi * G : 0);
+        const u16* src = static_cast<const u16*>(p.q) + b * p.qs[0] + hh * p.qs[1] + qi * p.qs[2] + g * (D / 4);
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            uint4 w = in ? *reinterpret_cast<const uint4*>(src + 8 * k) : make_uint4(0, 0, 0, 0);
+            if (flip) { w.x ^= 0x80008000u; w.y ^= 0x80008000u; w.z ^= 0x80008000u; w.w ^= 0x80008000u; }
+            q[i][k] = __builtin_bit_cast(bf16x8, w);
+        }
+    }
+
+    f32x4 o[RT][E];
+    float m[RT], l[RT];   // m: reference in raw score units, -inf before the first visible key
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        m[i] = kNegInf;
+        l[i] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[i][e] = f32x4{0, 0, 0, 0};
+    }
+    const float lift = kLift / c;
+
+    const int tpp = kc.page >> 6;   // tiles per page
+    int t = begin + wave, index = t / tpp, in = t - index * tpp;
+    for (; t < end; t += WAVES, in += WAVES) {
+        while (in >= tpp) { in -= tpp; ++index; }
+        const unsigned char* head = page_of(kc, b, h, index);
+        if (!head) continue;
+        Tile<D> tile;
+        tile.load(head, kc.page, in, lane);
+
+        f32x4 s[RT][4];
+        const auto score = [&](auto T) {
+            bf16x8 a[D / 32];
+            tile.template keys<decltype(T)::value>(a);
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < D / 32; ++k) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[k], q[i][k], x, 0, 0, 0);
+                s[i][decltype(T)::value] = x;
+            }
+        };
+        score(std::integral_constant<int, 0>{});
+        score(std::integral_constant<int, 1>{});
+        score(std::integral_constant<int, 2>{});
+        score(std::integral_constant<int, 3>{});
+
+        uint32_t bad = 0;
+        const bool masked = t >= whole;
+        if (masked) {
+            bad = tile.tame();
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (64 * t + 16 * u + 4 * g + j >= seen[i]) s[i][u][j] = kNegInf;
+        }
+
+        float top[RT];
+        bool raise = false;
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            float x = kNegInf;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x = fmaxf(x, s[i][u][j]);
+            top[i] = column_max(x);
+            raise |= m[i] == kNegInf ? top[i] > kNegInf : top[i] > m[i] + lift;
+        }
+        if (wave_any(raise)) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const float m_new = fmaxf(m[i], top[i]);
+                const float a = m[i] == kNegInf ? 0.0f : exp2_hw((m[i] - m_new) * c);
+                m[i] = m_new;
+                l[i] *= a;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[i][e] *= a;
+            }
+        }
+        bf16x8 pt[RT][2];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const float mc = m[i] == kNegInf ? 0.0f : m[i] * c;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[i][u][j] = exp2_hw(__builtin_fmaf(s[i][u][j], c, -mc));
+                    l[i] += s[i][u][j];
+                }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                pt[i][u] = __builtin_bit_cast(bf16x8, make_uint4(pack2(s[i][2 * u][0], s[i][2 * u][1]), pack2(s[i][2 * u][2], s[i][2 * u][3]),
+                                                                 pack2(s[i][2 * u + 1][0], s[i][2 * u + 1][1]), pack2(s[i][2 * u + 1][2], s[i][2 * u + 1][3])));
+        }
+        const auto product = [&](auto U) {
+            constexpr int u = decltype(U)::value;
+            bf16x8 a[E];
+            tile.template values<u>(a);
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[i][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[e], pt[i][u], o[i][e], 0, 0, 0);
+        };
+        product(std::integral_constant<int, 0>{});
+        product(std::integral_constant<int, 1>{});
+
+        // A masked tile with blocks that hold a NaN: their elements become NaN
+        // in the rows that see the key, counted by a product of ones.
+        if (masked && wave_any(bad != 0)) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                uint32_t va[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int at = 4 * (2 * u + k / 2) + 2 * (k % 2);
+                    va[k] = ((bad >> at) & 1u ? 0x3f80u : 0u) | ((bad >> (at + 1)) & 1u ? 0x3f800000u : 0u);
+                }
+                const bf16x8 a = __builtin_bit_cast(bf16x8, make_uint4(va[0], va[1], va[2], va[3]));
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    uint32_t vb[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int key = 64 * t + 16 * (2 * u + k / 2) + 4 * g + 2 * (k % 2);
+                        vb[k] = (key < seen[i] ? 0x3f80u : 0u) | (key + 1 < seen[i] ? 0x3f800000u : 0u);
+                    }
+                    f32x4 hit = {0, 0, 0, 0};
+                    hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, make_uint4(vb[0], vb[1], vb[2], vb[3])), hit, 0, 0, 0);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (hit[j] > 0.0f)
+#pragma unroll
+                            for (int e = 0; e < E; ++e) o[i][e][j] = __builtin_nanf("");
+                }
+            }
+        }
+    }
+
+    // Join the waves' states: a common reference per row, then sums.
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        l[i] = column_sum(l[i]);
+        if (g == 0) part_m[wave][16 * i + n] = m[i] == kNegInf ? kNegInf : m[i] * c;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int row = 16 * i + n;
+        float M = kNegInf;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) M = fmaxf(M, part_m[w][row]);
+        const float a = m[i] == kNegInf ? 0.0f : exp2_hw(m[i] * c - M);
+        if (g == 0) part_l[wave][row] = l[i] * a;
+        // column 4 g + j of the wave's O^T: elements E (4 g + j) + e of the row
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < E; e += 4)
+                *reinterpret_cast<float4*>(&part[wave][row][E * (4 * g + j) + e]) =
+                    make_float4(o[i][e][j] * a, o[i][e + 1][j] * a, o[i][e + 2][j] * a, o[i][e + 3][j] * a);
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < ROWS * (D / 8); x += WAVES * 64) {
+        const int r = x / (D / 8), d8 = (x % (D / 8)) * 8, row = row0 + r;
+        if (row >= rows) break;
+        float f[8], L = 0.0f, M = kNegInf;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            M = fmaxf(M, part_m[w][r]);
+            L += part_l[w][r];
+            const float4 u = *reinterpret_cast<const float4*>(&part[w][r][d8]), v = *reinterpret_cast<const float4*>(&part[w][r][d8 + 4]);
+            f[0] += u.x; f[1] += u.y; f[2] += u.z; f[3] += u.w;
+            f[4] += v.x; f[5] += v.y; f[6] += v.z; f[7] += v.w;
+        }
+        const int qi = row / G, hh = h * G + row - qi * G;
+        const size_t at = ((size_t)b * p.hq + hh) * kc.n + qi;
+        if (p.splits > 1) {
+            float* acc = p.ws + (at * p.splits + sp) * D + d8;
+            reinterpret_cast<float4*>(acc)[0] = make_float4(f[0], f[1], f[2], f[3]);
+            reinterpret_cast<float4*>(acc)[1] = make_float4(f[4], f[5], f[6], f[7]);
+            if (d8 == 0) {
+                float* ml = p.ws + (size_t)kc.B * p.hq * kc.n * p.splits * D + (at * p.splits + sp) * 2;
+                ml[0] = M;
+                ml[1] = L;
+            }
+            continue;
+        }
+        // no visible key: a sum of 0 (a row whose scores are all NaN has a NaN sum)
+        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+        const long long to = b * p.os[0] + hh * p.os[1] + qi * p.os[2] + d8;
+        if (p.out_bf16) {
+            *reinterpret_cast<uint4*>(static_cast<u16*>(p.o) + to) =
+                make_uint4(pack2(f[0] * inv, f[1] * inv), pack2(f[2] * inv, f[3] * inv), pack2(f[4] * inv, f[5] * inv), pack2(f[6] * inv, f[7] * inv));
+        } else {
+            float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.o) + to);
+            dst[0] = make_float4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+            dst[1] = make_float4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv);
+        }
+        if (p.lse && d8 == 0) p.lse[at] = L == 0.0f ? kNegInf : (M + __log2f(L)) * kLn2;
+    }
+}
+
+// Exact join of a row's key splits, one wave per row; splits without a visible
+// key have a sum of 0.
+template <int D>
+__global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Attn p) {
+    constexpr int PER = D / 64, U = 8;
+    const Kv4Cache& kc = p.c;
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (row >= (long long)kc.B * p.hq * kc.n) return;
+    const int i = (int)(row % kc.n);
+    const long long bh = row / kc.n;
+    const int b = (int)(bh / p.hq), hh = (int)(bh - (long long)b * p.hq);
+    if (i >= new_tokens(kc, b)) return;
+    const float* acc = p.ws + (size_t)row * p.splits * D;
+    const float* ml = p.ws + (size_t)kc.B * p.hq * kc.n * p.splits * D + (size_t)row * p.splits * 2;
+    float M = kNegInf, L = 0.0f, o[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] = 0.0f;
+    for (int s0 = 0; s0 < p.splits; s0 += U) {
+        float ms[U], ls[U], a[U][PER], top = M;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = min(s0 + u, p.splits - 1);
+            ms[u] = s0 + u < p.splits ? ml[2 * s] : kNegInf;
+            ls[u] = s0 + u < p.splits ? ml[2 * s + 1] : 0.0f;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) a[u][e] = acc[(size_t)s * D + e * 64 + lane];
+            top = fmaxf(top, ms[u]);
+        }
+        const float alpha = M == kNegInf ? 0.0f : exp2_hw(M - top);
+        M = top;
+        L *= alpha;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) o[e] *= alpha;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (ls[u] == 0.0f) continue;
+            const float w = exp2_hw(ms[u] - M);
+            L += w * ls[u];
+#pragma unroll
+            for (int e = 0; e < PER; ++e) o[e] += w * a[u][e];
+        }
+    }
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    const long long to = b * p.os[0] + hh * p.os[1] + i * p.os[2];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        if (p.out_bf16)
+            static_cast<__bf16*>(p.o)[to + e * 64 + lane] = (__bf16)(o[e] * inv);
+        else
+            static_cast<float*>(p.o)[to + e * 64 + lane] = o[e] * inv;
+    }
+    if (p.lse && lane == 0) p.lse[row] = L == 0.0f ? kNegInf : (M + __log2f(L)) * kLn2;
+}
+
+template <int D, int RT>
+hipError_t go(const Kv4Attn& p, hipStream_t stream) {
+    const int rows = p.c.n * (p.hq / p.c.hk), tiles = (rows + 16 * RT - 1) / (16 * RT);
+    // A negative scale goes into the queries' signs; a factor of zero (or below
+    // the normal numbers) becomes the smallest normal one, whose weights round
+    // to 1 as well, so that masked scores keep the weight 0.
+    float c = p.scale * kLog2e;
+    const bool flip = c < 0.0f;
+    c = flip ? -c : c;
+    if (c < std::numeric_limits<float>::min()) c = std::numeric_limits<float>::min();
+    const long long blocks = (long long)p.c.B * p.c.hk * tiles * p.splits;
+    hipError_t e = launch_kernel(kv4_attn_kernel<D, RT>, dim3((unsigned)blocks), dim3(WAVES * 64), stream, p, c, flip, tiles);
+    if (e != hipSuccess || p.splits == 1) return e;
+    const long long all = (long long)p.c.B * p.hq * p.c.n;
+    return launch_kernel(kv4_combine_kernel<D>, dim3((unsigned)((all + 3) / 4)), dim3(256), stream, p);
+}
+
+}  // namespace
+
+int kv4_rows_per_block(int rows) { return rows <= 16 ? 16 : 32; }
+
+hipError_t launch_kv4_attn(const Kv4Attn& p, hipStream_t stream) {
+    const bool one = kv4_rows_per_block(p.c.n * (p.hq / p.c.hk)) == 16;
+    if (p.c.d == 64) return one ? go<64, 1>(p, stream) : go<64, 2>(p, stream);
+    return one ? go<128, 1>(p, stream) : go<128, 2>(p, stream);
+}
+
+}  // namespace moa
