@@ -53,8 +53,8 @@ size_t moa_kv4_page_bytes(int64_t page, int64_t d);
  *
  * K, V      device inputs of storage type in_dtype (MOA_F32 or MOA_BF16),
  *           logical shape [B][Hk][N][d], element strides (batch, head, row) or
- *           NULL: contiguous; non-negative multiples of 16 bytes.  Rows may
- *           overlap.
+ *           NULL: contiguous; non-negative multiples of 16 bytes (ignored for
+ *           a dimension of size 1).  Rows may overlap.
  * cache     device pool, written: 16-byte aligned, num_pages * Hk *
  *           moa_kv4_page_bytes(page, d) bytes, overlapping nothing else.
  * seq_lens, new_lens, page_table

@@ -41,7 +41,8 @@ extern "C" {
  *           multiple of 16 up to d, B * (Hq + Hk) * N < 2^31.
  * *_strides element strides (batch, head, row) as for moa_attn_fwd_strided, or
  *           NULL: contiguous.  Non-negative, multiples of 16 bytes; an output
- *           must not write an element twice.  Input rows may overlap.
+ *           must not write an element twice.  Input rows may overlap.  The
+ *           stride of a dimension of size 1 is ignored.
  * axes, sections
  *           1 to 4 position axes.  sections (HOST array of axes values >= 0 with
  *           sum rot/2; NULL when axes == 1): the first sections[0] pairs turn by

@@ -56,8 +56,9 @@ int check_tensor(const void* p, const Strides& s, int64_t B, int64_t H, int64_t 
     return MOA_OK;
 }
 
-Strides strides_of(const int64_t* s, int64_t H, int64_t N, int64_t d) {
-    return s ? Strides{s[0], s[1], s[2]} : contiguous(H, N, d);
+// A dimension of size 1 has no stride to keep to.
+Strides strides_of(const int64_t* s, int64_t B, int64_t H, int64_t N, int64_t d) {
+    return s ? Strides{B > 1 ? s[0] : 0, H > 1 ? s[1] : 0, N > 1 ? s[2] : 0} : contiguous(H, N, d);
 }
 
 struct Buf {
@@ -131,7 +132,7 @@ int moa_kv4_write(const void* K, const void* V, void* cache, const int32_t* seq_
     int st = check_dims(s);
     if (st) return st;
     const size_t es = in_dtype == MOA_F32 ? 4 : 2;
-    const Strides sk = strides_of(k_strides, Hk, N, d), sv = strides_of(v_strides, Hk, N, d);
+    const Strides sk = strides_of(k_strides, B, Hk, N, d), sv = strides_of(v_strides, B, Hk, N, d);
     if ((st = check_tensor(K, sk, B, Hk, N, d, es, false)) || (st = check_tensor(V, sv, B, Hk, N, d, es, false))) return st;
     if (!s.any() || num_pages == 0) return MOA_OK;
     const Buf pool{cache, s.cache_bytes()};
@@ -155,7 +156,7 @@ int moa_kv4_read(const void* cache, void* K, void* V, const int32_t* seq_lens,
     int st = check_dims(s);
     if (st) return st;
     const size_t es = out_dtype == MOA_F32 ? 4 : 2;
-    const Strides sk = strides_of(k_strides, Hk, N, d), sv = strides_of(v_strides, Hk, N, d);
+    const Strides sk = strides_of(k_strides, B, Hk, N, d), sv = strides_of(v_strides, B, Hk, N, d);
     if ((st = check_tensor(K, sk, B, Hk, N, d, es, true)) || (st = check_tensor(V, sv, B, Hk, N, d, es, true))) return st;
     if (!s.any() || num_pages == 0) return MOA_OK;
     const Buf pool{cache, s.cache_bytes()}, k{K, extent_bytes(sk, B, Hk, N, d, es)}, v{V, extent_bytes(sv, B, Hk, N, d, es)};
@@ -198,7 +199,7 @@ int moa_kv4_attn_fwd(const void* Q, const void* cache, void* O, float* LSE, cons
     int st = check_dims(s);
     if (st) return st;
     if (!attn_sizes_ok(B, Hq, Hk, N, d, page, max_pages, max_len, num_splits)) return MOA_ERR_UNSUPPORTED;
-    const Strides sq = strides_of(q_strides, Hq, N, d), so = strides_of(o_strides, Hq, N, d);
+    const Strides sq = strides_of(q_strides, B, Hq, N, d), so = strides_of(o_strides, B, Hq, N, d);
     const size_t oes = out_dtype == MOA_F32 ? 4 : 2;
     if ((st = check_tensor(Q, sq, B, Hq, N, d, 2, false)) || (st = check_tensor(O, so, B, Hq, N, d, oes, true))) return st;
     if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(LSE) & 3)) return MOA_ERR_INVALID_ARG;

@@ -102,8 +102,9 @@ bool same(const View& a, const View& b) {
     return a.p == b.p && a.s.b == b.s.b && a.s.h == b.s.h && a.s.r == b.s.r;
 }
 
+// A dimension of size 1 has no stride to keep to.
 Strides strides_of(const int64_t* s, int64_t H, const Common& c) {
-    return s ? Strides{s[0], s[1], s[2]} : contiguous(H, c.N, c.d);
+    return s ? Strides{c.B > 1 ? s[0] : 0, H > 1 ? s[1] : 0, c.N > 1 ? s[2] : 0} : contiguous(H, c.N, c.d);
 }
 
 // Outputs against every input and each other; out[i] may be its own in[i].

@@ -3,59 +3,81 @@ from __future__ import annotations
 
 import torch
 
-from . import _DTYPE_CODES
-from ._call import (array, check_list, check_rows, ci, done, f32, function, handle, i64, on, ptr, same_device,
-                    strides, sz, vp)
+from . import MOA_F32, _DTYPE_CODES, _stream_handle
+from ._call import (Function, Strides12, Strides18, addressof, array, check_list, check_rows, ci, f32, i64, is_list, run,
+                    sz, vp, workspace as _workspace)
 
-_ARGS = [i64] * 6
-moa_qk_norm_rope = function(
+_SIZES = [i64] * 6
+moa_qk_norm_rope = Function(
     "moa_qk_norm_rope",
-    [vp] * 8 + _ARGS + [vp] * 4 + [ci, vp, ci, f32, ci, ci, vp])
-moa_qk_norm_rope_bwd = function(
+    [vp] * 8 + _SIZES + [vp] * 4 + [ci, vp, ci, f32, ci, ci, vp])
+moa_qk_norm_rope_bwd = Function(
     "moa_qk_norm_rope_bwd",
-    [vp] * 12 + _ARGS + [vp] * 6 + [ci, vp, ci, f32, ci, ci, vp, sz, vp])
-moa_qk_norm_rope_bwd_workspace_bytes = function("moa_qk_norm_rope_bwd_workspace_bytes", [i64] * 5, sz)
+    [vp] * 12 + _SIZES + [vp] * 6 + [ci, vp, ci, f32, ci, ci, vp, sz, vp])
+moa_qk_norm_rope_bwd_workspace_bytes = Function("moa_qk_norm_rope_bwd_workspace_bytes", [i64] * 5, sz)
+
+_int64, _float32 = torch.int64, torch.float32
+
+
+def _like(name, t, x, shape, device):
+    """t is a tensor like x: its strides."""
+    s = t.stride()
+    if t.shape != shape or t.dtype is not x.dtype or t.get_device() != device or s[-1] != 1:
+        check_rows(name, t, shape, x.dtype, device)
+    return s
+
+
+def _weight(name, w, d, device):
+    if w.dtype not in _DTYPE_CODES or not is_list(w, (d,), w.dtype, device):
+        if w.dtype not in _DTYPE_CODES:
+            raise TypeError(f"{name}: unsupported dtype {w.dtype}; use torch.float32 or torch.bfloat16")
+        check_list(name, w, (d,), w.dtype, device)
+    return _DTYPE_CODES[w.dtype]
 
 
 def _common(q, k, positions, inv_freq, q_weight, k_weight, sections):
-    """Checks what forward and backward share: (B, Hq, Hk, N, d, rot, axes, weight type)."""
-    check_rows("q", q)
-    B, Hq, N, d = q.shape
-    Hk = 0
+    """Checks what forward and backward share.  (shape of q, of k, strides of q, of k, device,
+    rot, axes, host array of the sections, weight type, addresses)."""
+    qn = q.shape
+    device = q.get_device()
+    qs = q.stride()
+    if len(qn) != 4 or device < 0 or q.dtype not in _DTYPE_CODES or qs[3] != 1:
+        check_rows("q", q)
+    B, _, N, d = qn
+    kn, ks, kp = (B, 0, N, d), (0, 0, 0), None
     if k is not None:
-        check_rows("k", k, (B, k.shape[1] if k.dim() == 4 else -1, N, d))
-        Hk = k.shape[1]
-        if k.dtype != q.dtype:
-            raise TypeError("q and k must share one dtype")
+        kn = k.shape
+        if len(kn) != 4 or kn[0] != B or kn[2] != N or kn[3] != d:
+            raise ValueError(f"k must be [B, Hk, N, d] with q's B, N and d, got {tuple(kn)} for {tuple(qn)}")
+        ks = _like("k", k, q, kn, device)
+        kp = k.data_ptr()
     elif k_weight is not None:
         raise ValueError("k_weight without k")
-    device = same_device(q, k, positions, inv_freq, q_weight, k_weight)
-    wdt = None
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is None:
-            continue
-        if w.dtype not in _DTYPE_CODES or (wdt is not None and w.dtype != wdt):
-            raise TypeError("q_weight and k_weight must both be torch.float32 or both torch.bfloat16")
-        wdt = w.dtype
-        check_list(name, w, (d,), wdt, device)
-    rot = 0
+    wcode, wq, wk = MOA_F32, None, None
+    if q_weight is not None:
+        wcode = _weight("q_weight", q_weight, d, device)
+        wq = q_weight.data_ptr()
+    if k_weight is not None:
+        code = _weight("k_weight", k_weight, d, device)
+        if wq is not None and code != wcode:
+            raise TypeError("q_weight and k_weight must share one dtype")
+        wcode, wk = code, k_weight.data_ptr()
+    rot, freq = 0, None
     if inv_freq is not None:
-        rot = 2 * inv_freq.numel()
-        check_list("inv_freq", inv_freq, (rot // 2,), torch.float32, device)
-    axes = 1 if sections is None else len(sections)
+        n = inv_freq.shape[0] if inv_freq.dim() == 1 else -1
+        if not is_list(inv_freq, (n,), _float32, device):
+            check_list("inv_freq", inv_freq, (n,), _float32, device)
+        rot, freq = 2 * n, inv_freq.data_ptr()
+    axes, sec = 1, None
+    if sections is not None:
+        axes, sec = len(sections), array(sections)
+    pos = None
     if positions is not None:
         shape = (B, N) if sections is None else (axes, B, N)
-        check_list("positions", positions, shape, torch.int64, device)
-    return B, Hq, Hk, N, d, rot, axes, 0 if wdt is None else _DTYPE_CODES[wdt]
-
-
-def _output(name, out, like):
-    if out is None:
-        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
-    check_rows(name, out, like.shape)
-    if out.dtype != like.dtype or out.device != like.device:
-        raise ValueError(f"{name} must have the input's dtype and device")
-    return out
+        if not is_list(positions, shape, _int64, device):
+            check_list("positions", positions, shape, _int64, device)
+        pos = positions.data_ptr()
+    return qn, kn, qs, ks, device, rot, axes, sec, wcode, (q.data_ptr(), kp, wq, wk, pos, freq)
 
 
 def qk_norm_rope(q, k=None, positions=None, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6,
@@ -71,15 +93,23 @@ def qk_norm_rope(q, k=None, positions=None, inv_freq=None, q_weight=None, k_weig
     or (2i, 2i + 1) when ``interleaved``.  ``q_out`` and ``k_out`` may be q and k (in place).
     Returns (q_out, k_out).  Raises ``MoaAttnError`` on a rejected call.
     """
-    B, Hq, Hk, N, d, rot, axes, wcode = _common(q, k, positions, inv_freq, q_weight, k_weight, sections)
-    qo = _output("q_out", q_out, q)
-    ko = None if k is None else _output("k_out", k_out, k)
-    with on(q.device):
-        done(moa_qk_norm_rope(q.data_ptr(), ptr(k), qo.data_ptr(), ptr(ko), ptr(q_weight), ptr(k_weight),
-                              ptr(positions), ptr(inv_freq), B, Hq, Hk, N, d, rot, strides(q), strides(k),
-                              strides(qo), strides(ko), axes, array(sections), int(interleaved), float(eps),
-                              _DTYPE_CODES[q.dtype], wcode, handle(stream, q)))
-    return qo, ko
+    qn, kn, qs, ks, device, rot, axes, sec, wcode, (qp, kp, wq, wk, pos, freq) = _common(
+        q, k, positions, inv_freq, q_weight, k_weight, sections)
+    if q_out is None:
+        q_out = q.new_empty(qn)
+    qos = _like("q_out", q_out, q, qn, device)
+    kos, kop = ks, None
+    if k is not None:
+        if k_out is None:
+            k_out = k.new_empty(kn)
+        kos, kop = _like("k_out", k_out, k, kn, device), k_out.data_ptr()
+    B, Hq, N, d = qn
+    strides = Strides12(*qs[:3], *ks[:3], *qos[:3], *kos[:3])
+    at = addressof(strides)   # eight bytes each
+    run(moa_qk_norm_rope, device, (
+        qp, kp, q_out.data_ptr(), kop, wq, wk, pos, freq, B, Hq, kn[1], N, d, rot, at, at + 24, at + 48, at + 72, axes,
+        sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, _stream_handle(stream, q)))
+    return q_out, (None if k is None else k_out)
 
 
 def qk_norm_rope_bwd(q, k, dq_out, dk_out, positions=None, inv_freq=None, q_weight=None, k_weight=None,
@@ -89,29 +119,30 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, positions=None, inv_freq=None, q_weig
     the gradients of its outputs (k and dk_out may be None).  dq and dk have q's dtype and may be
     given (also dq_out and dk_out themselves); the weights' gradients are fp32 [d], None where
     there is no weight.  The other arguments must be the forward's."""
-    B, Hq, Hk, N, d, rot, axes, wcode = _common(q, k, positions, inv_freq, q_weight, k_weight, sections)
+    qn, kn, qs, ks, device, rot, axes, sec, wcode, (qp, kp, wq, wk, pos, freq) = _common(
+        q, k, positions, inv_freq, q_weight, k_weight, sections)
     if (k is None) != (dk_out is None):
         raise ValueError("k and dk_out go together")
-    for name, g, x in (("dq_out", dq_out, q), ("dk_out", dk_out, k)):
-        if x is None:
-            continue
-        check_rows(name, g, x.shape)
-        if g.dtype != x.dtype or g.device != x.device:
-            raise ValueError(f"{name} must have the input's dtype and device")
-    dq = _output("dq", dq, q)
-    dk = None if k is None else _output("dk", dk, k)
-    dwq = None if q_weight is None else torch.empty(d, dtype=torch.float32, device=q.device)
-    dwk = None if k_weight is None else torch.empty(d, dtype=torch.float32, device=q.device)
-    if workspace is None and (dwq is not None or dwk is not None):
-        n = moa_qk_norm_rope_bwd_workspace_bytes(B, Hq, Hk, N, d)
+    if dq is None:
+        dq = q.new_empty(qn)
+    gqs, dqs = _like("dq_out", dq_out, q, qn, device), _like("dq", dq, q, qn, device)
+    gks, dks, gkp, dkp = ks, ks, None, None
+    if k is not None:
+        if dk is None:
+            dk = k.new_empty(kn)
+        gks, dks = _like("dk_out", dk_out, k, kn, device), _like("dk", dk, k, kn, device)
+        gkp, dkp = dk_out.data_ptr(), dk.data_ptr()
+    B, Hq, N, d = qn
+    dwq = None if wq is None else torch.empty(d, dtype=_float32, device=q.device)
+    dwk = None if wk is None else torch.empty(d, dtype=_float32, device=q.device)
+    if workspace is None and (wq is not None or wk is not None):
+        n = moa_qk_norm_rope_bwd_workspace_bytes(B, Hq, kn[1], N, d)
         workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
-    same_device(q, workspace)
-    ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    with on(q.device):
-        done(moa_qk_norm_rope_bwd(q.data_ptr(), ptr(k), dq_out.data_ptr(), ptr(dk_out), ptr(q_weight),
-                                  ptr(k_weight), ptr(positions), ptr(inv_freq), dq.data_ptr(), ptr(dk),
-                                  ptr(dwq), ptr(dwk), B, Hq, Hk, N, d, rot, strides(q), strides(k),
-                                  strides(dq_out), strides(dk_out), strides(dq), strides(dk), axes,
-                                  array(sections), int(interleaved), float(eps), _DTYPE_CODES[q.dtype],
-                                  wcode, ptr(workspace), ws_n, handle(stream, q)))
-    return dq, dk, dwq, dwk
+    ws, ws_n = _workspace(workspace, device)
+    strides = Strides18(*qs[:3], *ks[:3], *gqs[:3], *gks[:3], *dqs[:3], *dks[:3])
+    at = addressof(strides)   # eight bytes each
+    run(moa_qk_norm_rope_bwd, device, (
+        qp, kp, dq_out.data_ptr(), gkp, wq, wk, pos, freq, dq.data_ptr(), dkp, None if dwq is None else dwq.data_ptr(),
+        None if dwk is None else dwk.data_ptr(), B, Hq, kn[1], N, d, rot, at, at + 24, at + 48, at + 72, at + 96,
+        at + 120, axes, sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, ws, ws_n, _stream_handle(stream, q)))
+    return dq, (None if k is None else dk), dwq, dwk
