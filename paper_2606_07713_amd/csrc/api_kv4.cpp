@@ -93,17 +93,32 @@ Kv4Cache cache_of(const Dims& s) {
 
 void put(long long (&to)[3], const Strides& s) { to[0] = s.b; to[1] = s.h; to[2] = s.r; }
 
-// Key splits of the attention: enough workgroups for the compute units, at
-// least one 64-key tile per wave.
-int pick_splits(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t max_len, int requested) {
+// Key splits of the attention.  A workgroup's four waves take its 64-key tiles
+// in steps of four; starting and ending it costs about two steps, and the
+// second pass about three, one more for every 16 splits and for every 6 MB of
+// partial states.  `wave` workgroups run at a time: one per compute unit where
+// up to 16 rows of d = 128 leave it to the memory, two where a tile is half as
+// large or its work twice (measured, splits:us, 32 heads on 8: one query, 4097
+// keys, d = 128 1:23.7 8:11.3 17:9.1 64:11.4; 16384 1:77 16:12.8 32:11.4 64:14.3;
+// 48 queries of 8192 1:82.8 2:74.5 4:75.6, 64 of them 1:92 2:94; 200 rows of one
+// sequence on 20011 keys 1:123 2:104 5:100 8:108, 512 on 8192 1:83 2:92).
+int pick_splits(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d, int64_t max_len, int requested) {
     if (requested > 0) return requested;
     const int64_t rows = N * (Hq / Hk), per = kv4_rows_per_block((int)rows);
-    const int64_t blocks = B * Hk * ((rows + per - 1) / per);
-    int64_t s = (512 + blocks - 1) / blocks;
-    const int64_t cap = (max_len + 255) / 256;
-    if (s > cap) s = cap;
-    if (s > kMaxSplits) s = kMaxSplits;
-    return s < 1 ? 1 : (int)s;
+    const int64_t blocks = B * Hk * ((rows + per - 1) / per), tiles = (max_len + 63) / 64;
+    const int64_t wave = rows <= 16 && d == 128 ? 256 : 512;
+    const double states = (double)(B * Hq * N) * (double)d * sizeof(float) / 6e6;
+    int best = 1;
+    double least = 0;
+    for (int64_t s = 1; s <= kMaxSplits && s <= tiles && (s == 1 || s * blocks <= 4 * wave); ++s) {
+        const int64_t rounds = (s * blocks + wave - 1) / wave, steps = ((tiles + s - 1) / s + 3) / 4;
+        const double cost = (double)(rounds * (steps + 2)) + (s > 1 ? 3 + (double)s / 16 + (double)s * states : 0);
+        if (s == 1 || cost < least) {
+            best = (int)s;
+            least = cost;
+        }
+    }
+    return best;
 }
 
 bool attn_sizes_ok(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d, int64_t page, int64_t max_pages,
@@ -112,6 +127,12 @@ bool attn_sizes_ok(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d, int6
     if (num_splits < 0 || num_splits > kMaxSplits || !moa_kv4_page_bytes(page, d)) return false;
     if (B > kLim || Hq > kLim || N > kLim / kMaxSplits - 64 || max_pages > kLim / page) return false;
     return B * Hq <= kLim && (B * Hq == 0 || (N + 64) * kMaxSplits <= kLim / (B * Hq));
+}
+
+// Partial states of a call with these splits (none with one).
+size_t states_bytes(int64_t B, int64_t Hq, int64_t N, int64_t d, int splits) {
+    if (splits <= 1) return 0;
+    return align256((size_t)(B * Hq * N) * (size_t)splits * (size_t)(d + 2) * sizeof(float));
 }
 
 }  // namespace
@@ -174,15 +195,13 @@ int moa_kv4_attn_num_splits(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_
                             int64_t max_pages, int64_t max_len, int num_splits) {
     if (!attn_sizes_ok(B, Hq, Hk, N, d, page, max_pages, max_len, num_splits) || B * Hq * N == 0) return 1;
     const int64_t cap = max_pages * page;
-    return pick_splits(B, Hq, Hk, N, max_len > 0 && max_len < cap ? max_len : cap, num_splits);
+    return pick_splits(B, Hq, Hk, N, d, max_len > 0 && max_len < cap ? max_len : cap, num_splits);
 }
 
 size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d,
                                     int64_t page, int64_t max_pages, int64_t max_len,
                                     int num_splits) {
-    const int s = moa_kv4_attn_num_splits(B, Hq, Hk, N, d, page, max_pages, max_len, num_splits);
-    if (s <= 1 || !attn_sizes_ok(B, Hq, Hk, N, d, page, max_pages, max_len, num_splits)) return 0;
-    return align256((size_t)(B * Hq * N) * (size_t)s * (size_t)(d + 2) * sizeof(float));
+    return states_bytes(B, Hq, N, d, moa_kv4_attn_num_splits(B, Hq, Hk, N, d, page, max_pages, max_len, num_splits));
 }
 
 int moa_kv4_attn_fwd(const void* Q, const void* cache, void* O, float* LSE, const int32_t* seq_lens,
@@ -205,7 +224,7 @@ int moa_kv4_attn_fwd(const void* Q, const void* cache, void* O, float* LSE, cons
     if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(LSE) & 3)) return MOA_ERR_INVALID_ARG;
     if (!s.any() || Hq == 0) return MOA_OK;
     const int splits = moa_kv4_attn_num_splits(B, Hq, Hk, N, d, page, max_pages, max_len, num_splits);
-    const size_t need = moa_kv4_attn_workspace_bytes(B, Hq, Hk, N, d, page, max_pages, max_len, num_splits);
+    const size_t need = states_bytes(B, Hq, N, d, splits);
     if (need && (!workspace || workspace_bytes < need)) return MOA_ERR_WORKSPACE;
     const Buf ins[] = {{Q, extent_bytes(sq, B, Hq, N, d, 2)}, {cache, s.cache_bytes()}};
     const Buf outs[] = {{O, extent_bytes(so, B, Hq, N, d, oes)}, {LSE, LSE ? (size_t)(B * Hq * N) * 4 : 0}, {workspace, need}};

@@ -57,12 +57,25 @@ __device__ __forceinline__ bf16x8 key8(uint32_t w, float scale) {
     return __builtin_bit_cast(bf16x8, r);
 }
 
-// Four bytes per scale, in the order of the keys.
+// The power of two of byte I of w.  One instruction for each byte: left to
+// itself the compiler takes a shift and a mask for bytes 0 to 2.
 template <int I>
-__device__ __forceinline__ float scale_byte(uint32_t w) { return scale_of((w >> (8 * I)) & 255u); }
+__device__ __forceinline__ float scale_byte(uint32_t w) {
+    float r;
+    if constexpr (I == 0)
+        asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(r) : "v"(23), "v"(w));
+    else if constexpr (I == 1)
+        asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(r) : "v"(23), "v"(w));
+    else if constexpr (I == 2)
+        asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(r) : "v"(23), "v"(w));
+    else
+        r = scale_of(w >> 24);
+    return r;
+}
 
-// One 64-key tile's codes and scales of one lane.
-template <int D>
+// One 64-key tile's codes and scales of one lane.  ONCE: no other workgroup
+// reads them, so they need not stay in the caches.
+template <int D, bool ONCE>
 struct Tile {
     uint32_t k[4][D / 32], v[4][D / 32];   // [16-key group][dwords]
     uint32_t ks, vs[4];
@@ -83,13 +96,13 @@ struct Tile {
         vs[0] = s.x; vs[1] = s.y; vs[2] = s.z; vs[3] = s.w;
     }
     static __device__ __forceinline__ void read(const unsigned char* p, uint32_t (&w)[D / 32]) {
-        if constexpr (D == 128) {
-            const uint4 x = *reinterpret_cast<const uint4*>(p);
-            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-        } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(p);
-            w[0] = x.x; w[1] = x.y;
-        }
+        typedef uint32_t vec __attribute__((ext_vector_type(D / 32)));
+        const vec* at = reinterpret_cast<const vec*>(p);
+        vec x;
+        if constexpr (ONCE) x = __builtin_nontemporal_load(at);
+        else x = *at;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) w[i] = x[i];
     }
     // S^T of 16-key group t: 4 keys 16 t + 4 g .. of row lane % 16.
     template <int T>
@@ -141,8 +154,8 @@ struct Tile {
     }
 };
 
-template <int D, int RT>
-__global__ __launch_bounds__(WAVES * 64) void kv4_attn_kernel(Kv4Attn p, float c, bool flip, int row_tiles) {
+template <int D, int RT, bool ONCE>
+__global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, float c, bool flip, int row_tiles) {
     constexpr int E = D / 16, ROWS = 16 * RT, LD = D + 4;
     __shared__ __attribute__((aligned(16))) float part[WAVES][ROWS][LD];
     __shared__ float part_m[WAVES][ROWS], part_l[WAVES][ROWS];
@@ -158,7 +171,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_attn_kernel(Kv4Attn p, float c
 
     const int count = new_tokens(kc, b), rows = count * G, row0 = rt * ROWS;
     if (row0 >= rows) return;
-    const long long len = kc.seq_lens[b], cap = (long long)kc.max_pages * kc.page;
+    const long long len = kc.seq_lens[b], cap = kc.num_pages ? (long long)kc.max_pages * kc.page : 0;
     const long long first = len - count;   // position of query 0
     // A row sees keys 0 .. sees(row) - 1; rows behind the last one are computed
     // as it is, with queries of zero, and not stored.
@@ -201,14 +214,25 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_attn_kernel(Kv4Attn p, float c
     const float lift = kLift / c;
 
     const int tpp = kc.page >> 6;   // tiles per page
-    int t = begin + wave, index = t / tpp, in = t - index * tpp;
-    for (; t < end; t += WAVES, in += WAVES) {
-        while (in >= tpp) { in -= tpp; ++index; }
-        const unsigned char* head = page_of(kc, b, h, index);
-        if (!head) continue;
-        Tile<D> tile;
-        tile.load(head, kc.page, in, lane);
-
+    int at = begin + wave, index = at / tpp, in = at - index * tpp;
+    // Loads the tile at `at` and moves on; false: there is none (no more tiles,
+    // or its page is not in the pool).  Something is loaded in any case, so that
+    // the number of loads in flight is known where a tile's own are waited for:
+    // with loads on one side of a branch every wait was for all of them.
+    const auto fetch = [&](Tile<D, ONCE>& tile) -> bool {
+        const unsigned char* head = nullptr;
+        int tile_in = 0;
+        if (at < end) {
+            while (in >= tpp) { in -= tpp; ++index; }
+            head = page_of(kc, b, h, index);
+            tile_in = head ? in : 0;
+        }
+        tile.load(head ? head : kc.base + (size_t)h * kc.page_bytes, kc.page, tile_in, lane);
+        at += WAVES;
+        in += WAVES;
+        return head != nullptr;
+    };
+    const auto attend = [&](Tile<D, ONCE>& tile, int t) {
         f32x4 s[RT][4];
         const auto score = [&](auto T) {
             bf16x8 a[D / 32];
@@ -320,6 +344,18 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_attn_kernel(Kv4Attn p, float c
                 }
             }
         }
+    };
+    // Two tiles in registers: the next one's loads are in flight while one is
+    // worked on.
+    if (at < end) {
+        Tile<D, ONCE> tile0, tile1;
+        bool have0 = fetch(tile0);
+        for (int t = begin + wave; t < end; t += 2 * WAVES) {
+            const bool have1 = fetch(tile1);
+            if (have0) attend(tile0, t);
+            have0 = fetch(tile0);
+            if (have1) attend(tile1, t + WAVES);
+        }
     }
 
     // Join the waves' states: a common reference per row, then sums.
@@ -388,57 +424,79 @@ __global__ __launch_bounds__(WAVES * 64) void kv4_attn_kernel(Kv4Attn p, float c
     }
 }
 
-// Exact join of a row's key splits, one wave per row; splits without a visible
-// key have a sum of 0.
-template <int D>
+// Exact join of a row's key splits; splits without a visible key have a sum of
+// 0.  The pass is a chain of load latencies, so W waves share a row (1, or 4
+// for more than 4 splits), each takes U of its splits at a time, and all of
+// these loads are in flight together: up to 32 splits cost one latency.
+template <int D, int W>
 __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Attn p) {
-    constexpr int PER = D / 64, U = 8;
+    constexpr int PER = D / 64, U = W == 1 ? 4 : 8;
+    typedef float vec __attribute__((ext_vector_type(PER)));
+    __shared__ vec part[4][64];
+    __shared__ float part_m[4], part_l[4];
     const Kv4Cache& kc = p.c;
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const long long row = (long long)blockIdx.x * (4 / W) + (W == 1 ? wave : 0);
     if (row >= (long long)kc.B * p.hq * kc.n) return;
     const int i = (int)(row % kc.n);
     const long long bh = row / kc.n;
     const int b = (int)(bh / p.hq), hh = (int)(bh - (long long)b * p.hq);
-    if (i >= new_tokens(kc, b)) return;
-    const float* acc = p.ws + (size_t)row * p.splits * D;
+    const vec* acc = reinterpret_cast<const vec*>(p.ws + (size_t)row * p.splits * D) + lane;
     const float* ml = p.ws + (size_t)kc.B * p.hq * kc.n * p.splits * D + (size_t)row * p.splits * 2;
-    float M = kNegInf, L = 0.0f, o[PER];
-#pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = 0.0f;
-    for (int s0 = 0; s0 < p.splits; s0 += U) {
-        float ms[U], ls[U], a[U][PER], top = M;
+    float M = kNegInf, L = 0.0f;
+    vec o = 0.0f;
+    for (int s0 = W == 1 ? 0 : wave; s0 < p.splits; s0 += U * W) {
+        float ms[U], ls[U], top = M;
+        vec a[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int s = min(s0 + u, p.splits - 1);
-            ms[u] = s0 + u < p.splits ? ml[2 * s] : kNegInf;
-            ls[u] = s0 + u < p.splits ? ml[2 * s + 1] : 0.0f;
+            const int s = min(s0 + u * W, p.splits - 1);
+            ms[u] = ml[2 * s];
+            ls[u] = ml[2 * s + 1];
+            a[u] = acc[(size_t)s * 64];
+        }
 #pragma unroll
-            for (int e = 0; e < PER; ++e) a[u][e] = acc[(size_t)s * D + e * 64 + lane];
-            top = fmaxf(top, ms[u]);
+        for (int u = 0; u < U; ++u) {
+            if (s0 + u * W >= p.splits) ls[u] = 0.0f;
+            if (ls[u] != 0.0f) top = fmaxf(top, ms[u]);
         }
         const float alpha = M == kNegInf ? 0.0f : exp2_hw(M - top);
         M = top;
         L *= alpha;
-#pragma unroll
-        for (int e = 0; e < PER; ++e) o[e] *= alpha;
+        o *= alpha;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (ls[u] == 0.0f) continue;
             const float w = exp2_hw(ms[u] - M);
             L += w * ls[u];
-#pragma unroll
-            for (int e = 0; e < PER; ++e) o[e] += w * a[u][e];
+            o += w * a[u];
         }
     }
-    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-    const long long to = b * p.os[0] + hh * p.os[1] + i * p.os[2];
+    if (i >= new_tokens(kc, b)) return;   // nothing was written for this row, and nothing is
+    if constexpr (W > 1) {
+        part[wave][lane] = o;
+        if (lane == 0) { part_m[wave] = M; part_l[wave] = L; }
+        __syncthreads();
+        if (wave != 0) return;
+        const float top = fmaxf(fmaxf(part_m[0], part_m[1]), fmaxf(part_m[2], part_m[3]));
+        L = 0.0f;
+        o = 0.0f;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-        if (p.out_bf16)
-            static_cast<__bf16*>(p.o)[to + e * 64 + lane] = (__bf16)(o[e] * inv);
-        else
-            static_cast<float*>(p.o)[to + e * 64 + lane] = o[e] * inv;
+        for (int w = 0; w < 4; ++w) {
+            if (part_l[w] == 0.0f) continue;
+            const float f = exp2_hw(part_m[w] - top);
+            L += f * part_l[w];
+            o += f * part[w][lane];
+        }
+        M = top;
+    }
+    o *= L == 0.0f ? 0.0f : 1.0f / L;
+    const long long to = b * p.os[0] + hh * p.os[1] + i * p.os[2] + PER * lane;
+    if (p.out_bf16) {
+        typedef __bf16 out __attribute__((ext_vector_type(PER)));
+        *reinterpret_cast<out*>(static_cast<__bf16*>(p.o) + to) = __builtin_convertvector(o, out);
+    } else {
+        *reinterpret_cast<vec*>(static_cast<float*>(p.o) + to) = o;
     }
     if (p.lse && lane == 0) p.lse[row] = L == 0.0f ? kNegInf : (M + __log2f(L)) * kLn2;
 }
@@ -454,10 +512,14 @@ hipError_t go(const Kv4Attn& p, hipStream_t stream) {
     c = flip ? -c : c;
     if (c < std::numeric_limits<float>::min()) c = std::numeric_limits<float>::min();
     const long long blocks = (long long)p.c.B * p.c.hk * tiles * p.splits;
-    hipError_t e = launch_kernel(kv4_attn_kernel<D, RT>, dim3((unsigned)blocks), dim3(WAVES * 64), stream, p, c, flip, tiles);
+    const auto run = [&](auto kernel) {
+        return launch_kernel(kernel, dim3((unsigned)blocks), dim3(WAVES * 64), stream, p, c, flip, tiles);
+    };
+    const hipError_t e = tiles == 1 ? run(kv4_attn_kernel<D, RT, true>) : run(kv4_attn_kernel<D, RT, false>);
     if (e != hipSuccess || p.splits == 1) return e;
     const long long all = (long long)p.c.B * p.hq * p.c.n;
-    return launch_kernel(kv4_combine_kernel<D>, dim3((unsigned)((all + 3) / 4)), dim3(256), stream, p);
+    if (p.splits <= 4 || all >= 2048) return launch_kernel(kv4_combine_kernel<D, 1>, dim3((unsigned)((all + 3) / 4)), dim3(256), stream, p);
+    return launch_kernel(kv4_combine_kernel<D, 4>, dim3((unsigned)all), dim3(256), stream, p);
 }
 
 }  // namespace
