@@ -7,14 +7,14 @@ wrong, only when a test fails.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
 from . import MOA_OK, MoaAttnError, _DTYPE_CODES, lib
 
 i64, vp, f32, ci, sz = ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_int, ctypes.c_size_t
-addressof = ctypes.addressof
-Strides6, Strides12, Strides18 = (ctypes.c_int64 * (3 * n) for n in (2, 4, 6))
+_three = struct.Struct("3q").pack
 
 
 class Function:
@@ -43,6 +43,16 @@ def run(function, device, args):
             status = f(*args)
     if status != MOA_OK:
         raise MoaAttnError(status)
+
+
+def strides3(s):
+    """A host array of a tensor's (batch, head, row) strides s."""
+    return _three(s[0], s[1], s[2])
+
+
+def new_like(x):
+    """A contiguous tensor like x (empty_like takes a third less time than new_empty)."""
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
 
 
 def array(values):

@@ -14,7 +14,7 @@ import math
 import torch
 
 from . import MOA_BF16, MOA_F32, _DTYPE_CODES, _stream_handle
-from ._call import (Function, Strides6, addressof, check_list, check_rows, ci, f32, i64, is_list, run, sz, vp,
+from ._call import (Function, check_list, check_rows, ci, f32, i64, is_list, new_like, run, strides3, sz, vp,
                     workspace as _workspace)
 
 moa_kv4_page_bytes = Function("moa_kv4_page_bytes", [i64] * 2, sz)
@@ -87,10 +87,8 @@ def kv4_write(k, v, cache, seq_lens, page_table=None, new_lens=None, stream=None
     heads, page, num_pages, max_pages, pool, lens, new, table = _place(cache, d, B, seq_lens, new_lens, page_table, device)
     if Hk != heads:
         raise ValueError(f"k has {Hk} heads, the cache {heads}")
-    strides = Strides6(*ks[:3], *vs[:3])
-    at = addressof(strides)   # eight bytes each
     run(moa_kv4_write, device, (k.data_ptr(), v.data_ptr(), pool, lens, new, table, B, Hk, N, d, page, num_pages, max_pages,
-                                at, at + 24, _DTYPE_CODES[k.dtype], _stream_handle(stream, k)))
+                                strides3(ks), strides3(vs), _DTYPE_CODES[k.dtype], _stream_handle(stream, k)))
 
 
 def kv4_read(cache, N, d, seq_lens, page_table=None, new_lens=None, out_dtype=None, k_out=None, v_out=None,
@@ -112,13 +110,12 @@ def kv4_read(cache, N, d, seq_lens, page_table=None, new_lens=None, out_dtype=No
     else:
         check_rows("k_out", k_out, n, dt, device)
     if v_out is None:
-        v_out = cache.new_empty(n, dtype=dt)
+        v_out = new_like(k_out)
     else:
         check_rows("v_out", v_out, n, dt, device)
-    strides = Strides6(*k_out.stride()[:3], *v_out.stride()[:3])
-    at = addressof(strides)   # eight bytes each
     run(moa_kv4_read, device, (pool, k_out.data_ptr(), v_out.data_ptr(), lens, new, table, B, heads, N, d, page, num_pages,
-                               max_pages, at, at + 24, _DTYPE_CODES[dt], _stream_handle(stream, cache)))
+                               max_pages, strides3(k_out.stride()), strides3(v_out.stride()), _DTYPE_CODES[dt],
+                               _stream_handle(stream, cache)))
     return k_out, v_out
 
 
@@ -141,7 +138,7 @@ def kv4_attn_fwd(q, cache, seq_lens, page_table=None, new_lens=None, scale=None,
     if odt not in _DTYPE_CODES:
         raise TypeError(f"unsupported dtype {odt}; use torch.float32 or torch.bfloat16")
     if out is None:
-        out = q.new_empty(n, dtype=odt)
+        out = new_like(q) if odt is _bf16 else q.new_empty(n, dtype=odt)
     else:
         check_rows("out", out, n, odt, device)
     lse = q.new_empty((B, Hq, N), dtype=torch.float32) if return_lse else None
@@ -150,10 +147,8 @@ def kv4_attn_fwd(q, cache, seq_lens, page_table=None, new_lens=None, scale=None,
         if need:
             workspace = q.new_empty(need, dtype=_uint8)
     ws, ws_n = _workspace(workspace, device)
-    strides = Strides6(*qs[:3], *out.stride()[:3])
-    at = addressof(strides)   # eight bytes each
     run(moa_kv4_attn_fwd, device, (
         q.data_ptr(), pool, out.data_ptr(), lse.data_ptr() if return_lse else None, lens, new, table, B, Hq, heads, N, d,
-        page, num_pages, max_pages, max_len, at, at + 24, 1.0 / math.sqrt(d) if scale is None else scale, causal,
+        page, num_pages, max_pages, max_len, strides3(qs), strides3(out.stride()), 1.0 / math.sqrt(d) if scale is None else scale, causal,
         MOA_F32 if odt is torch.float32 else MOA_BF16, ws, ws_n, num_splits, _stream_handle(stream, q)))
     return (out, lse) if return_lse else out

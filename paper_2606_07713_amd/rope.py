@@ -4,8 +4,8 @@ from __future__ import annotations
 import torch
 
 from . import MOA_F32, _DTYPE_CODES, _stream_handle
-from ._call import (Function, Strides12, Strides18, addressof, array, check_list, check_rows, ci, f32, i64, is_list, run,
-                    sz, vp, workspace as _workspace)
+from ._call import (Function, array, check_list, check_rows, ci, f32, i64, is_list, new_like, run, strides3, sz, vp,
+                    workspace as _workspace)
 
 _SIZES = [i64] * 6
 moa_qk_norm_rope = Function(
@@ -96,19 +96,17 @@ def qk_norm_rope(q, k=None, positions=None, inv_freq=None, q_weight=None, k_weig
     qn, kn, qs, ks, device, rot, axes, sec, wcode, (qp, kp, wq, wk, pos, freq) = _common(
         q, k, positions, inv_freq, q_weight, k_weight, sections)
     if q_out is None:
-        q_out = q.new_empty(qn)
+        q_out = new_like(q)
     qos = _like("q_out", q_out, q, qn, device)
     kos, kop = ks, None
     if k is not None:
         if k_out is None:
-            k_out = k.new_empty(kn)
+            k_out = new_like(k)
         kos, kop = _like("k_out", k_out, k, kn, device), k_out.data_ptr()
     B, Hq, N, d = qn
-    strides = Strides12(*qs[:3], *ks[:3], *qos[:3], *kos[:3])
-    at = addressof(strides)   # eight bytes each
     run(moa_qk_norm_rope, device, (
-        qp, kp, q_out.data_ptr(), kop, wq, wk, pos, freq, B, Hq, kn[1], N, d, rot, at, at + 24, at + 48, at + 72, axes,
-        sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, _stream_handle(stream, q)))
+        qp, kp, q_out.data_ptr(), kop, wq, wk, pos, freq, B, Hq, kn[1], N, d, rot, strides3(qs), strides3(ks),
+        strides3(qos), strides3(kos), axes, sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, _stream_handle(stream, q)))
     return q_out, (None if k is None else k_out)
 
 
@@ -124,12 +122,12 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, positions=None, inv_freq=None, q_weig
     if (k is None) != (dk_out is None):
         raise ValueError("k and dk_out go together")
     if dq is None:
-        dq = q.new_empty(qn)
+        dq = new_like(q)
     gqs, dqs = _like("dq_out", dq_out, q, qn, device), _like("dq", dq, q, qn, device)
     gks, dks, gkp, dkp = ks, ks, None, None
     if k is not None:
         if dk is None:
-            dk = k.new_empty(kn)
+            dk = new_like(k)
         gks, dks = _like("dk_out", dk_out, k, kn, device), _like("dk", dk, k, kn, device)
         gkp, dkp = dk_out.data_ptr(), dk.data_ptr()
     B, Hq, N, d = qn
@@ -139,10 +137,8 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, positions=None, inv_freq=None, q_weig
         n = moa_qk_norm_rope_bwd_workspace_bytes(B, Hq, kn[1], N, d)
         workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
     ws, ws_n = _workspace(workspace, device)
-    strides = Strides18(*qs[:3], *ks[:3], *gqs[:3], *gks[:3], *dqs[:3], *dks[:3])
-    at = addressof(strides)   # eight bytes each
     run(moa_qk_norm_rope_bwd, device, (
         qp, kp, dq_out.data_ptr(), gkp, wq, wk, pos, freq, dq.data_ptr(), dkp, None if dwq is None else dwq.data_ptr(),
-        None if dwk is None else dwk.data_ptr(), B, Hq, kn[1], N, d, rot, at, at + 24, at + 48, at + 72, at + 96,
-        at + 120, axes, sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, ws, ws_n, _stream_handle(stream, q)))
+        None if dwk is None else dwk.data_ptr(), B, Hq, kn[1], N, d, rot, strides3(qs), strides3(ks), strides3(gqs),
+        strides3(gks), strides3(dqs), strides3(dks), axes, sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, ws, ws_n, _stream_handle(stream, q)))
     return dq, (None if k is None else dk), dwq, dwk
