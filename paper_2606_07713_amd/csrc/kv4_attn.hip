@@ -15,9 +15,12 @@
 // in a product is free, two such accumulators, packed to bf16, are the B
 // operand of the second product as they are.
 //
-// Softmax: running reference m per row (raised only when a tile's maximum is
-// more than 8 log2 units above it, for the whole wave at once), fp32 sums of
-// the unrounded weights per lane, joined over the lanes once at the end.
+// Softmax: a running reference per row, the maximum of the first tile that the
+// row sees; later tiles are weighed against it without looking for their own
+// maximum, and only a sum beyond 2^20 (scores 16 and more log2 units above the
+// reference; fp32 and bf16 hold such weights as well as small ones) raises it,
+// for the whole wave at once.  fp32 sums of the unrounded weights per lane,
+// joined over the lanes once at the end.
 #include <limits>
 
 #include "kv4_common.h"
@@ -29,7 +32,7 @@ namespace {
 using namespace kv4;
 
 constexpr int WAVES = 4;
-constexpr float kLift = 8.0f;   // log2 units that weights may grow above the reference
+constexpr float kLargeSum = 1048576.0f;   // a lane's sum of one tile's weights that raises the reference
 
 // Max over the four lanes with the same lane % 16.
 __device__ __forceinline__ float column_max(float x) {
@@ -203,16 +206,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
     }
 
     f32x4 o[RT][E];
-    float m[RT], l[RT];   // m: reference in raw score units, -inf before the first visible key
+    float ref[RT], l[RT];   // reference in log2 units, -inf before the first visible key
+    bool ready = false;     // every row has one
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-        m[i] = kNegInf;
+        ref[i] = kNegInf;
         l[i] = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) o[i][e] = f32x4{0, 0, 0, 0};
     }
-    const float lift = kLift / c;
-
     const int tpp = kc.page >> 6;   // tiles per page
     int at = begin + wave, index = at / tpp, in = at - index * tpp;
     // Loads the tile at `at` and moves on; false: there is none (no more tiles,
@@ -263,45 +265,60 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
                         if (64 * t + 16 * u + 4 * g + j >= seen[i]) s[i][u][j] = kNegInf;
         }
 
-        float top[RT];
-        bool raise = false;
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            float x = kNegInf;
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x = fmaxf(x, s[i][u][j]);
-            top[i] = column_max(x);
-            raise |= m[i] == kNegInf ? top[i] > kNegInf : top[i] > m[i] + lift;
-        }
-        if (wave_any(raise)) {
+        // The weights 2^(s c - ref) and their sums.
+        bf16x8 pt[RT][2];
+        float sum[RT];
+        const auto weights = [&]() {
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                const float m_new = fmaxf(m[i], top[i]);
-                const float a = m[i] == kNegInf ? 0.0f : exp2_hw((m[i] - m_new) * c);
-                m[i] = m_new;
+                const float shift = ref[i] == kNegInf ? 0.0f : -ref[i];
+                float w[4][4], x = 0.0f;
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        w[u][j] = exp2_hw(__builtin_fmaf(s[i][u][j], c, shift));
+                        x += w[u][j];
+                    }
+                sum[i] = x;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    pt[i][u] = __builtin_bit_cast(bf16x8, make_uint4(pack2(w[2 * u][0], w[2 * u][1]), pack2(w[2 * u][2], w[2 * u][3]),
+                                                                     pack2(w[2 * u + 1][0], w[2 * u + 1][1]), pack2(w[2 * u + 1][2], w[2 * u + 1][3])));
+            }
+        };
+        // Against the present references, without a maximum, unless the tile is
+        // masked, a row has seen nothing yet or a sum comes out too large.
+        bool raise = masked || !ready;
+        if (!raise) {
+            weights();
+            bool large = false;
+#pragma unroll
+            for (int i = 0; i < RT; ++i) large |= sum[i] > kLargeSum;
+            raise = wave_any(large);
+        }
+        if (raise) {
+            ready = true;
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                float x = kNegInf;
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x = fmaxf(x, s[i][u][j]);
+                x = fmaxf(ref[i], column_max(x) * c);
+                const float a = ref[i] == kNegInf ? 0.0f : exp2_hw(ref[i] - x);
+                ref[i] = x;
                 l[i] *= a;
 #pragma unroll
                 for (int e = 0; e < E; ++e) o[i][e] *= a;
+                ready &= !wave_any(x == kNegInf);
             }
+            weights();
         }
-        bf16x8 pt[RT][2];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const float mc = m[i] == kNegInf ? 0.0f : m[i] * c;
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s[i][u][j] = exp2_hw(__builtin_fmaf(s[i][u][j], c, -mc));
-                    l[i] += s[i][u][j];
-                }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                pt[i][u] = __builtin_bit_cast(bf16x8, make_uint4(pack2(s[i][2 * u][0], s[i][2 * u][1]), pack2(s[i][2 * u][2], s[i][2 * u][3]),
-                                                                 pack2(s[i][2 * u + 1][0], s[i][2 * u + 1][1]), pack2(s[i][2 * u + 1][2], s[i][2 * u + 1][3])));
-        }
+        for (int i = 0; i < RT; ++i) l[i] += sum[i];
+
         const auto product = [&](auto U) {
             constexpr int u = decltype(U)::value;
             bf16x8 a[E];
@@ -362,7 +379,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         l[i] = column_sum(l[i]);
-        if (g == 0) part_m[wave][16 * i + n] = m[i] == kNegInf ? kNegInf : m[i] * c;
+        if (g == 0) part_m[wave][16 * i + n] = ref[i];
     }
     __syncthreads();
 #pragma unroll
@@ -371,7 +388,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
         float M = kNegInf;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) M = fmaxf(M, part_m[w][row]);
-        const float a = m[i] == kNegInf ? 0.0f : exp2_hw(m[i] * c - M);
+        const float a = ref[i] == kNegInf ? 0.0f : exp2_hw(ref[i] - M);
         if (g == 0) part_l[wave][row] = l[i] * a;
         // column 4 g + j of the wave's O^T: elements E (4 g + j) + e of the row
 #pragma unroll
