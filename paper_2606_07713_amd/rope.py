@@ -1,6 +1,8 @@
 """Norms of queries and keys for each head with the rotation by position (``include/moa_rope.h``)."""
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import MOA_F32, _DTYPE_CODES, _stream_handle
@@ -16,7 +18,8 @@ moa_qk_norm_rope_bwd = Function(
     [vp] * 12 + _SIZES + [vp] * 6 + [ci, vp, ci, f32, ci, ci, vp, sz, vp])
 moa_qk_norm_rope_bwd_workspace_bytes = Function("moa_qk_norm_rope_bwd_workspace_bytes", [i64] * 5, sz)
 
-_int64, _float32 = torch.int64, torch.float32
+_bwd_ws_bytes = functools.lru_cache(maxsize=1024)(moa_qk_norm_rope_bwd_workspace_bytes)
+_int64, _float32, _empty_like = torch.int64, torch.float32, torch.empty_like
 
 
 def _like(name, t, x, shape, device):
@@ -28,11 +31,12 @@ def _like(name, t, x, shape, device):
 
 
 def _weight(name, w, d, device):
-    if w.dtype not in _DTYPE_CODES or not is_list(w, (d,), w.dtype, device):
-        if w.dtype not in _DTYPE_CODES:
-            raise TypeError(f"{name}: unsupported dtype {w.dtype}; use torch.float32 or torch.bfloat16")
+    code = _DTYPE_CODES.get(w.dtype)
+    if code is None:
+        raise TypeError(f"{name}: unsupported dtype {w.dtype}; use torch.float32 or torch.bfloat16")
+    if w.shape != (d,) or w.get_device() != device or not w.is_contiguous():
         check_list(name, w, (d,), w.dtype, device)
-    return _DTYPE_CODES[w.dtype]
+    return code
 
 
 def _common(q, k, positions, inv_freq, q_weight, k_weight, sections):
@@ -131,11 +135,10 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, positions=None, inv_freq=None, q_weig
         gks, dks = _like("dk_out", dk_out, k, kn, device), _like("dk", dk, k, kn, device)
         gkp, dkp = dk_out.data_ptr(), dk.data_ptr()
     B, Hq, N, d = qn
-    dwq = None if wq is None else torch.empty(d, dtype=_float32, device=q.device)
-    dwk = None if wk is None else torch.empty(d, dtype=_float32, device=q.device)
+    dwq = None if wq is None else _empty_like(q_weight, dtype=_float32)
+    dwk = None if wk is None else _empty_like(k_weight, dtype=_float32)
     if workspace is None and (wq is not None or wk is not None):
-        n = moa_qk_norm_rope_bwd_workspace_bytes(B, Hq, kn[1], N, d)
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+        workspace = q.new_empty(_bwd_ws_bytes(B, Hq, kn[1], N, d), dtype=torch.uint8)
     ws, ws_n = _workspace(workspace, device)
     run(moa_qk_norm_rope_bwd, device, (
         qp, kp, dq_out.data_ptr(), gkp, wq, wk, pos, freq, dq.data_ptr(), dkp, None if dwq is None else dwq.data_ptr(),
