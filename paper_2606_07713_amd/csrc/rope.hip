@@ -137,12 +137,20 @@ struct Turn {
     }
 };
 
-__device__ __forceinline__ void load_weights(const RopeProblem& p, int ts, int e0, float (&w)[8]) {
+// This lane's eight weights of tensor ts (1 without a norm).
+__device__ __forceinline__ void load_weights(const RopeProblem& p, int ts, int j, float (&w)[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        w[e] = !p.w[ts] ? 1.0f
-               : p.w_bf16 ? __uint_as_float((uint32_t)static_cast<const u16*>(p.w[ts])[e0 + e] << 16)
-                          : static_cast<const float*>(p.w[ts])[e0 + e];
+    for (int e = 0; e < 8; ++e) w[e] = 1.0f;
+    if (!p.w[ts]) return;
+    if (p.w_bf16) {
+        Chunk<u16> c;
+        c.load(static_cast<const u16*>(p.w[ts]) + 8 * j);
+        c.get(w);
+    } else {
+        Chunk<float> c;
+        c.load(static_cast<const float*>(p.w[ts]) + 8 * j);
+        c.get(w);
+    }
 }
 
 // The heads that one lane group takes of its token: heads first, first + step,
@@ -197,9 +205,12 @@ __global__ __launch_bounds__(THREADS) void rope_fwd_kernel(RopeProblem p, int lo
             if (w.ts < 2 && w.h + u * w.step < w.limit()) c[u].load(base + (w.h + u * w.step) * stride);
             else c[u].zero();
     };
-    // The first rows are on their way while the angles are taken.
+    // The first rows and the weights are on their way while the angles are taken.
     Chunk<T> next[U];
     load(next);
+    float wq[8], wk[8];
+    load_weights(p, 0, j, wq);
+    load_weights(p, 1, j, wk);
     take_angles(p, cs, t0, tb, tokens);
     __syncthreads();
     if (t0 + t >= tokens) return;
@@ -216,12 +227,10 @@ __global__ __launch_bounds__(THREADS) void rope_fwd_kernel(RopeProblem p, int lo
         load(next);
         if (ts != have) {
             have = ts;
-            load_weights(p, ts, 8 * j, A);
-            load_weights(p, ts, 8 * (j + (turn.partner - lane)), Bp);
-            if constexpr (IL) {
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) { const float v = Bp[e]; Bp[e] = Bp[e + 1]; Bp[e + 1] = v; }
-            }
+            for (int e = 0; e < 8; ++e) A[e] = ts ? wk[e] : wq[e];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) Bp[e] = IL ? A[e ^ 1] : __shfl(A[e], turn.partner);
 #pragma unroll
             for (int e = 0; e < 8; ++e) { A[e] *= turn.c[e]; Bp[e] = turn.turned ? Bp[e] * turn.s[e] : 0.0f; }
         }
@@ -258,7 +267,9 @@ __global__ __launch_bounds__(THREADS) void rope_bwd_kernel(RopeProblem p, int lo
     const int tokens = p.B * p.N, tb = 1 << log_tb;
     const int j = threadIdx.x % LPR, grp = threadIdx.x / LPR, lane = threadIdx.x & 63;
     const int t = grp & (tb - 1);
-    float dw[2][8];
+    float dw[2][8], wq[8], wk[8];
+    load_weights(p, 0, j, wq);
+    load_weights(p, 1, j, wk);
 #pragma unroll
     for (int ts = 0; ts < 2; ++ts)
 #pragma unroll
@@ -299,8 +310,6 @@ __global__ __launch_bounds__(THREADS) void rope_bwd_kernel(RopeProblem p, int lo
         if (t0 + t >= tokens) continue;
         Turn<IL> turn;
         turn.set(p, cs + t * (p.rot >> 1), j, lane);
-        float w[8];
-        int have = -1;
         while (walk.ts < 2) {
             const int ts = walk.ts, h0 = walk.h, limit = walk.limit();
             Chunk<T> cx[U], cg[U];
@@ -308,10 +317,9 @@ __global__ __launch_bounds__(THREADS) void rope_bwd_kernel(RopeProblem p, int lo
             for (int u = 0; u < U; ++u) { cx[u] = nx[u]; cg[u] = ng[u]; }
             walk.template next<U>();
             load(nx, ng);
-            if (ts != have) {
-                have = ts;
-                load_weights(p, ts, 8 * j, w);
-            }
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = ts ? wk[e] : wq[e];
             const bool norm = (ts ? p.w[1] : p.w[0]) != nullptr;
             T* to = ts ? y[1] : y[0];
             const long long stride = ts ? p.ys[1][1] : p.ys[0][1];
@@ -364,28 +372,30 @@ __global__ __launch_bounds__(THREADS) void rope_bwd_kernel(RopeProblem p, int lo
 }
 
 // Sums the workgroups' partial sums in a fixed order: a workgroup per tensor
-// and 16 elements, 64 threads per element.
+// and 16 elements, 64 threads per element, all loads of a thread in flight at
+// once.
 template <int D>
 __global__ __launch_bounds__(1024) void rope_dw_kernel(const float* __restrict__ ws, float* dwq,
                                                        float* dwk, int blocks) {
-    __shared__ float red[64][17];
+    constexpr int PER = kRopeBwdMaxBlocks / 64;
+    __shared__ float red[16][16];
     const int e = threadIdx.x & 15, k = threadIdx.x >> 4;
     const int ts = blockIdx.x / (D / 16), col = (blockIdx.x % (D / 16)) * 16 + e;
     float* out = ts ? dwk : dwq;
     if (!out) return;
-    // all loads of a thread in flight at once
-    constexpr int PER = kRopeBwdMaxBlocks / 64;
     float v[PER], sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[i] = k + 64 * i < blocks ? ws[((size_t)(k + 64 * i) * 2 + ts) * D + col] : 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) sum += v[i];
-    red[k][e] = sum;
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if ((threadIdx.x & 63) < 16) red[threadIdx.x >> 6][e] = sum;
     __syncthreads();
-    if (k == 0) {
+    if (threadIdx.x < 16) {
         float all = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 64; ++i) all += red[i][e];
+        for (int i = 0; i < 16; ++i) all += red[i][e];
         out[col] = all;
     }
 }
