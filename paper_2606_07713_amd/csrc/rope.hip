@@ -416,9 +416,11 @@ hipError_t fwd(const RopeProblem& p, hipStream_t stream) {
     const int tokens = p.B * p.N, heads = p.H[0] + p.H[1];
     const int log_tb = pick_log_tb(tokens, THREADS / (D / 8));
     const int tiles = (tokens + (1 << log_tb) - 1) >> log_tb, least = (THREADS / (D / 8)) >> log_tb;
-    // Few tokens: their heads go to several workgroups.
+    // Few tokens: their heads go to several workgroups, until there is one for
+    // every compute unit (24 heads of 6216 tokens, fp32, d = 64: 19.2 us with the
+    // heads in two halves on 778 workgroups, 15.9 whole on 389).
     int per = heads;
-    while (per > least && (long long)tiles * ((heads + per - 1) / per) < 512) per = per / 2 > least ? per / 2 : least;
+    while (per > least && (long long)tiles * ((heads + per - 1) / per) < 256) per = per / 2 > least ? per / 2 : least;
     return launch_kernel(rope_fwd_kernel<T, D, IL>, dim3(tiles, (heads + per - 1) / per), dim3(THREADS), stream, p,
                          log_tb, per);
 }
