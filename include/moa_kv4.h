@@ -62,7 +62,7 @@ size_t moa_kv4_page_bytes(int64_t page, int64_t d);
  * B, Hk, N, d, page, num_pages, max_pages
  *           B, Hk, N >= 0; supported: d in {64, 128}, page a multiple of 64 up to
  *           2^20, max_pages * page < 2^31, num_pages < 2^31, and
- *           B * Hk * (N + 6) < 2^31.
+ *           B * Hk * (N + 6) < 2^30.
  * Two rows of one call must not be the same token of the same page (which one
  * stays is then undefined).  One kernel.  Returns MOA_OK once the work is
  * enqueued, or when there are no rows.
@@ -118,7 +118,8 @@ size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t N
  * new_lens[b] are left as they are.
  * B, Hq, Hk, N, ...
  *           as for moa_kv4_write, Hq a multiple of Hk; supported:
- *           B * Hq * (N + 64) * 256 < 2^31.
+ *           B * Hq * N < 2^26, and fewer than 2^24 workgroups (of 16 rows of one
+ *           key/value head and one key split, or 32 where a head has more).
  * scale     finite; 0 and negative values are valid.
  * max_len   as above (0: the capacity).  Any value is right; a good one is fast.
  * workspace, workspace_bytes

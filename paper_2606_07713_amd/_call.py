@@ -2,7 +2,9 @@
 
 Calls of a few microseconds on the GPU wait for their host side, so a wrapper tests its arguments
 with as few attribute reads as it can and goes through the functions here, which find out what is
-wrong, only when a test fails.
+wrong, only when a test fails.  A wrapper that is given a ``stream`` calls itself with that stream current:
+what it allocates then belongs to the stream, and memory that it frees is not used again while the
+stream still works on it.
 """
 from __future__ import annotations
 

@@ -15,6 +15,8 @@ using namespace moa;
 constexpr int64_t kLim = std::numeric_limits<int32_t>::max();
 constexpr int64_t kMaxPage = int64_t(1) << 20;
 constexpr int kMaxSplits = 256;
+// Workgroups of 256 threads in one launch: its threads are counted in 32 bits.
+constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;
 
 struct Dims {
     int64_t B, Hk, N, d, page, num_pages, max_pages;
@@ -31,7 +33,7 @@ int check_dims(const Dims& s) {
     if (!moa_kv4_page_bytes(s.page, s.d)) return MOA_ERR_UNSUPPORTED;
     if (s.B > kLim || s.Hk > kLim || s.N > kLim - 6 || s.num_pages > kLim || s.max_pages > kLim / s.page)
         return MOA_ERR_UNSUPPORTED;
-    if (s.B * s.Hk > kLim || (s.B * s.Hk > 0 && s.N + 6 > kLim / (s.B * s.Hk))) return MOA_ERR_UNSUPPORTED;
+    if (s.B * s.Hk > kLim || (s.B * s.Hk > 0 && s.N + 6 > kLim / 2 / (s.B * s.Hk))) return MOA_ERR_UNSUPPORTED;
     if (s.num_pages > 0 && s.Hk > (int64_t(1) << 46) / s.num_pages / (int64_t)moa_kv4_page_bytes(s.page, s.d))
         return MOA_ERR_UNSUPPORTED;
     if (!s.table && s.any() && (s.max_pages != 1 || s.num_pages < s.B)) return MOA_ERR_INVALID_ARG;
@@ -125,8 +127,10 @@ bool attn_sizes_ok(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d, int6
                    int64_t max_len, int num_splits) {
     if (B < 0 || Hq < 0 || Hk < 1 || N < 0 || max_pages < 0 || max_len < 0 || Hq % Hk) return false;
     if (num_splits < 0 || num_splits > kMaxSplits || !moa_kv4_page_bytes(page, d)) return false;
-    if (B > kLim || Hq > kLim || N > kLim / kMaxSplits - 64 || max_pages > kLim / page) return false;
-    return B * Hq <= kLim && (B * Hq == 0 || (N + 64) * kMaxSplits <= kLim / (B * Hq));
+    if (B > kLim || Hq > kLim || N > kLim || max_pages > kLim / page) return false;
+    if (B * Hq > kLim || (B * Hq > 0 && N > (kMaxBlocks * 4) / (B * Hq))) return false;   // four rows a workgroup in the second pass
+    const int64_t rows = N * (Hq / Hk), per = kv4_rows_per_block((int)rows);
+    return B * Hk * ((rows + per - 1) / per) <= kMaxBlocks / (num_splits > 0 ? num_splits : 1);
 }
 
 // Partial states of a call with these splits (none with one).

@@ -77,6 +77,9 @@ def _place(cache, d, B, seq_lens, new_lens, page_table, device):
 def kv4_write(k, v, cache, seq_lens, page_table=None, new_lens=None, stream=None):
     """Quantises new keys and values k, v [B, heads, N, d] (bf16 or fp32, any views with contiguous
     heads) into ``cache``, in place.  Raises ``MoaAttnError`` on a rejected call."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return kv4_write(k, v, cache, seq_lens, page_table, new_lens)
     n, ks, vs = k.shape, k.stride(), v.stride()
     device = k.get_device()
     if len(n) != 4 or device < 0 or k.dtype not in _DTYPE_CODES or ks[3] != 1:
@@ -88,7 +91,7 @@ def kv4_write(k, v, cache, seq_lens, page_table=None, new_lens=None, stream=None
     if Hk != heads:
         raise ValueError(f"k has {Hk} heads, the cache {heads}")
     run(moa_kv4_write, device, (k.data_ptr(), v.data_ptr(), pool, lens, new, table, B, Hk, N, d, page, num_pages, max_pages,
-                                strides3(ks), strides3(vs), _DTYPE_CODES[k.dtype], _stream_handle(stream, k)))
+                                strides3(ks), strides3(vs), _DTYPE_CODES[k.dtype], _stream_handle(None, k)))
 
 
 def kv4_read(cache, N, d, seq_lens, page_table=None, new_lens=None, out_dtype=None, k_out=None, v_out=None,
@@ -96,6 +99,9 @@ def kv4_read(cache, N, d, seq_lens, page_table=None, new_lens=None, out_dtype=No
     """The keys and values [B, heads, N, d] that ``cache`` holds for N rows per sequence, as
     ``out_dtype`` (default bf16; exact).  Rows behind ``new_lens`` are left as they are in ``k_out``
     and ``v_out`` (in new tensors: unset).  ``new_lens=seq_lens`` reads whole sequences."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return kv4_read(cache, N, d, seq_lens, page_table, new_lens, out_dtype, k_out, v_out)
     B = seq_lens.shape[0] if seq_lens.dim() == 1 else -1
     device = cache.get_device()
     if device < 0:
@@ -115,7 +121,7 @@ def kv4_read(cache, N, d, seq_lens, page_table=None, new_lens=None, out_dtype=No
         check_rows("v_out", v_out, n, dt, device)
     run(moa_kv4_read, device, (pool, k_out.data_ptr(), v_out.data_ptr(), lens, new, table, B, heads, N, d, page, num_pages,
                                max_pages, strides3(k_out.stride()), strides3(v_out.stride()), _DTYPE_CODES[dt],
-                               _stream_handle(stream, cache)))
+                               _stream_handle(None, cache)))
     return k_out, v_out
 
 
@@ -128,6 +134,10 @@ def kv4_attn_fwd(q, cache, seq_lens, page_table=None, new_lens=None, scale=None,
     sequence, where the caller knows it (it guides the key splits only; 0: the table's capacity).
     ``scale`` defaults to 1/sqrt(d).  Returns O [B, Hq, N, d] (and LSE [B, Hq, N] fp32 when
     ``return_lse``).  Raises ``MoaAttnError`` on a rejected call."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return kv4_attn_fwd(q, cache, seq_lens, page_table, new_lens, scale, causal, max_len, out_dtype, return_lse,
+                                num_splits, out, workspace)
     n, qs = q.shape, q.stride()
     device = q.get_device()
     if len(n) != 4 or device < 0 or q.dtype is not _bf16 or qs[3] != 1:
@@ -150,5 +160,5 @@ def kv4_attn_fwd(q, cache, seq_lens, page_table=None, new_lens=None, scale=None,
     run(moa_kv4_attn_fwd, device, (
         q.data_ptr(), pool, out.data_ptr(), lse.data_ptr() if return_lse else None, lens, new, table, B, Hq, heads, N, d,
         page, num_pages, max_pages, max_len, strides3(qs), strides3(out.stride()), 1.0 / math.sqrt(d) if scale is None else scale, causal,
-        MOA_F32 if odt is torch.float32 else MOA_BF16, ws, ws_n, num_splits, _stream_handle(stream, q)))
+        MOA_F32 if odt is torch.float32 else MOA_BF16, ws, ws_n, num_splits, _stream_handle(None, q)))
     return (out, lse) if return_lse else out

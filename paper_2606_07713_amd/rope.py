@@ -91,12 +91,15 @@ def qk_norm_rope(q, k=None, positions=None, inv_freq=None, q_weight=None, k_weig
     elements by position (None: no rotation).
 
     q, k: bf16 or fp32 device tensors, any views with contiguous heads (slices of a packed
-    projection output, ``[B, N, H, d]`` transposed); k may be None.  ``positions``: int64 [B, N],
-    or [axes, B, N] with ``sections`` = rotated pairs of each axis (time, height, width, ...);
+    projection output, ``[B, N, H, d]`` transposed); k may be None.  ``positions``: contiguous
+    int64 [B, N], or [axes, B, N] with ``sections`` = rotated pairs of each axis (time, height, width, ...);
     None: 0 .. N-1.  ``inv_freq``: fp32 [rot/2], radians per position.  Pairs are (i, i + rot/2),
     or (2i, 2i + 1) when ``interleaved``.  ``q_out`` and ``k_out`` may be q and k (in place).
     Returns (q_out, k_out).  Raises ``MoaAttnError`` on a rejected call.
     """
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return qk_norm_rope(q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved, sections, q_out, k_out)
     qn, kn, qs, ks, device, rot, axes, sec, wcode, (qp, kp, wq, wk, pos, freq) = _common(
         q, k, positions, inv_freq, q_weight, k_weight, sections)
     if q_out is None:
@@ -110,7 +113,7 @@ def qk_norm_rope(q, k=None, positions=None, inv_freq=None, q_weight=None, k_weig
     B, Hq, N, d = qn
     run(moa_qk_norm_rope, device, (
         qp, kp, q_out.data_ptr(), kop, wq, wk, pos, freq, B, Hq, kn[1], N, d, rot, strides3(qs), strides3(ks),
-        strides3(qos), strides3(kos), axes, sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, _stream_handle(stream, q)))
+        strides3(qos), strides3(kos), axes, sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, _stream_handle(None, q)))
     return q_out, (None if k is None else k_out)
 
 
@@ -121,6 +124,10 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, positions=None, inv_freq=None, q_weig
     the gradients of its outputs (k and dk_out may be None).  dq and dk have q's dtype and may be
     given (also dq_out and dk_out themselves); the weights' gradients are fp32 [d], None where
     there is no weight.  The other arguments must be the forward's."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return qk_norm_rope_bwd(q, k, dq_out, dk_out, positions, inv_freq, q_weight, k_weight, eps, interleaved,
+                                    sections, dq, dk, workspace)
     qn, kn, qs, ks, device, rot, axes, sec, wcode, (qp, kp, wq, wk, pos, freq) = _common(
         q, k, positions, inv_freq, q_weight, k_weight, sections)
     if (k is None) != (dk_out is None):
@@ -143,5 +150,6 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, positions=None, inv_freq=None, q_weig
     run(moa_qk_norm_rope_bwd, device, (
         qp, kp, dq_out.data_ptr(), gkp, wq, wk, pos, freq, dq.data_ptr(), dkp, None if dwq is None else dwq.data_ptr(),
         None if dwk is None else dwk.data_ptr(), B, Hq, kn[1], N, d, rot, strides3(qs), strides3(ks), strides3(gqs),
-        strides3(gks), strides3(dqs), strides3(dks), axes, sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, ws, ws_n, _stream_handle(stream, q)))
+        strides3(gks), strides3(dqs), strides3(dks), axes, sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, ws,
+        ws_n, _stream_handle(None, q)))
     return dq, (None if k is None else dk), dwq, dwk

@@ -363,6 +363,47 @@ def test_norm_rope_write_attend_together():
         assert torch.equal(layer(x, pos, torch.empty_like(out1))[2], got)
 
 
+def test_pool_beyond_four_gigabytes():
+    # pages whose offsets pass 32 bits; most of the pool is never touched
+    import torch
+    import paper_2606_07713_amd as moa
+    page, Hk, d = 256, 8, 128
+    num = (5 << 30) // (Hk * page * (d + d // 16))
+    cache = moa.kv4_cache(num, Hk, page, d)
+    table = _ints([[num - 1, 0, num // 2]])
+    lens, gen = [600], torch.Generator().manual_seed(3)
+    k, v = (torch.randn((1, Hk, 600, d), generator=gen).to(torch.bfloat16).to("cuda") for _ in range(2))
+    moa.kv4_write(k, v, cache, _ints(lens), page_table=table)
+    ko, vo = moa.kv4_read(cache, 600, d, _ints(lens), page_table=table)
+    for got, x in ((ko, k), (vo, v)):
+        assert torch.equal(got.cpu().double(), quantised(x.cpu()))
+    q = torch.randn((1, 16, 2, d), generator=gen).to(torch.bfloat16).to("cuda")
+    o, lse = moa.kv4_attn_fwd(q, cache, _ints(lens), page_table=table, causal=True, return_lse=True)
+    torch.cuda.synchronize()
+    near = cache[[num - 1, 0, num // 2]]
+    _check_attn(q, near, _ints([[0, 1, 2]]), page, lens, None, True, None, o, lse)
+
+
+def test_given_stream_owns_what_the_call_allocates():
+    # calls on a stream of their own, while the current stream allocates and writes
+    import torch
+    import paper_2606_07713_amd as moa
+    lens = [3000]
+    cache, table = _cache_of(1, 2, 128, 64, lens)
+    q = torch.randn((1, 8, 1, 128), device="cuda").to(torch.bfloat16)
+    seq = _ints(lens)
+    want = moa.kv4_attn_fwd(q, cache, seq, page_table=table)
+    assert moa.moa_kv4_attn_num_splits(1, 8, 2, 1, 128, 64, table.shape[1], 0, 0) > 1
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = []
+    for _ in range(20):
+        got.append(moa.kv4_attn_fwd(q, cache, seq, page_table=table, stream=s))
+        torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want) for g in got)
+
+
 def test_on_another_stream():
     import torch
     import paper_2606_07713_amd as moa

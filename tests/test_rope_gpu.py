@@ -197,6 +197,19 @@ def test_queries_alone_default_positions_and_no_rows():
     assert y.shape == e.shape and dq.shape == e.shape and not dw.any()
 
 
+def test_strides_beyond_32_bits():
+    import torch
+    import paper_2606_07713_amd as moa
+    buf = torch.empty((1 << 31) + (1 << 20), dtype=torch.bfloat16, device="cuda")
+    far = buf.as_strided((2, 3, 5, 64), ((1 << 31) + 64, 64, 192, 1))
+    q, k, w, freq, pos, _ = _inputs(2, 3, 1, 5, 64, "bf16", 64, 1, (True, True), False, 4)
+    far.copy_(q)
+    how = dict(positions=pos, inv_freq=freq, q_weight=w[0])
+    want = moa.qk_norm_rope(q, **how)[0]
+    got = moa.qk_norm_rope(far, q_out=far, **how)[0]
+    assert torch.equal(got, want)
+
+
 def test_infinity_outside_the_rotated_elements_stays_there():
     import torch
     import paper_2606_07713_amd as moa

@@ -52,7 +52,7 @@ ROPE_BAD = [
     (dict(wdt=7), 1), (dict(Qo=2 * P), 1), (dict(Ko=3 * P), 1), (dict(Qo=P + 16), 1), (dict(Qo=5 * P), 1),
     (dict(Ko=7 * P), 1), (dict(Ko=8 * P), 1), (dict(qs=[-64, 64, 64]), 1), (dict(qs=[4096, 512, 63]), 2),
     (dict(qos=[512, 64, 0]), 1), (dict(qos=[512, 64, 32]), 1), (dict(Qo=P, qos=[4096, 64, 256]), 1),
-    (dict(B=1 << 20, N=1 << 12), 2), (dict(Hq=1 << 40), 2), (dict(qs=[1 << 41, 64, 64]), 2),
+    (dict(B=1 << 20, N=1 << 7), 2), (dict(B=1 << 20, N=64, Hq=40), 2), (dict(Hq=1 << 40), 2), (dict(qs=[1 << 41, 64, 64]), 2),
 ]
 
 
@@ -113,7 +113,7 @@ KV4_BAD = [
     (dict(a=None), 1), (dict(b=None), 1), (dict(c=None), 1), (dict(lens=None), 1), (dict(a=P + 8), 1), (dict(c=4 * P + 8), 1),
     (dict(lens=8 * P + 2), 1), (dict(table=10 * P + 1), 1), (dict(B=-1), 1), (dict(N=-1), 1), (dict(num=-1), 1), (dict(page=0), 1),
     (dict(d=32), 2), (dict(page=48), 2), (dict(page=96), 2), (dict(page=1 << 21), 2), (dict(max=1 << 26), 2),
-    (dict(N=(1 << 31) - 10), 2), (dict(B=1 << 20, Hk=1 << 12), 2), (dict(table=None), 1), (dict(table=None, max=1, num=1), 1),
+    (dict(N=(1 << 29) - 10), 2), (dict(B=1 << 20, Hk=1 << 12), 2), (dict(table=None), 1), (dict(table=None, max=1, num=1), 1),
     (dict(dt=2), 1), (dict(ks=[1024, -512, 64]), 1), (dict(ks=[1024, 512, 60]), 2), (dict(c=P), 1),
     (dict(c=2 * P - 16), 1),
 ]
@@ -148,7 +148,7 @@ ATTN_BAD = [
     (dict(Q=None), 1), (dict(c=None), 1), (dict(O=None), 1), (dict(lens=None), 1), (dict(Hq=3), 1), (dict(Hk=0), 1),
     (dict(scale=float("inf")), 1), (dict(causal=2), 1), (dict(odt=3), 1), (dict(splits=-1), 1), (dict(splits=257), 1),
     (dict(max_len=-1), 1), (dict(lse=3 * P + 2), 1), (dict(ws=16 * P + 4), 1), (dict(ws=None), 3), (dict(n=100), 3),
-    (dict(d=96), 2), (dict(page=100), 2), (dict(N=1 << 23), 2), (dict(O=P), 1), (dict(O=4 * P), 1), (dict(lse=2 * P), 1),
+    (dict(d=96), 2), (dict(page=100), 2), (dict(N=1 << 23), 2), (dict(N=1 << 18, splits=256), 2), (dict(O=P), 1), (dict(O=4 * P), 1), (dict(lse=2 * P), 1),
     (dict(ws=2 * P), 1), (dict(ws=4 * P - 16), 1), (dict(O=8 * P), 1), (dict(qs=[768, 192, 33]), 2), (dict(os=[768, 0, 64]), 1),
     (dict(Q=P + 2), 1),
 ]
