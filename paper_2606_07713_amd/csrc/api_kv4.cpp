@@ -101,9 +101,10 @@ void put(long long (&to)[3], const Strides& s) { to[0] = s.b; to[1] = s.h; to[2]
 // partial states.  `wave` workgroups run at a time: one per compute unit where
 // up to 16 rows of d = 128 leave it to the memory, two where a tile is half as
 // large or its work twice (measured, splits:us, 32 heads on 8: one query, 4097
-// keys, d = 128 1:23.7 8:11.3 17:9.1 64:11.4; 16384 1:77 16:12.8 32:11.4 64:14.3;
-// 48 queries of 8192 1:82.8 2:74.5 4:75.6, 64 of them 1:92 2:94; 200 rows of one
-// sequence on 20011 keys 1:123 2:104 5:100 8:108, 512 on 8192 1:83 2:92).
+// keys, d = 128 1:22.9 8:10.9 17:9.1 64:11.4; 16384 1:72 16:12.6 32:11.2 64:14.1;
+// 48 queries of 8192 1:75.9 2:72.5 4:74.6, 64 of them 1:91.5 2:93.1; 200 queries
+// of one sequence on 20011 keys 1:113 2:96 4:97 5:84 8:94, 512 on 8192 1:75.5
+// 2:86).
 int pick_splits(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d, int64_t max_len, int requested) {
     if (requested > 0) return requested;
     const int64_t rows = N * (Hq / Hk), per = kv4_rows_per_block((int)rows);
