@@ -77,7 +77,8 @@ int moa_kv4_write(const void* K, const void* V, void* cache, const int32_t* seq_
  * tokens (exact in bf16 and fp32), into K and V of storage type out_dtype.
  * Rows behind new_lens[b] and rows of skipped tokens are left as they are.  K
  * and V must not write an element twice or overlap each other or an input.
- * (new_lens = seq_lens reads whole sequences: token i to row i.)
+ * (new_lens = seq_lens, with N at least the longest, reads whole sequences:
+ * token i to row i.)
  */
 int moa_kv4_read(const void* cache, void* K, void* V, const int32_t* seq_lens,
                  const int32_t* new_lens, const int32_t* page_table, int64_t B, int64_t Hk,

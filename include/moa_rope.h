@@ -54,8 +54,8 @@ extern "C" {
  * input, but for the two in-place forms.  Q, K, Qo and Ko may be views that
  * interleave in one buffer (heads of a packed projection output) as long as
  * either their rows or their batches take turns in it.  Pointers are 16-byte
- * aligned, positions 8-byte; a pointer may be NULL only when its tensor has no
- * elements.
+ * aligned, positions 8-byte, inv_freq 4-byte; a pointer may be NULL only when
+ * its tensor has no elements.
  *
  * Computation: fp32 from exact inputs, one rounding at the end; angles in
  * fp64, reduced to one turn before sine and cosine are taken in fp32, so that

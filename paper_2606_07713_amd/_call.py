@@ -11,9 +11,7 @@ from __future__ import annotations
 import ctypes
 import struct
 
-import torch
-
-from . import MOA_OK, MoaAttnError, _DTYPE_CODES, lib
+from . import MOA_OK, MoaAttnError, _DTYPE_CODES, _torch as torch, lib
 
 i64, vp, f32, ci, sz = ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_int, ctypes.c_size_t
 _three = struct.Struct("3q").pack

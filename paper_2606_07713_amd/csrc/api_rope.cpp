@@ -52,9 +52,8 @@ int check_common(const Common& c, const void* const (&w)[2]) {
         if (sum != c.rot / 2) return MOA_ERR_INVALID_ARG;
     }
     if ((c.any(0) || c.any(1)) && c.rot > 0 && !c.inv_freq) return MOA_ERR_INVALID_ARG;
-    for (const void* p : {w[0], w[1], static_cast<const void*>(c.inv_freq)})
-        if (!aligned16(p)) return MOA_ERR_INVALID_ARG;
-    if (reinterpret_cast<uintptr_t>(c.positions) & 7) return MOA_ERR_INVALID_ARG;
+    if (!aligned16(w[0]) || !aligned16(w[1])) return MOA_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(c.inv_freq) & 3) || (reinterpret_cast<uintptr_t>(c.positions) & 7)) return MOA_ERR_INVALID_ARG;
     const int64_t lim = std::numeric_limits<int32_t>::max();
     if (c.B > lim || c.N > lim || c.Hq > lim || c.Hk > lim) return MOA_ERR_UNSUPPORTED;
     const int64_t tokens = c.B * c.N, heads = c.Hq + c.Hk;

@@ -11,9 +11,7 @@ from __future__ import annotations
 import functools
 import math
 
-import torch
-
-from . import MOA_BF16, MOA_F32, _DTYPE_CODES, _stream_handle
+from . import MOA_BF16, MOA_F32, _DTYPE_CODES, _stream_handle, _torch as torch
 from ._call import (Function, check_list, check_rows, ci, f32, i64, is_list, new_like, run, strides3, sz, vp,
                     workspace as _workspace)
 
@@ -28,7 +26,8 @@ moa_kv4_attn_fwd = Function(
     "moa_kv4_attn_fwd", [vp] * 7 + [i64] * 9 + [vp, vp, f32, ci, ci, vp, sz, ci, vp])
 
 _ws_bytes = functools.lru_cache(maxsize=1024)(moa_kv4_attn_workspace_bytes)
-_int32, _uint8, _bf16 = torch.int32, torch.uint8, torch.bfloat16
+if torch is not None:   # the C functions above need none
+    _int32, _uint8, _bf16 = torch.int32, torch.uint8, torch.bfloat16
 
 
 @functools.lru_cache(maxsize=256)
@@ -98,7 +97,8 @@ def kv4_read(cache, N, d, seq_lens, page_table=None, new_lens=None, out_dtype=No
              stream=None):
     """The keys and values [B, heads, N, d] that ``cache`` holds for N rows per sequence, as
     ``out_dtype`` (default bf16; exact).  Rows behind ``new_lens`` are left as they are in ``k_out``
-    and ``v_out`` (in new tensors: unset).  ``new_lens=seq_lens`` reads whole sequences."""
+    and ``v_out`` (in new tensors: unset).  ``new_lens=seq_lens`` with N at least the longest reads
+    whole sequences, token i to row i."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return kv4_read(cache, N, d, seq_lens, page_table, new_lens, out_dtype, k_out, v_out)

@@ -3,9 +3,7 @@ from __future__ import annotations
 
 import functools
 
-import torch
-
-from . import MOA_F32, _DTYPE_CODES, _stream_handle
+from . import MOA_F32, _DTYPE_CODES, _stream_handle, _torch as torch
 from ._call import (Function, array, check_list, check_rows, ci, f32, i64, is_list, new_like, run, strides3, sz, vp,
                     workspace as _workspace)
 
@@ -19,7 +17,8 @@ moa_qk_norm_rope_bwd = Function(
 moa_qk_norm_rope_bwd_workspace_bytes = Function("moa_qk_norm_rope_bwd_workspace_bytes", [i64] * 5, sz)
 
 _bwd_ws_bytes = functools.lru_cache(maxsize=1024)(moa_qk_norm_rope_bwd_workspace_bytes)
-_int64, _float32, _empty_like = torch.int64, torch.float32, torch.empty_like
+if torch is not None:   # the C functions above need none
+    _int64, _float32, _empty_like = torch.int64, torch.float32, torch.empty_like
 
 
 def _like(name, t, x, shape, device):

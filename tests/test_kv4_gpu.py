@@ -251,18 +251,19 @@ def test_no_page_table_and_strided_output():
     _check_attn(q, cache, None, 320, lens, None, True, None, o, lse)
 
 
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("N,causal", [(1, True), (7, True), (40, True), (5, False)])
-def test_nan_blocks_reach_only_the_rows_that_see_them(N, causal):
+def test_nan_blocks_reach_only_the_rows_that_see_them(N, causal, d):
     # a token with a NaN in one value block, seen by some rows of the tile; unset memory behind
     import torch
     import paper_2606_07713_amd as moa
     lens = [150]
-    cache, table = _cache_of(1, 1, 128, 64, lens)
-    for at, where in ((149, 40), (146, 100)):
-        v = torch.zeros((1, 1, 1, 128), device="cuda")
+    cache, table = _cache_of(1, 1, d, 64, lens)
+    for at, where in ((149, 40), (146, d - 28)):
+        v = torch.zeros((1, 1, 1, d), device="cuda")
         v[..., where] = math.nan
         moa.kv4_write(torch.zeros_like(v), v, cache, _ints([at + 1]), page_table=table)
-    q = torch.randn((1, 4, N, 128), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to("cuda")
+    q = torch.randn((1, 4, N, d), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to("cuda")
     for splits in (1, 2):
         o, lse = moa.kv4_attn_fwd(q, cache, _ints(lens), page_table=table, causal=causal, return_lse=True,
                                   out_dtype=torch.float32, num_splits=splits)

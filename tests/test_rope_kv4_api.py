@@ -176,6 +176,17 @@ def test_sizes():
         assert _attn(Q=None, O=None, lse=None, ws=None, n=0, **kw) == moa.MOA_OK
 
 
+def test_c_functions_without_torch():
+    # the C entry points need no torch, as those of moa_attn.h
+    import sys
+    code = ("import sys; sys.modules['torch'] = None\n"
+            "import paper_2606_07713_amd as moa\n"
+            "assert moa.moa_kv4_page_bytes(64, 128) == 8704 and moa.moa_attn_status_string(0) == 'ok'\n"
+            "assert moa.moa_qk_norm_rope_bwd_workspace_bytes(1, 1, 1, 1, 64) > 0\n")
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+
+
 def test_torch_wrappers_refuse():
     import torch
     x = torch.zeros((1, 2, 3, 64), dtype=torch.bfloat16)
