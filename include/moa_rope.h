@@ -45,7 +45,7 @@ extern "C" {
  *           stride of a dimension of size 1 is ignored.
  * axes, sections
  *           1 to 4 position axes.  sections (HOST array of axes values >= 0 with
- *           sum rot/2; NULL when axes == 1): the first sections[0] pairs turn by
+ *           sum rot/2; may be NULL when axes == 1): the first sections[0] pairs turn by
  *           the position on axis 0, the next sections[1] by axis 1, and so on.
  * eps       finite, >= 0.
  * stream    hipStream_t as void*.

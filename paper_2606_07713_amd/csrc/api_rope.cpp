@@ -42,8 +42,8 @@ int check_common(const Common& c, const void* const (&w)[2]) {
     if (c.d != 64 && c.d != 128) return MOA_ERR_UNSUPPORTED;
     if (c.rot > c.d) return MOA_ERR_INVALID_ARG;
     if (c.rot % 16) return MOA_ERR_UNSUPPORTED;
-    if (c.axes > 1) {
-        if (!c.sections) return MOA_ERR_INVALID_ARG;
+    if (c.axes > 1 && !c.sections) return MOA_ERR_INVALID_ARG;
+    if (c.sections) {
         int64_t sum = 0;
         for (int a = 0; a < c.axes; ++a) {
             if (c.sections[a] < 0 || c.sections[a] > c.rot) return MOA_ERR_INVALID_ARG;

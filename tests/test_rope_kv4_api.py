@@ -48,7 +48,7 @@ ROPE_BAD = [
     (dict(Q=None), 1), (dict(Ko=None), 1), (dict(Q=P + 8), 1), (dict(pos=7 * P + 4), 1), (dict(freq=None), 1),
     (dict(B=-1), 1), (dict(N=-1), 1), (dict(d=0), 1), (dict(d=96), 2), (dict(rot=-16), 1), (dict(rot=80), 1),
     (dict(rot=24), 2), (dict(axes=0), 1), (dict(axes=5), 1), (dict(axes=2), 1), (dict(axes=2, sec=[16, 15]), 1),
-    (dict(axes=2, sec=[33, -1]), 1), (dict(il=2), 1), (dict(eps=float("nan")), 1), (dict(eps=-1.0), 1), (dict(dt=2), 1),
+    (dict(axes=2, sec=[33, -1]), 1), (dict(sec=[31]), 1), (dict(sec=[33]), 1), (dict(il=2), 1), (dict(eps=float("nan")), 1), (dict(eps=-1.0), 1), (dict(dt=2), 1),
     (dict(wdt=7), 1), (dict(Qo=2 * P), 1), (dict(Ko=3 * P), 1), (dict(Qo=P + 16), 1), (dict(Qo=5 * P), 1),
     (dict(Ko=7 * P), 1), (dict(Ko=8 * P), 1), (dict(qs=[-64, 64, 64]), 1), (dict(qs=[4096, 512, 63]), 2),
     (dict(qos=[512, 64, 0]), 1), (dict(qos=[512, 64, 32]), 1), (dict(Qo=P, qos=[4096, 64, 256]), 1),
