@@ -38,7 +38,8 @@ extern "C" {
  * B, Hq, Hk, N, d, rot
  *           batch, query heads, key heads, tokens, head size, rotated
  *           elements.  All may be 0 but d; supported: d in {64, 128}, rot a
- *           multiple of 16 up to d, B * N < 2^27, B * (Hq + Hk) * N < 2^31.
+ *           multiple of 16 up to d, B * N < 2^27, Hq + Hk < 2^30,
+ *           B * (Hq + Hk) * N < 2^31.
  * *_strides element strides (batch, head, row) as for moa_attn_fwd_strided, or
  *           NULL: contiguous.  Non-negative, multiples of 16 bytes; an output
  *           must not write an element twice.  Input rows may overlap.  The

@@ -58,7 +58,8 @@ int check_common(const Common& c, const void* const (&w)[2]) {
     if (c.B > lim || c.N > lim || c.Hq > lim || c.Hk > lim) return MOA_ERR_UNSUPPORTED;
     const int64_t tokens = c.B * c.N, heads = c.Hq + c.Hk;
     // 2^27 tokens: 16 and more of them a workgroup, whose threads are counted in 32 bits
-    if (tokens >= (int64_t(1) << 27) || heads > lim || (tokens > 0 && heads > lim / tokens)) return MOA_ERR_UNSUPPORTED;
+    // and the kernels step over heads a few times 32 past the last one
+    if (tokens >= (int64_t(1) << 27) || heads >= (int64_t(1) << 30) || (tokens > 0 && heads > lim / tokens)) return MOA_ERR_UNSUPPORTED;
     return MOA_OK;
 }
 

@@ -52,7 +52,8 @@ ROPE_BAD = [
     (dict(wdt=7), 1), (dict(Qo=2 * P), 1), (dict(Ko=3 * P), 1), (dict(Qo=P + 16), 1), (dict(Qo=5 * P), 1),
     (dict(Ko=7 * P), 1), (dict(Ko=8 * P), 1), (dict(qs=[-64, 64, 64]), 1), (dict(qs=[4096, 512, 63]), 2),
     (dict(qos=[512, 64, 0]), 1), (dict(qos=[512, 64, 32]), 1), (dict(Qo=P, qos=[4096, 64, 256]), 1),
-    (dict(B=1 << 20, N=1 << 7), 2), (dict(B=1 << 20, N=64, Hq=40), 2), (dict(Hq=1 << 40), 2), (dict(qs=[1 << 41, 64, 64]), 2),
+    (dict(B=1 << 20, N=1 << 7), 2), (dict(B=1 << 20, N=64, Hq=40), 2), (dict(Hq=1 << 40), 2),
+    (dict(B=1, N=1, Hq=(1 << 30) - 2), 2), (dict(qs=[1 << 41, 64, 64]), 2),
 ]
 
 
