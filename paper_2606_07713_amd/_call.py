@@ -45,6 +45,13 @@ def run(function, device, args):
         raise MoaAttnError(status)
 
 
+def on_stream(stream, t):
+    """A context with the given stream, one of t's device, as the current one."""
+    if stream.device != t.device:
+        raise ValueError(f"a stream of {stream.device} for tensors on {t.device}")
+    return torch.cuda.stream(stream)
+
+
 def strides3(s):
     """A host array of a tensor's (batch, head, row) strides s."""
     return _three(s[0], s[1], s[2])

@@ -12,7 +12,7 @@ import functools
 import math
 
 from . import MOA_BF16, MOA_F32, _DTYPE_CODES, _stream_handle, _torch as torch
-from ._call import (Function, check_list, check_rows, ci, f32, i64, is_list, new_like, run, strides3, sz, vp,
+from ._call import (Function, check_list, check_rows, ci, f32, i64, is_list, new_like, on_stream, run, strides3, sz, vp,
                     workspace as _workspace)
 
 moa_kv4_page_bytes = Function("moa_kv4_page_bytes", [i64] * 2, sz)
@@ -77,7 +77,7 @@ def kv4_write(k, v, cache, seq_lens, page_table=None, new_lens=None, stream=None
     """Quantises new keys and values k, v [B, heads, N, d] (bf16 or fp32, any views with contiguous
     heads) into ``cache``, in place.  Raises ``MoaAttnError`` on a rejected call."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with on_stream(stream, k):
             return kv4_write(k, v, cache, seq_lens, page_table, new_lens)
     n, ks, vs = k.shape, k.stride(), v.stride()
     device = k.get_device()
@@ -100,7 +100,7 @@ def kv4_read(cache, N, d, seq_lens, page_table=None, new_lens=None, out_dtype=No
     and ``v_out`` (in new tensors: unset).  ``new_lens=seq_lens`` with N at least the longest reads
     whole sequences, token i to row i."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with on_stream(stream, cache):
             return kv4_read(cache, N, d, seq_lens, page_table, new_lens, out_dtype, k_out, v_out)
     B = seq_lens.shape[0] if seq_lens.dim() == 1 else -1
     device = cache.get_device()
@@ -135,7 +135,7 @@ def kv4_attn_fwd(q, cache, seq_lens, page_table=None, new_lens=None, scale=None,
     ``scale`` defaults to 1/sqrt(d).  Returns O [B, Hq, N, d] (and LSE [B, Hq, N] fp32 when
     ``return_lse``).  Raises ``MoaAttnError`` on a rejected call."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with on_stream(stream, q):
             return kv4_attn_fwd(q, cache, seq_lens, page_table, new_lens, scale, causal, max_len, out_dtype, return_lse,
                                 num_splits, out, workspace)
     n, qs = q.shape, q.stride()

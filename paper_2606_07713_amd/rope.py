@@ -4,7 +4,7 @@ from __future__ import annotations
 import functools
 
 from . import MOA_F32, _DTYPE_CODES, _stream_handle, _torch as torch
-from ._call import (Function, array, check_list, check_rows, ci, f32, i64, is_list, new_like, run, strides3, sz, vp,
+from ._call import (Function, array, check_list, check_rows, ci, f32, i64, is_list, new_like, on_stream, run, strides3, sz, vp,
                     workspace as _workspace)
 
 _SIZES = [i64] * 6
@@ -97,7 +97,7 @@ def qk_norm_rope(q, k=None, positions=None, inv_freq=None, q_weight=None, k_weig
     Returns (q_out, k_out).  Raises ``MoaAttnError`` on a rejected call.
     """
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with on_stream(stream, q):
             return qk_norm_rope(q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved, sections, q_out, k_out)
     qn, kn, qs, ks, device, rot, axes, sec, wcode, (qp, kp, wq, wk, pos, freq) = _common(
         q, k, positions, inv_freq, q_weight, k_weight, sections)
@@ -124,7 +124,7 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, positions=None, inv_freq=None, q_weig
     given (also dq_out and dk_out themselves); the weights' gradients are fp32 [d], None where
     there is no weight.  The other arguments must be the forward's."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with on_stream(stream, q):
             return qk_norm_rope_bwd(q, k, dq_out, dk_out, positions, inv_freq, q_weight, k_weight, eps, interleaved,
                                     sections, dq, dk, workspace)
     qn, kn, qs, ks, device, rot, axes, sec, wcode, (qp, kp, wq, wk, pos, freq) = _common(

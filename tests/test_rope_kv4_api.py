@@ -203,3 +203,16 @@ def test_torch_wrappers_refuse():
     with pytest.raises(ValueError):
         moa.kv4_cache(1, 1, 48, 64, device="cpu")
     assert moa.kv4_cache(3, 2, 64, 128, device="cpu").shape == (3, 2, 64 * 136)
+
+
+def test_torch_wrappers_refuse_a_stream_of_another_device():
+    import types
+    import torch
+    x = torch.zeros((1, 2, 3, 64), dtype=torch.bfloat16)
+    lens, cache = torch.zeros(1, dtype=torch.int32), torch.zeros((1, 2, 64 * 68), dtype=torch.uint8)
+    stream = types.SimpleNamespace(device=torch.device("cuda", 1))
+    for call in (lambda: moa.qk_norm_rope(x, stream=stream), lambda: moa.qk_norm_rope_bwd(x, None, x, None, stream=stream),
+                 lambda: moa.kv4_write(x, x, cache, lens, stream=stream), lambda: moa.kv4_read(cache, 1, 64, lens, stream=stream),
+                 lambda: moa.kv4_attn_fwd(x, cache, lens, stream=stream)):
+        with pytest.raises(ValueError, match="stream of cuda:1"):
+            call()
