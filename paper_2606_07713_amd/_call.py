@@ -14,7 +14,6 @@ import struct
 from . import MOA_OK, MoaAttnError, _DTYPE_CODES, _torch as torch, lib
 
 i64, vp, f32, ci, sz = ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_int, ctypes.c_size_t
-_three = struct.Struct("3q").pack
 
 
 class Function:
@@ -33,14 +32,22 @@ class Function:
         return (self.f or self.bind())(*args)
 
 
-def run(function, device, args):
-    """Calls a status function with ``device`` (an index) current; raises on a rejected call."""
-    f = function.f or function.bind()
+class Packed(Function):
+    """The library's function ``name`` of a record of ``words`` (a struct format)."""
+
+    def __init__(self, name, words):
+        super().__init__(name, [vp])
+        self.pack = struct.Struct(words).pack
+
+
+def run(function, device, *words):
+    """Calls a Packed status function with ``device`` (an index) current; raises on a rejected call."""
+    f, record = function.f or function.bind(), function.pack(*words)
     if device == torch._C._cuda_getDevice():
-        status = f(*args)
+        status = f(record)
     else:
         with torch.cuda.device(device):
-            status = f(*args)
+            status = f(record)
     if status != MOA_OK:
         raise MoaAttnError(status)
 
@@ -52,21 +59,9 @@ def on_stream(stream, t):
     return torch.cuda.stream(stream)
 
 
-def strides3(s):
-    """A host array of a tensor's (batch, head, row) strides s."""
-    return _three(s[0], s[1], s[2])
-
-
 def new_like(x):
     """A contiguous tensor like x (empty_like takes a third less time than new_empty)."""
     return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
-
-
-def array(values):
-    """A host array of int64, or None."""
-    if values is None:
-        return None
-    return (ctypes.c_int64 * len(values))(*[int(x) for x in values])
 
 
 def is_list(t, shape, dtype, device):
@@ -100,7 +95,7 @@ def check_rows(name, t, shape=None, dtype=None, device=None):
 def workspace(ws, device):
     """(address, bytes) of a workspace tensor or None."""
     if ws is None:
-        return None, 0
+        return 0, 0
     if ws.get_device() != device or not ws.is_contiguous():
         raise ValueError(f"the workspace must be a contiguous tensor on device {device}")
     return ws.data_ptr(), ws.numel() * ws.element_size()

@@ -7,6 +7,7 @@
 #include "../../include/moa_kv4.h"
 #include "api_checks.h"
 #include "kv4.h"
+#include "packed.h"
 
 namespace {
 
@@ -252,6 +253,27 @@ int moa_kv4_attn_fwd(const void* Q, const void* cache, void* O, float* LSE, cons
     p.splits = splits;
     p.ws = static_cast<float*>(workspace);
     return hip_status(launch_kv4_attn(p, static_cast<hipStream_t>(stream)));
+}
+
+// Words: the arguments in their order, but 4 for each tensor's strides (the last
+// not read).
+int moa_packed_kv4_write(const int64_t* a) {
+    using packed::Ptr;
+    return moa_kv4_write(Ptr{a[0]}, Ptr{a[1]}, Ptr{a[2]}, Ptr{a[3]}, Ptr{a[4]}, Ptr{a[5]}, a[6], a[7], a[8], a[9],
+                         a[10], a[11], a[12], a + 13, a + 17, (int)a[21], Ptr{a[22]});
+}
+
+int moa_packed_kv4_read(const int64_t* a) {
+    using packed::Ptr;
+    return moa_kv4_read(Ptr{a[0]}, Ptr{a[1]}, Ptr{a[2]}, Ptr{a[3]}, Ptr{a[4]}, Ptr{a[5]}, a[6], a[7], a[8], a[9],
+                        a[10], a[11], a[12], a + 13, a + 17, (int)a[21], Ptr{a[22]});
+}
+
+int moa_packed_kv4_attn_fwd(const int64_t* a) {
+    using packed::Ptr;
+    return moa_kv4_attn_fwd(Ptr{a[0]}, Ptr{a[1]}, Ptr{a[2]}, Ptr{a[3]}, Ptr{a[4]}, Ptr{a[5]}, Ptr{a[6]}, a[7], a[8],
+                            a[9], a[10], a[11], a[12], a[13], a[14], a[15], a + 16, a + 20, packed::real(a[24]),
+                            (int)a[25], (int)a[26], Ptr{a[27]}, (size_t)a[28], (int)a[29], Ptr{a[30]});
 }
 
 }  // extern "C"

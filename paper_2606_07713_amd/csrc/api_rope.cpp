@@ -5,6 +5,7 @@
 
 #include "../../include/moa_rope.h"
 #include "api_checks.h"
+#include "packed.h"
 #include "rope.h"
 
 namespace {
@@ -231,6 +232,25 @@ int moa_qk_norm_rope_bwd(const void* Q, const void* K, const void* dQo, const vo
     }
     p.ws = static_cast<float*>(workspace);
     return hip_status(launch_rope_bwd(p, static_cast<hipStream_t>(stream)));
+}
+
+// Words: the arguments in their order, but 4 for each tensor's strides (the last
+// not read), and a flag and 4 for the sections.
+int moa_packed_qk_norm_rope(const int64_t* a) {
+    using packed::Ptr;
+    return moa_qk_norm_rope(Ptr{a[0]}, Ptr{a[1]}, Ptr{a[2]}, Ptr{a[3]}, Ptr{a[4]}, Ptr{a[5]}, Ptr{a[6]}, Ptr{a[7]},
+                            a[8], a[9], a[10], a[11], a[12], a[13], a + 14, a + 18, a + 22, a + 26, (int)a[30],
+                            a[31] ? a + 32 : nullptr, (int)a[36], packed::real(a[37]), (int)a[38], (int)a[39],
+                            Ptr{a[40]});
+}
+
+int moa_packed_qk_norm_rope_bwd(const int64_t* a) {
+    using packed::Ptr;
+    return moa_qk_norm_rope_bwd(Ptr{a[0]}, Ptr{a[1]}, Ptr{a[2]}, Ptr{a[3]}, Ptr{a[4]}, Ptr{a[5]}, Ptr{a[6]},
+                                Ptr{a[7]}, Ptr{a[8]}, Ptr{a[9]}, Ptr{a[10]}, Ptr{a[11]}, a[12], a[13], a[14], a[15],
+                                a[16], a[17], a + 18, a + 22, a + 26, a + 30, a + 34, a + 38, (int)a[42],
+                                a[43] ? a + 44 : nullptr, (int)a[48], packed::real(a[49]), (int)a[50], (int)a[51],
+                                Ptr{a[52]}, (size_t)a[53], Ptr{a[54]});
 }
 
 }  // extern "C"

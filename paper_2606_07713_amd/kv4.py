@@ -12,7 +12,7 @@ import functools
 import math
 
 from . import MOA_BF16, MOA_F32, _DTYPE_CODES, _stream_handle, _torch as torch
-from ._call import (Function, check_list, check_rows, ci, f32, i64, is_list, new_like, on_stream, run, strides3, sz, vp,
+from ._call import (Function, Packed, check_list, check_rows, ci, f32, i64, is_list, new_like, on_stream, run, sz, vp,
                     workspace as _workspace)
 
 moa_kv4_page_bytes = Function("moa_kv4_page_bytes", [i64] * 2, sz)
@@ -25,6 +25,9 @@ moa_kv4_attn_workspace_bytes = Function("moa_kv4_attn_workspace_bytes", _SPLIT, 
 moa_kv4_attn_fwd = Function(
     "moa_kv4_attn_fwd", [vp] * 7 + [i64] * 9 + [vp, vp, f32, ci, ci, vp, sz, ci, vp])
 
+_write = Packed("moa_packed_kv4_write", "6q 7q 8q 2q")
+_read = Packed("moa_packed_kv4_read", "6q 7q 8q 2q")
+_attn = Packed("moa_packed_kv4_attn_fwd", "7q 9q 8q d 2q 4q")
 _ws_bytes = functools.lru_cache(maxsize=1024)(moa_kv4_attn_workspace_bytes)
 if torch is not None:   # the C functions above need none
     _int32, _uint8, _bf16 = torch.int32, torch.uint8, torch.bfloat16
@@ -58,7 +61,7 @@ def _place(cache, d, B, seq_lens, new_lens, page_table, device):
     page = _page_of(size, d)
     if not is_list(seq_lens, (B,), _int32, device):
         check_list("seq_lens", seq_lens, (B,), _int32, device)
-    new = table = None
+    new = table = 0
     if new_lens is not None:
         check_list("new_lens", new_lens, (B,), _int32, device)
         new = new_lens.data_ptr()
@@ -89,8 +92,8 @@ def kv4_write(k, v, cache, seq_lens, page_table=None, new_lens=None, stream=None
     heads, page, num_pages, max_pages, pool, lens, new, table = _place(cache, d, B, seq_lens, new_lens, page_table, device)
     if Hk != heads:
         raise ValueError(f"k has {Hk} heads, the cache {heads}")
-    run(moa_kv4_write, device, (k.data_ptr(), v.data_ptr(), pool, lens, new, table, B, Hk, N, d, page, num_pages, max_pages,
-                                strides3(ks), strides3(vs), _DTYPE_CODES[k.dtype], _stream_handle(None, k)))
+    run(_write, device, k.data_ptr(), v.data_ptr(), pool, lens, new, table, B, Hk, N, d, page, num_pages, max_pages,
+        *ks, *vs, _DTYPE_CODES[k.dtype], _stream_handle(None, k))
 
 
 def kv4_read(cache, N, d, seq_lens, page_table=None, new_lens=None, out_dtype=None, k_out=None, v_out=None,
@@ -119,9 +122,8 @@ def kv4_read(cache, N, d, seq_lens, page_table=None, new_lens=None, out_dtype=No
         v_out = new_like(k_out)
     else:
         check_rows("v_out", v_out, n, dt, device)
-    run(moa_kv4_read, device, (pool, k_out.data_ptr(), v_out.data_ptr(), lens, new, table, B, heads, N, d, page, num_pages,
-                               max_pages, strides3(k_out.stride()), strides3(v_out.stride()), _DTYPE_CODES[dt],
-                               _stream_handle(None, cache)))
+    run(_read, device, pool, k_out.data_ptr(), v_out.data_ptr(), lens, new, table, B, heads, N, d, page, num_pages,
+        max_pages, *k_out.stride(), *v_out.stride(), _DTYPE_CODES[dt], _stream_handle(None, cache))
     return k_out, v_out
 
 
@@ -157,8 +159,8 @@ def kv4_attn_fwd(q, cache, seq_lens, page_table=None, new_lens=None, scale=None,
         if need:
             workspace = q.new_empty(need, dtype=_uint8)
     ws, ws_n = _workspace(workspace, device)
-    run(moa_kv4_attn_fwd, device, (
-        q.data_ptr(), pool, out.data_ptr(), lse.data_ptr() if return_lse else None, lens, new, table, B, Hq, heads, N, d,
-        page, num_pages, max_pages, max_len, strides3(qs), strides3(out.stride()), 1.0 / math.sqrt(d) if scale is None else scale, causal,
-        MOA_F32 if odt is torch.float32 else MOA_BF16, ws, ws_n, num_splits, _stream_handle(None, q)))
+    run(_attn, device, q.data_ptr(), pool, out.data_ptr(), lse.data_ptr() if return_lse else 0, lens, new, table, B, Hq,
+        heads, N, d, page, num_pages, max_pages, max_len, *qs, *out.stride(),
+        1.0 / math.sqrt(d) if scale is None else scale, causal, MOA_F32 if odt is torch.float32 else MOA_BF16, ws, ws_n,
+        num_splits, _stream_handle(None, q))
     return (out, lse) if return_lse else out

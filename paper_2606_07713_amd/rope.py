@@ -4,7 +4,7 @@ from __future__ import annotations
 import functools
 
 from . import MOA_F32, _DTYPE_CODES, _stream_handle, _torch as torch
-from ._call import (Function, array, check_list, check_rows, ci, f32, i64, is_list, new_like, on_stream, run, strides3, sz, vp,
+from ._call import (Function, Packed, check_list, check_rows, ci, f32, i64, is_list, new_like, on_stream, run, sz, vp,
                     workspace as _workspace)
 
 _SIZES = [i64] * 6
@@ -16,7 +16,11 @@ moa_qk_norm_rope_bwd = Function(
     [vp] * 12 + _SIZES + [vp] * 6 + [ci, vp, ci, f32, ci, ci, vp, sz, vp])
 moa_qk_norm_rope_bwd_workspace_bytes = Function("moa_qk_norm_rope_bwd_workspace_bytes", [i64] * 5, sz)
 
+_HOW = "q 5q q d 2q"   # axes, sections with a flag before, interleaved, eps, types
+_fwd = Packed("moa_packed_qk_norm_rope", "8q 6q 16q" + _HOW + "q")
+_bwd = Packed("moa_packed_qk_norm_rope_bwd", "12q 6q 24q" + _HOW + "3q")
 _bwd_ws_bytes = functools.lru_cache(maxsize=1024)(moa_qk_norm_rope_bwd_workspace_bytes)
+_NONE4, _NONE5 = (0,) * 4, (0,) * 5   # strides and sections that are not there
 if torch is not None:   # the C functions above need none
     _int64, _float32, _empty_like = torch.int64, torch.float32, torch.empty_like
 
@@ -40,14 +44,14 @@ def _weight(name, w, d, device):
 
 def _common(q, k, positions, inv_freq, q_weight, k_weight, sections):
     """Checks what forward and backward share.  (shape of q, of k, strides of q, of k, device,
-    rot, axes, host array of the sections, weight type, addresses)."""
+    rot, axes, sections with a flag before, weight type, addresses)."""
     qn = q.shape
     device = q.get_device()
     qs = q.stride()
     if len(qn) != 4 or device < 0 or q.dtype not in _DTYPE_CODES or qs[3] != 1:
         check_rows("q", q)
     B, _, N, d = qn
-    kn, ks, kp = (B, 0, N, d), (0, 0, 0), None
+    kn, ks, kp = (B, 0, N, d), _NONE4, 0
     if k is not None:
         kn = k.shape
         if len(kn) != 4 or kn[0] != B or kn[2] != N or kn[3] != d:
@@ -56,25 +60,25 @@ def _common(q, k, positions, inv_freq, q_weight, k_weight, sections):
         kp = k.data_ptr()
     elif k_weight is not None:
         raise ValueError("k_weight without k")
-    wcode, wq, wk = MOA_F32, None, None
+    wcode, wq, wk = MOA_F32, 0, 0
     if q_weight is not None:
         wcode = _weight("q_weight", q_weight, d, device)
         wq = q_weight.data_ptr()
     if k_weight is not None:
         code = _weight("k_weight", k_weight, d, device)
-        if wq is not None and code != wcode:
+        if q_weight is not None and code != wcode:
             raise TypeError("q_weight and k_weight must share one dtype")
         wcode, wk = code, k_weight.data_ptr()
-    rot, freq = 0, None
+    rot, freq = 0, 0
     if inv_freq is not None:
         n = inv_freq.shape[0] if inv_freq.dim() == 1 else -1
         if not is_list(inv_freq, (n,), _float32, device):
             check_list("inv_freq", inv_freq, (n,), _float32, device)
         rot, freq = 2 * n, inv_freq.data_ptr()
-    axes, sec = 1, None
-    if sections is not None:
-        axes, sec = len(sections), array(sections)
-    pos = None
+    axes, sec = 1, _NONE5
+    if sections is not None:   # more than four are refused by their number
+        axes, sec = len(sections), (1, *map(int, sections), 0, 0, 0, 0)[:5]
+    pos = 0
     if positions is not None:
         shape = (B, N) if sections is None else (axes, B, N)
         if not is_list(positions, shape, _int64, device):
@@ -104,15 +108,14 @@ def qk_norm_rope(q, k=None, positions=None, inv_freq=None, q_weight=None, k_weig
     if q_out is None:
         q_out = new_like(q)
     qos = _like("q_out", q_out, q, qn, device)
-    kos, kop = ks, None
+    kos, kop = ks, 0
     if k is not None:
         if k_out is None:
             k_out = new_like(k)
         kos, kop = _like("k_out", k_out, k, kn, device), k_out.data_ptr()
     B, Hq, N, d = qn
-    run(moa_qk_norm_rope, device, (
-        qp, kp, q_out.data_ptr(), kop, wq, wk, pos, freq, B, Hq, kn[1], N, d, rot, strides3(qs), strides3(ks),
-        strides3(qos), strides3(kos), axes, sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, _stream_handle(None, q)))
+    run(_fwd, device, qp, kp, q_out.data_ptr(), kop, wq, wk, pos, freq, B, Hq, kn[1], N, d, rot, *qs, *ks, *qos, *kos,
+        axes, *sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, _stream_handle(None, q))
     return q_out, (None if k is None else k_out)
 
 
@@ -134,21 +137,20 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, positions=None, inv_freq=None, q_weig
     if dq is None:
         dq = new_like(q)
     gqs, dqs = _like("dq_out", dq_out, q, qn, device), _like("dq", dq, q, qn, device)
-    gks, dks, gkp, dkp = ks, ks, None, None
+    gks, dks, gkp, dkp = ks, ks, 0, 0
     if k is not None:
         if dk is None:
             dk = new_like(k)
         gks, dks = _like("dk_out", dk_out, k, kn, device), _like("dk", dk, k, kn, device)
         gkp, dkp = dk_out.data_ptr(), dk.data_ptr()
     B, Hq, N, d = qn
-    dwq = None if wq is None else _empty_like(q_weight, dtype=_float32)
-    dwk = None if wk is None else _empty_like(k_weight, dtype=_float32)
-    if workspace is None and (wq is not None or wk is not None):
+    dwq = None if q_weight is None else _empty_like(q_weight, dtype=_float32)
+    dwk = None if k_weight is None else _empty_like(k_weight, dtype=_float32)
+    if workspace is None and (dwq is not None or dwk is not None):
         workspace = q.new_empty(_bwd_ws_bytes(B, Hq, kn[1], N, d), dtype=torch.uint8)
     ws, ws_n = _workspace(workspace, device)
-    run(moa_qk_norm_rope_bwd, device, (
-        qp, kp, dq_out.data_ptr(), gkp, wq, wk, pos, freq, dq.data_ptr(), dkp, None if dwq is None else dwq.data_ptr(),
-        None if dwk is None else dwk.data_ptr(), B, Hq, kn[1], N, d, rot, strides3(qs), strides3(ks), strides3(gqs),
-        strides3(gks), strides3(dqs), strides3(dks), axes, sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, ws,
-        ws_n, _stream_handle(None, q)))
+    run(_bwd, device, qp, kp, dq_out.data_ptr(), gkp, wq, wk, pos, freq, dq.data_ptr(), dkp,
+        0 if dwq is None else dwq.data_ptr(), 0 if dwk is None else dwk.data_ptr(), B, Hq, kn[1], N, d, rot, *qs, *ks,
+        *gqs, *gks, *dqs, *dks, axes, *sec, interleaved, eps, _DTYPE_CODES[q.dtype], wcode, ws, ws_n,
+        _stream_handle(None, q))
     return dq, (None if k is None else dk), dwq, dwk

@@ -13,6 +13,8 @@ HEADERS = {"moa_rope.h": ["moa_qk_norm_rope", "moa_qk_norm_rope_bwd", "moa_qk_no
                          "moa_kv4_page_bytes", "moa_kv4_read", "moa_kv4_write"]}
 
 moa = pytest.importorskip("paper_2606_07713_amd", reason="HIP library not built")
+from paper_2606_07713_amd import kv4, rope  # noqa: E402
+
 P = 1 << 20          # addresses that nothing is read at: every call here is refused, or has no rows
 
 
@@ -216,3 +218,43 @@ def test_torch_wrappers_refuse_a_stream_of_another_device():
                  lambda: moa.kv4_attn_fwd(x, cache, lens, stream=stream)):
         with pytest.raises(ValueError, match="stream of cuda:1"):
             call()
+
+
+# entry point: its record's function; which argument counts the heads of each strides argument; those of
+# tokens and head size; that of the sections
+RECORDS = {
+    "moa_qk_norm_rope": (rope._fwd, {14: 9, 15: 10, 16: 9, 17: 10}, 11, 12, 19),
+    "moa_qk_norm_rope_bwd": (rope._bwd, {18: 13, 19: 14, 20: 13, 21: 14, 22: 13, 23: 14}, 15, 16, 25),
+    "moa_kv4_write": (kv4._write, {13: 7, 14: 7}, 8, 9, None),
+    "moa_kv4_read": (kv4._read, {13: 7, 14: 7}, 8, 9, None),
+    "moa_kv4_attn_fwd": (kv4._attn, {16: 8, 17: 8}, 10, 11, None),
+}
+
+
+def _as_record(name):
+    """The entry point ``name``, called through the record that the torch wrappers hand over."""
+    packed, strides, tokens, size, sections = RECORDS[name]
+
+    def call(*args):
+        words = []
+        for i, x in enumerate(args):
+            if i in strides:
+                h, n, d = args[strides[i]], args[tokens], args[size]
+                words += [*(x or (h * n * d, n * d, d)), 1]
+            elif i == sections:
+                words += (1, *x, 0, 0, 0, 0)[:5] if x else (0,) * 5
+            else:
+                words.append(0 if x is None else x)
+        return packed(packed.pack(*words))
+    return call
+
+
+@pytest.mark.parametrize("name,call,bad", [
+    ("moa_qk_norm_rope", _rope, ROPE_BAD), ("moa_qk_norm_rope_bwd", _rope_bwd, ROPE_BWD_BAD),
+    ("moa_kv4_write", lambda **kw: _rows(moa.moa_kv4_write, **kw), KV4_BAD),
+    ("moa_kv4_read", lambda **kw: _rows(moa.moa_kv4_read, **kw), KV4_BAD), ("moa_kv4_attn_fwd", _attn, ATTN_BAD)])
+def test_records_hand_over_every_argument(monkeypatch, name, call, bad):
+    monkeypatch.setattr(moa, name, _as_record(name))
+    for kw, status in bad:
+        if not any(isinstance(x, int) and abs(x) >= 1 << 31 for x in kw.values()):   # strides of such sizes pass 64 bits
+            assert call(**kw) == status, kw
