@@ -534,13 +534,13 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Attn p) {
 template <int D, int RT>
 hipError_t go(const Kv4Attn& p, hipStream_t stream) {
     const int rows = p.c.n * (p.hq / p.c.hk), tiles = (rows + 16 * RT - 1) / (16 * RT);
-    // A negative scale goes into the queries' signs; a factor of zero (or below
-    // the normal numbers) becomes the smallest normal one, whose weights round
-    // to 1 as well, so that masked scores keep the weight 0.
+    // A negative scale goes into the queries' signs; a factor of zero becomes the
+    // smallest one there is (kernels here keep subnormal numbers), whose weights
+    // round to 1 as well, so that masked scores keep the weight 0.
     float c = p.scale * kLog2e;
     const bool flip = c < 0.0f;
     c = flip ? -c : c;
-    if (c < std::numeric_limits<float>::min()) c = std::numeric_limits<float>::min();
+    if (c == 0.0f) c = std::numeric_limits<float>::denorm_min();
     const long long blocks = (long long)p.c.B * p.c.hk * tiles * p.splits;
     const auto run = [&](auto kernel) {
         return launch_kernel(kernel, dim3((unsigned)blocks), dim3(WAVES * 64), stream, p, c, flip, tiles);

@@ -317,6 +317,26 @@ def test_extreme_scores():
         _check_attn(q, cache, table, 64, lens, None, True, scale, o, lse)
 
 
+def test_no_and_almost_no_scale_against_huge_scores():
+    # scores of 0 and +-2^126 times 0: equal weights; times 2^-130: weights exp(0), exp(+-2^-4)
+    import torch
+    import paper_2606_07713_amd as moa
+    cache, table = _pool(1, 64, 64, 1, 64, torch.Generator().manual_seed(1))
+    k = torch.zeros((1, 1, 40, 64), device="cuda")
+    k[:, :, 1::3, 0], k[:, :, 2::3, 0] = 2.0 ** 63, -2.0 ** 63
+    v = torch.arange(40, device="cuda").remainder(3).eq(1).float()[None, None, :, None].expand(1, 1, 40, 64).contiguous()
+    moa.kv4_write(k, v, cache, _ints([40]), page_table=table)
+    q = torch.zeros((1, 1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 2.0 ** 63
+    for scale in (0.0, 2.0 ** -130, -2.0 ** -130):
+        o = moa.kv4_attn_fwd(q, cache, _ints([40]), page_table=table, causal=True, scale=scale, out_dtype=torch.float32)
+        for i, n in enumerate((39, 40)):
+            w = torch.exp(k[0, 0, :n, 0].double() * 2.0 ** 63 * scale)
+            want = (w * v[0, 0, :n, 0].double()).sum() / w.sum()
+            # weights rounded to bf16 (2^-8 of each, in a mean of zeros and ones), the sums to fp32
+            assert (o[0, 0, i].double() - want).abs().max() <= want * (2.0 ** -8 + 2.0 ** -18)
+
+
 def test_norm_rope_write_attend_together():
     """A prompt, then decoded tokens, as a layer uses them: projections' heads normalised and
     rotated, keys and values written, queries attending; eagerly and replayed from a graph."""
