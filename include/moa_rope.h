@@ -60,7 +60,9 @@ extern "C" {
  *
  * Computation: fp32 from exact inputs, one rounding at the end; angles in
  * fp64, reduced to one turn before sine and cosine are taken in fp32, so that
- * far positions lose nothing.  One kernel; deterministic.
+ * far positions lose nothing.  A row whose squares add up to more than fp32
+ * holds (elements of 2^60 and more) has a norm of infinity: y = 0.  One kernel;
+ * deterministic.
  */
 int moa_qk_norm_rope(const void* Q, const void* K, void* Qo, void* Ko, const void* wq,
                      const void* wk, const int64_t* positions, const float* inv_freq, int64_t B,

@@ -137,6 +137,13 @@ struct Turn {
     }
 };
 
+// 1 / sqrt(x).  The hardware's root takes a subnormal x for zero: such a mean
+// square (without an eps) is scaled first.
+__device__ __forceinline__ float inverse_root(float x) {
+    const bool tiny = x < 0x1p-100f;
+    return __builtin_amdgcn_rsqf(tiny ? x * 0x1p60f : x) * (tiny ? 0x1p30f : 1.0f);
+}
+
 // This lane's eight weights of tensor ts (1 without a norm).
 __device__ __forceinline__ void load_weights(const RopeProblem& p, int ts, int j, float (&w)[8]) {
 #pragma unroll
@@ -247,7 +254,7 @@ __global__ __launch_bounds__(THREADS) void rope_fwd_kernel(RopeProblem p, int lo
                 float sq = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sq = __builtin_fmaf(f[e], f[e], sq);
-                r = __builtin_amdgcn_rsqf(group_sum<LPR>(sq) * (1.0f / D) + p.eps);
+                r = inverse_root(group_sum<LPR>(sq) * (1.0f / D) + p.eps);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] = r * __builtin_fmaf(f[e], A[e], o[e] * Bp[e]);
@@ -337,7 +344,7 @@ __global__ __launch_bounds__(THREADS) void rope_bwd_kernel(RopeProblem p, int lo
                     for (int e = 0; e < 8; ++e) sq = __builtin_fmaf(f[e], f[e], sq);
                     sq = group_sum<LPR>(sq) * (1.0f / D) + p.eps;
                     const bool in = h0 + u * walk.step < limit;
-                    const float r = in ? __builtin_amdgcn_rsqf(sq) : 0.0f;
+                    const float r = in ? inverse_root(sq) : 0.0f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         f[e] *= r;

@@ -221,6 +221,26 @@ def test_infinity_outside_the_rotated_elements_stays_there():
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_whose_mean_square_is_subnormal(d):
+    # +-2^-66 everywhere: a mean square of exactly 2^-132, rows of +-1 times the weight
+    import torch
+    import paper_2606_07713_amd as moa
+    sign = torch.where(torch.rand((1, 2, 3, d), generator=torch.Generator().manual_seed(1)) < 0.5, -1.0, 1.0).to("cuda")
+    q = sign * 2.0 ** -66
+    w = torch.linspace(0.5, 2.0, d, device="cuda")
+    y = moa.qk_norm_rope(q, q_weight=w, eps=0.0)[0]
+    # a reciprocal root off by one unit (2^-23) and two roundings
+    assert ((y - sign * w).abs() <= 2.0 ** -22 * w).all()
+    g = torch.randn((1, 2, 3, d), generator=torch.Generator().manual_seed(2)).to("cuda")
+    dq, _, dw, _ = moa.qk_norm_rope_bwd(q, None, g, None, q_weight=w, eps=0.0)
+    want = (g * sign).double().sum((0, 1, 2))
+    assert ((dw.double() - want).abs() <= 16 * 2.0 ** -24 * g.double().abs().sum((0, 1, 2))).all()
+    gw = g.double() * w.double()
+    want = 2.0 ** 66 * (gw - sign * (gw * sign).mean(-1, keepdim=True))
+    assert ((dq.double() - want).abs() <= 2.0 ** 66 * (d + 16) * 2.0 ** -24 * gw.abs().amax(-1, keepdim=True)).all()
+
+
 def test_captured_call_replays():
     import torch
     import paper_2606_07713_amd as moa
