@@ -128,8 +128,8 @@ size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t N
  *           overlapping nothing (else MOA_ERR_WORKSPACE); NULL/0 when that is 0.
  *
  * Computation: bf16 matrix products with fp32 accumulation of the exact stored
- * values (bf16 holds them); softmax statistics in fp32, LSE from the fp32
- * weights; the weights are rounded to bf16 before they multiply V.  Stored NaN
+ * values (bf16 holds them); softmax statistics in fp32, from the fp32 weights; a
+ * weight multiplies V as the sum of two bf16 numbers, 17 bits.  Stored NaN
  * blocks and unset tokens do not touch rows that do not see them.  One kernel,
  * or two when the keys are split; no atomics, deterministic.
  */

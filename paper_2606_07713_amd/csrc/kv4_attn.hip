@@ -13,7 +13,10 @@
 // their power of two, exactly.  The S^T accumulators leave a lane with the four
 // keys 16 t + 4 g .. of row n = lane % 16 -- and since the order of the keys
 // in a product is free, two such accumulators, packed to bf16, are the B
-// operand of the second product as they are.
+// operand of the second product as they are.  That product is taken twice, with
+// the weights' nearest bf16 numbers and with those of what these leave: one
+// bf16 number per weight (2^-9) would be off by as much as a bf16 output is by
+// itself, and by far more than an fp32 output.
 //
 // Softmax: a running reference per row, the maximum of the first tile that the
 // row sees; later tiles are weighed against it without looking for their own
@@ -54,6 +57,13 @@ __device__ __forceinline__ float column_sum(float x) {
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const bf16x2 t = {(__bf16)lo, (__bf16)hi};
     return __builtin_bit_cast(uint32_t, t);
+}
+
+// a and b as two bf16 numbers each: the nearest, and the nearest to the rest.
+// Together they hold 17 bits, 2^-18 of a weight at most is lost.
+__device__ __forceinline__ void two_terms(float a, float b, uint32_t& hi, uint32_t& lo) {
+    hi = pack2(a, b);
+    lo = pack2(a - bf16lo_to_f32(hi), b - bf16hi_to_f32(hi));
 }
 
 template <int B>
@@ -121,24 +131,21 @@ struct Tile {
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) a[i] = key8(k[T][i], s);
     }
-    // V^T operands of the 32 keys of groups 2 U and 2 U + 1 for the column's
-    // D/16 elements.
-    template <int U>
-    __device__ __forceinline__ void values(bf16x8 (&a)[D / 16]) const {
-        uint32_t r[D / 16][4];
-        quad<0>(v[2 * U], vs[2 * U], r);
-        quad<1>(v[2 * U + 1], vs[2 * U + 1], r);
+    // V^T operands of the 32 keys of groups 2 U and 2 U + 1 for elements 4 F .. of
+    // the column's D/16.
+    template <int U, int F>
+    __device__ __forceinline__ void values(bf16x8 (&a)[4]) const {
+        uint32_t r[4][4];
+        quad<0>(v[2 * U][2 * F], v[2 * U][2 * F + 1], vs[2 * U], r);
+        quad<1>(v[2 * U + 1][2 * F], v[2 * U + 1][2 * F + 1], vs[2 * U + 1], r);
 #pragma unroll
-        for (int e = 0; e < D / 16; ++e) a[e] = __builtin_bit_cast(bf16x8, make_uint4(r[e][0], r[e][1], r[e][2], r[e][3]));
+        for (int e = 0; e < 4; ++e) a[e] = __builtin_bit_cast(bf16x8, make_uint4(r[e][0], r[e][1], r[e][2], r[e][3]));
     }
+    // w01: keys 0, 1 of four elements, w23: keys 2, 3
     template <int H>
-    static __device__ __forceinline__ void quad(const uint32_t (&w)[D / 32], uint32_t s, uint32_t (&r)[D / 16][4]) {
-        const float s0 = scale_byte<0>(s), s1 = scale_byte<1>(s), s2 = scale_byte<2>(s), s3 = scale_byte<3>(s);
-#pragma unroll
-        for (int f = 0; f < D / 64; ++f) {   // four elements: dword 2 f has keys 0, 1, dword 2 f + 1 keys 2, 3
-            pair(w[2 * f], s0, s1, r[4 * f][2 * H], r[4 * f + 1][2 * H], r[4 * f + 2][2 * H], r[4 * f + 3][2 * H]);
-            pair(w[2 * f + 1], s2, s3, r[4 * f][2 * H + 1], r[4 * f + 1][2 * H + 1], r[4 * f + 2][2 * H + 1], r[4 * f + 3][2 * H + 1]);
-        }
+    static __device__ __forceinline__ void quad(uint32_t w01, uint32_t w23, uint32_t s, uint32_t (&r)[4][4]) {
+        pair(w01, scale_byte<0>(s), scale_byte<1>(s), r[0][2 * H], r[1][2 * H], r[2][2 * H], r[3][2 * H]);
+        pair(w23, scale_byte<2>(s), scale_byte<3>(s), r[0][2 * H + 1], r[1][2 * H + 1], r[2][2 * H + 1], r[3][2 * H + 1]);
     }
     static __device__ __forceinline__ void pair(uint32_t w, float sa, float sb, uint32_t& e0, uint32_t& e1, uint32_t& e2, uint32_t& e3) {
         const uint32_t a01 = values2<0>(w, sa), a23 = values2<1>(w, sa), b01 = values2<2>(w, sb), b23 = values2<3>(w, sb);
@@ -278,8 +285,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
                         if (64 * t + 16 * u + 4 * g + j >= seen[i]) s[i][u][j] = kNegInf;
         }
 
-        // The weights 2^(s c - ref) and their sums.
-        bf16x8 pt[RT][2];
+        // The weights 2^(s c - ref), each as two bf16 numbers, and their sums.
+        bf16x8 pt[RT][2], rest[RT][2];
         float sum[RT];
         const auto weights = [&]() {
 #pragma unroll
@@ -295,9 +302,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
                     }
                 sum[i] = x;
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    pt[i][u] = __builtin_bit_cast(bf16x8, make_uint4(pack2(w[2 * u][0], w[2 * u][1]), pack2(w[2 * u][2], w[2 * u][3]),
-                                                                     pack2(w[2 * u + 1][0], w[2 * u + 1][1]), pack2(w[2 * u + 1][2], w[2 * u + 1][3])));
+                for (int u = 0; u < 2; ++u) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) two_terms(w[2 * u + k / 2][2 * (k % 2)], w[2 * u + k / 2][2 * (k % 2) + 1], hi[k], lo[k]);
+                    pt[i][u] = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+                    rest[i][u] = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+                }
             }
         };
         // Against the present references, without a maximum, unless the tile is
@@ -332,17 +343,31 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
 #pragma unroll
         for (int i = 0; i < RT; ++i) l[i] += sum[i];
 
-        const auto product = [&](auto U) {
-            constexpr int u = decltype(U)::value;
-            bf16x8 a[E];
-            tile.template values<u>(a);
+        // The products of four elements follow their unpacking at once, so that the next
+        // four are unpacked while the matrix unit works.
+        const auto product = [&](auto U, auto F) {
+            constexpr int u = decltype(U)::value, f = decltype(F)::value;
+            if constexpr (f < D / 64) {
+                bf16x8 a[4];
+                tile.template values<u, f>(a);
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
+                for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[i][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[e], pt[i][u], o[i][e], 0, 0, 0);
+                    for (int e = 0; e < 4; ++e)
+                        o[i][4 * f + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[e], pt[i][u], o[i][4 * f + e], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[i][4 * f + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[e], rest[i][u], o[i][4 * f + e], 0, 0, 0);
+            }
         };
-        product(std::integral_constant<int, 0>{});
-        product(std::integral_constant<int, 1>{});
+        constexpr std::integral_constant<int, 0> zero;
+        constexpr std::integral_constant<int, 1> one;
+        product(zero, zero);
+        product(zero, one);
+        product(one, zero);
+        product(one, one);
 
         // A masked tile with blocks that hold a NaN: their elements become NaN
         // in the rows that see the key, counted by a product of ones.

@@ -47,3 +47,45 @@ def stored(cache, page, d, table, b, n):
         v = torch.where(c >= 8, -1.0, 1.0) * LEVELS[c % 8] * torch.exp2(s - 127)
         out.append(torch.where(s == 255, float("nan"), v).transpose(0, 1))
     return out
+
+
+U = 2.0 ** -24
+
+
+def attention(q, K, V, seen, scale):
+    """One head in fp64: q [n, d] over K, V [m, d] (CPU), row i sees the first seen[i] keys.
+    (O, LSE, sum P |V|, the largest scale * sum |q k| of a row)."""
+    hide = torch.arange(K.shape[0])[None] >= seen[:, None]
+    s = (q @ K.t() * scale).masked_fill(hide, -torch.inf)
+    lse = torch.logsumexp(s, -1)
+    p = torch.where(hide, 0.0, torch.exp(s - lse[:, None]))
+    held = torch.isnan(V)
+    V = torch.where(held, 0.0, V)
+    o, mag = p @ V, p @ V.abs()
+    o[(~hide).double() @ held.double() > 0] = torch.nan
+    sizes = (q.abs() @ torch.nan_to_num(K).abs().t()).masked_fill(hide, 0)
+    reach = sizes.amax(-1) * abs(scale) if K.shape[0] else sizes.sum(-1)
+    empty = seen <= 0
+    o[empty], mag[empty], lse[empty] = 0.0, 0.0, -torch.inf
+    return o, lse, mag, reach
+
+
+def attention_error(o, lse, ref, keys, d):
+    """The largest shares that O and LSE (fp64) take of their bounds, or a text that says what is
+    NaN or infinite where `ref` is not.
+
+    A weight goes into the product with V as two bf16 numbers, of which the second leaves half a
+    step of 2^-8 of a rest of at most 2^-9: 2^-18 of sum P |V|.  Scores are off by (d + 4) units of
+    2^-24 of scale * sum |q k|, which weights and sums have; fp32 sums of n terms add n / 64 + 64
+    units; the output's type adds half a step (given by its own rounding: fp32 here)."""
+    want, wl, mag, reach = ref
+    for name, got, right in (("O", o, want), ("LSE", lse, wl)):
+        for what, test in (("NaN", torch.isnan), ("infinite", torch.isinf)):
+            if not torch.equal(test(got), test(right)):
+                return f"{name}: {what} at {int((test(got) != test(right)).sum())} places"
+    ds, sums = (d + 4) * U * reach, (keys / 64 + 64) * U
+    live = torch.isfinite(wl)
+    lim = (2.0 ** -18 + 2 * ds[:, None] + sums) * mag + U * want.abs() + 1e-30
+    err = torch.nan_to_num((o - want).abs() / lim).amax().item() if o.numel() else 0.0
+    lerr = ((lse - wl).abs() / (ds + sums + 4 * U * wl.abs()))[live]
+    return err, lerr.amax().item() if lerr.numel() else 0.0
