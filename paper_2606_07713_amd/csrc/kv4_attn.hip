@@ -22,7 +22,7 @@
 // row sees; later tiles are weighed against it without looking for their own
 // maximum, and only a sum beyond 2^20 (scores 16 and more log2 units above the
 // reference; fp32 and bf16 hold such weights as well as small ones) raises it,
-// for the whole wave at once.  fp32 sums of the unrounded weights per lane,
+// for the whole wave at once, and so does a tile with values of 2^65 and more.  fp32 sums of the unrounded weights per lane,
 // joined over the lanes once at the end.
 //
 // What bounds it: with few rows the memory (64 sequences of 8192 keys, 8 stored
@@ -153,6 +153,13 @@ struct Tile {
         e1 = __builtin_amdgcn_perm(b01, a01, 0x07060302);
         e2 = __builtin_amdgcn_perm(b23, a23, 0x05040100);
         e3 = __builtin_amdgcn_perm(b23, a23, 0x07060302);
+    }
+    // Whether a value's scale is 2^65 or more (a byte of 192 and more).
+    __device__ __forceinline__ bool large_values() const {
+        uint32_t x = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) x |= vs[t] & (vs[t] << 1);
+        return (x & 0x80808080u) != 0;
     }
     // Value scales that no written block has (255: the block held a NaN; unset
     // memory) become 2^-127, a finite factor for keys that a row does not see.
@@ -312,11 +319,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
             }
         };
         // Against the present references, without a maximum, unless the tile is
-        // masked, a row has seen nothing yet or a sum comes out too large.
+        // masked, a row has seen nothing yet, a sum comes out too large or the
+        // values are so large themselves (2^22 of weight a tile, 2^25 tiles: below
+        // 2^65 the products stay in fp32) that weights above 1 are not for them.
         bool raise = masked || !ready;
         if (!raise) {
             weights();
-            bool large = false;
+            bool large = tile.large_values();
 #pragma unroll
             for (int i = 0; i < RT; ++i) large |= sum[i] > kLargeSum;
             raise = wave_any(large);

@@ -3,7 +3,7 @@ bounds of a few units of fp32 but for the weights' own 2^-18 (``kv4_util.attenti
 import pytest
 
 from kv4_util import attention, attention_error, stored
-from test_kv4_gpu import ATTNS, _cache_of, _ints
+from test_kv4_gpu import ATTNS, _cache_of, _ints, _pool
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +41,25 @@ def test_weights_keep_their_digits(case):
                               causal=causal, scale=scale, num_splits=splits, out_dtype=torch.float32, return_lse=True)
     torch.cuda.synchronize()
     check(q, cache, table, page, lens, new, causal, scale, o, lse)
+
+
+@pytest.mark.parametrize("d,N,splits", [(64, 1, 1), (128, 1, 3), (128, 40, 1)])
+def test_values_near_the_largest_that_the_format_holds(d, N, splits):
+    # later keys weigh up to 2^14 times the first tile's, the values are +-2^112 to 6 * 2^112: sums of 2^14 V
+    # leave fp32, the results do not
+    import torch
+    import paper_2606_07713_amd as moa
+    n, page = 64 * 24, 64
+    cache, table = _pool(1, n, page, 1, d, torch.Generator().manual_seed(1))
+    gen = torch.Generator().manual_seed(2)
+    k = torch.zeros((1, 1, n, d))
+    k[0, 0, :, 0] = torch.arange(n) // 64 // 12 * 8.0 + torch.randint(0, 3, (n,), generator=gen)
+    v = torch.randint(1, 7, (1, 1, n, d), generator=gen) * 2.0 ** 112
+    v[0, 0, :, ::2] *= -1
+    moa.kv4_write(k.to("cuda"), v.to("cuda"), cache, _ints([n]), page_table=table)
+    q = torch.zeros((1, 1, N, d), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    o, lse = moa.kv4_attn_fwd(q, cache, _ints([n]), page_table=table, scale=1.0, num_splits=splits, return_lse=True,
+                              out_dtype=torch.float32)
+    torch.cuda.synchronize()
+    check(q, cache, table, page, [n], None, False, 1.0, o, lse)
