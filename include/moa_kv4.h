@@ -121,7 +121,7 @@ size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t N
  *           as for moa_kv4_write, Hq a multiple of Hk; supported:
  *           B * Hq * N < 2^26, and fewer than 2^24 workgroups (of 16 rows of one
  *           key/value head and one key split, or 32 where a head has more).
- * scale     finite; 0 and negative values are valid.
+ * scale     finite, at most 2^127 in size; 0 and negative values are valid.
  * max_len   as above (0: the capacity).  Any value is right; a good one is fast.
  * workspace, workspace_bytes
  *           at least moa_kv4_attn_workspace_bytes(...) bytes, 16-byte aligned,
@@ -129,7 +129,10 @@ size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t N
  *
  * Computation: bf16 matrix products with fp32 accumulation of the exact stored
  * values (bf16 holds them); softmax statistics in fp32, from the fp32 weights; a
- * weight multiplies V as the sum of two bf16 numbers, 17 bits.  Stored NaN
+ * weight multiplies V as the sum of two bf16 numbers, 17 bits.  A score whose
+ * product with scale * log2(e) is not below fp32's largest number makes its row
+ * NaN, one that is below fp32's lowest weighs nothing, and a row that sees only
+ * such is NaN (LSE: infinite, of that sign).  Stored NaN
  * blocks and unset tokens do not touch rows that do not see them.  One kernel,
  * or two when the keys are split; no atomics, deterministic.
  */

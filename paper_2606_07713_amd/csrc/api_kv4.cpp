@@ -16,6 +16,7 @@ using namespace moa;
 constexpr int64_t kLim = std::numeric_limits<int32_t>::max();
 constexpr int64_t kMaxPage = int64_t(1) << 20;
 constexpr int kMaxSplits = 256;
+constexpr float kMaxScale = 0x1p127f;   // times log2(e) is still finite
 // Workgroups of 256 threads in one launch: its threads are counted in 32 bits.
 constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;
 
@@ -224,6 +225,7 @@ int moa_kv4_attn_fwd(const void* Q, const void* cache, void* O, float* LSE, cons
     int st = check_dims(s);
     if (st) return st;
     if (!attn_sizes_ok(B, Hq, Hk, N, d, page, max_pages, max_len, num_splits)) return MOA_ERR_UNSUPPORTED;
+    if (std::fabs(scale) > kMaxScale) return MOA_ERR_UNSUPPORTED;
     const Strides sq = strides_of(q_strides, B, Hq, N, d), so = strides_of(o_strides, B, Hq, N, d);
     const size_t oes = out_dtype == MOA_F32 ? 4 : 2;
     if ((st = check_tensor(Q, sq, B, Hq, N, d, 2, false)) || (st = check_tensor(O, so, B, Hq, N, d, oes, true))) return st;

@@ -31,6 +31,7 @@
 // tile of 16 rows takes a SIMD 1860 cycles from the caches, 325 vector and 32
 // matrix instructions; of 32 rows 2950): 32 heads on 8, 8192 causal queries, d =
 // 128, 588 us, 0.94 PFLOP/s.  Short calls are chains of latencies.
+#include <cfloat>
 #include <limits>
 
 #include "kv4_common.h"
@@ -339,7 +340,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
                 for (int u = 0; u < 4; ++u)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) x = fmaxf(x, s[i][u][j]);
-                x = fmaxf(ref[i], column_max(x) * c);
+                // Finite for a row that sees a key of the tile, whatever its scores: -inf
+                // is the mark of rows that have seen none.  A score beyond fp32 leaves an
+                // infinite weight or none at all, and the row NaN.
+                x = fminf(column_max(x) * c, FLT_MAX);
+                if (64 * t < seen[i]) x = fmaxf(x, -FLT_MAX);
+                x = fmaxf(ref[i], x);
                 const float a = ref[i] == kNegInf ? 0.0f : exp2_hw(ref[i] - x);
                 ref[i] = x;
                 l[i] *= a;
@@ -473,8 +479,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
             }
             continue;
         }
-        // no visible key: a sum of 0 (a row whose scores are all NaN has a NaN sum)
-        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+        const bool none = M == kNegInf;   // no visible key
+        const float inv = none ? 0.0f : 1.0f / L;
         const long long to = b * p.os[0] + hh * p.os[1] + qi * p.os[2] + d8;
         if (p.out_bf16) {
             *reinterpret_cast<uint4*>(static_cast<u16*>(p.o) + to) =
@@ -484,12 +490,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
             dst[0] = make_float4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
             dst[1] = make_float4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv);
         }
-        if (p.lse && d8 == 0) p.lse[at] = L == 0.0f ? kNegInf : (M + __log2f(L)) * kLn2;
+        if (p.lse && d8 == 0) p.lse[at] = none ? kNegInf : (M + __log2f(L)) * kLn2;
     }
 }
 
-// Exact join of a row's key splits; splits without a visible key have a sum of
-// 0.  The pass is a chain of load latencies, so W waves share a row (1, or 4
+// Exact join of a row's key splits; splits without a visible key have a reference
+// of -inf and sums of 0.  The pass is a chain of load latencies, so W waves share a row (1, or 4
 // for more than 4 splits), each takes U of its splits at a time, and all of
 // these loads are in flight together: up to 32 splits cost one latency.
 template <int D, int W>
@@ -521,8 +527,8 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Attn p) {
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (s0 + u * W >= p.splits) ls[u] = 0.0f;
-            if (ls[u] != 0.0f) top = fmaxf(top, ms[u]);
+            if (s0 + u * W >= p.splits) ms[u] = kNegInf;
+            top = fmaxf(top, ms[u]);
         }
         const float alpha = M == kNegInf ? 0.0f : exp2_hw(M - top);
         M = top;
@@ -530,7 +536,7 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Attn p) {
         o *= alpha;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (ls[u] == 0.0f) continue;
+            if (ms[u] == kNegInf) continue;
             const float w = exp2_hw(ms[u] - M);
             L += w * ls[u];
             o += w * a[u];
@@ -547,14 +553,15 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Attn p) {
         o = 0.0f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            if (part_l[w] == 0.0f) continue;
+            if (part_m[w] == kNegInf) continue;
             const float f = exp2_hw(part_m[w] - top);
             L += f * part_l[w];
             o += f * part[w][lane];
         }
         M = top;
     }
-    o *= L == 0.0f ? 0.0f : 1.0f / L;
+    const bool none = M == kNegInf;   // no visible key
+    o *= none ? 0.0f : 1.0f / L;
     const long long to = b * p.os[0] + hh * p.os[1] + i * p.os[2] + PER * lane;
     if (p.out_bf16) {
         typedef __bf16 out __attribute__((ext_vector_type(PER)));
@@ -562,7 +569,7 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Attn p) {
     } else {
         *reinterpret_cast<vec*>(static_cast<float*>(p.o) + to) = o;
     }
-    if (p.lse && lane == 0) p.lse[row] = L == 0.0f ? kNegInf : (M + __log2f(L)) * kLn2;
+    if (p.lse && lane == 0) p.lse[row] = none ? kNegInf : (M + __log2f(L)) * kLn2;
 }
 
 template <int D, int RT>

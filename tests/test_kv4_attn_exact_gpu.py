@@ -63,3 +63,28 @@ def test_values_near_the_largest_that_the_format_holds(d, N, splits):
                               out_dtype=torch.float32)
     torch.cuda.synchronize()
     check(q, cache, table, page, [n], None, False, 1.0, o, lse)
+
+
+def test_scores_that_leave_fp32_do_not_pass_for_rows_that_see_nothing():
+    # scores of +-2^126 times 8: the row is NaN; a score that overflows downwards beside others weighs nothing
+    import torch
+    import paper_2606_07713_amd as moa
+    cache, table = _pool(1, 1024, 64, 1, 64, torch.Generator().manual_seed(1))
+    for n, splits in ((3, 1), (700, 1), (700, 4)):
+        k = torch.zeros((1, 1, n, 64), device="cuda")
+        v = torch.ones_like(k)
+        for sign in (1.0, -1.0):
+            k[..., 0] = sign * 2.0 ** 63
+            moa.kv4_write(k, v, cache, _ints([n]), page_table=table)
+            q = torch.zeros((1, 2, 1, 64), dtype=torch.bfloat16, device="cuda")
+            q[..., 0] = 2.0 ** 63
+            o, lse = moa.kv4_attn_fwd(q, cache, _ints([n]), page_table=table, scale=8.0, num_splits=splits, return_lse=True)
+            assert torch.isnan(o).all(), (n, splits, sign)
+            assert torch.equal(lse, torch.full_like(lse, sign * float("inf"))), (n, splits, sign)
+        k[..., ::3, 0] = 0
+        moa.kv4_write(k, v, cache, _ints([n]), page_table=table)
+        o, lse = moa.kv4_attn_fwd(q, cache, _ints([n]), page_table=table, scale=8.0, num_splits=splits, return_lse=True,
+                                  out_dtype=torch.float32)
+        want = torch.tensor(float(-(-n // 3)), dtype=torch.float64).log()
+        # equal weights of one: sums exact, a logarithm and its products
+        assert (o == 1).all() and ((lse.cpu().double() - want).abs() <= 4 * 2.0 ** -24 * want).all()
