@@ -60,9 +60,10 @@ extern "C" {
  *
  * Computation: fp32 from exact inputs, one rounding at the end; angles in
  * fp64, reduced to one turn before sine and cosine are taken in fp32, so that
- * far positions lose nothing.  A row whose squares add up to more than fp32
- * holds (elements of 2^60 and more) has a norm of infinity: y = 0.  One kernel;
- * deterministic.
+ * far positions lose nothing.  Rows whose squares leave fp32 (elements of 2^60
+ * and more, or below 2^-45 with an eps too small to hide them) are divided by a
+ * power of two first and lose nothing either, with weights below 2^60; a row of
+ * zeros without an eps is 0 / 0, NaN.  One kernel; deterministic.
  */
 int moa_qk_norm_rope(const void* Q, const void* K, void* Qo, void* Ko, const void* wq,
                      const void* wk, const int64_t* positions, const float* inv_freq, int64_t B,

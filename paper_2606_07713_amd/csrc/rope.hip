@@ -17,6 +17,8 @@
 // reduced to one turn (fp32 angles of position 10^6 would be off by 0.06).
 // Partners are eight-element chunks of another lane of the group (rot/2 is a
 // multiple of 8), or neighbours in the same lane when pairs are interleaved.
+#include <cfloat>
+
 #include "device_common.h"
 #include "rope.h"
 
@@ -24,7 +26,6 @@ namespace moa {
 namespace {
 
 constexpr int THREADS = 256;
-
 // The rows written are not read again here; stores that pass the caches by
 // leave them to the rows read (16 heads each of 8192 tokens, bf16, d = 128: 33.2
 // -> 29.0 us, the gradients 53.3 -> 44.8; loads past the caches gained nothing).
@@ -44,12 +45,13 @@ struct Chunk<u16> {
         f[4] = bf16lo_to_f32(a.z); f[5] = bf16hi_to_f32(a.z);
         f[6] = bf16lo_to_f32(a.w); f[7] = bf16hi_to_f32(a.w);
     }
+    __device__ __forceinline__ void set(const float (&f)[8]) { a = pack(f); }
     __device__ __forceinline__ Chunk from_lane(int lane) const {
         Chunk r;
         r.a = make_uint4(__shfl(a.x, lane), __shfl(a.y, lane), __shfl(a.z, lane), __shfl(a.w, lane));
         return r;
     }
-    static __device__ __forceinline__ void store(u16* p, const float (&f)[8]) {
+    static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
         typedef __bf16 v2 __attribute__((ext_vector_type(2)));
         uint32_t w[4];
 #pragma unroll
@@ -57,7 +59,10 @@ struct Chunk<u16> {
             const v2 t = {(__bf16)f[2 * i], (__bf16)f[2 * i + 1]};
             w[i] = __builtin_bit_cast(uint32_t, t);
         }
-        store16(p, u32x4{w[0], w[1], w[2], w[3]});
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static __device__ __forceinline__ void store(u16* p, const float (&f)[8]) {
+        store16(p, __builtin_bit_cast(u32x4, pack(f)));
     }
 };
 template <>
@@ -71,6 +76,10 @@ struct Chunk<float> {
     __device__ __forceinline__ void get(float (&f)[8]) const {
         f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
         f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    }
+    __device__ __forceinline__ void set(const float (&f)[8]) {
+        a = make_float4(f[0], f[1], f[2], f[3]);
+        b = make_float4(f[4], f[5], f[6], f[7]);
     }
     __device__ __forceinline__ Chunk from_lane(int lane) const {
         Chunk r;
@@ -137,11 +146,41 @@ struct Turn {
     }
 };
 
-// 1 / sqrt(x).  The hardware's root takes a subnormal x for zero: such a mean
-// square (without an eps) is scaled first.
-__device__ __forceinline__ float inverse_root(float x) {
-    const bool tiny = x < 0x1p-100f;
-    return __builtin_amdgcn_rsqf(tiny ? x * 0x1p60f : x) * (tiny ? 0x1p30f : 1.0f);
+// Mean of a row's squares; f: this lane's elements.
+template <int LPR>
+__device__ __forceinline__ float mean_square(const float (&f)[8]) {
+    float sq = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sq = __builtin_fmaf(f[e], f[e], sq);
+    return group_sum<LPR>(sq) * (1.0f / (8 * LPR));
+}
+
+// Whether fp32 held the terms of m, a mean of squares and eps, with all their
+// digits.  It does not in rows below 2^-45 without an eps that hides them and in
+// rows of 2^60 and more; such rows are done again, divided by a power of two.
+__device__ __forceinline__ bool in_range(float m) { return m > 0x1p-90f && m < 0x1p120f; }
+
+// Divides a row x by 2^down, which brings the larger of its largest element and
+// sqrt(eps) near 1 (elements that become subnormal by it are 2^-126 of that).
+// With r = 1 / sqrt(mean square + eps / 4^down) of the divided row, r x is the
+// norm, and 1 / sqrt of the undivided row is r 2^-down.
+template <int LPR, typename T>
+__device__ __forceinline__ void divide(Chunk<T>& x, float eps, float& r, int& down) {
+    constexpr int NONE = -200;
+    float f[8], top = 0.0f;
+    x.get(f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]));
+#pragma unroll
+    for (int k = 1; k < LPR; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
+    const int of_eps = eps > 0.0f ? (__builtin_amdgcn_frexp_expf(eps) + 1) >> 1 : NONE;
+    const int of_top = top > FLT_MAX ? 128 : top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : NONE;
+    down = max(of_eps, of_top);
+    down = down == NONE ? 0 : down;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = ldexpf(f[e], -down);
+    x.set(f);
+    r = __builtin_amdgcn_rsqf(mean_square<LPR>(f) + ldexpf(eps, -2 * down));
 }
 
 // This lane's eight weights of tensor ts (1 without a norm).
@@ -244,21 +283,37 @@ __global__ __launch_bounds__(THREADS) void rope_fwd_kernel(RopeProblem p, int lo
         const bool norm = (ts ? p.w[1] : p.w[0]) != nullptr;
         T* to = ts ? y[1] : y[0];
         const long long stride = ts ? p.ys[1][1] : p.ys[0][1];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
+        bool redo[U];
+        const auto row = [&](int u, float r, auto again) {
             float f[8], o[8];
             c[u].get(f);
             turn.partners(c[u], f, o);
-            float r = 1.0f;
-            if (norm) {
-                float sq = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sq = __builtin_fmaf(f[e], f[e], sq);
-                r = inverse_root(group_sum<LPR>(sq) * (1.0f / D) + p.eps);
+            const bool in = h + u * w.step < limit;
+            if (!again) {
+                redo[u] = false;
+                if (norm) {
+                    const float m = mean_square<LPR>(f) + p.eps;
+                    r = __builtin_amdgcn_rsqf(m);
+                    redo[u] = in && !in_range(m);
+                }
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] = r * __builtin_fmaf(f[e], A[e], o[e] * Bp[e]);
-            if (h + u * w.step < limit) Chunk<T>::store(to + (h + u * w.step) * stride, f);
+            if (in && redo[u] == again) Chunk<T>::store(to + (h + u * w.step) * stride, f);
+        };
+        bool any = false;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            row(u, 1.0f, std::false_type{});
+            any |= redo[u];
+        }
+        if (!wave_any(any)) continue;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float r;
+            int down;
+            divide<LPR>(c[u], p.eps, r, down);
+            row(u, r, std::true_type{});
         }
     }
 }
@@ -330,21 +385,24 @@ __global__ __launch_bounds__(THREADS) void rope_bwd_kernel(RopeProblem p, int lo
             const bool norm = (ts ? p.w[1] : p.w[0]) != nullptr;
             T* to = ts ? y[1] : y[0];
             const long long stride = ts ? p.ys[1][1] : p.ys[0][1];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
+            bool redo[U];
+            const auto row = [&](int u, float r, int down, auto again) {
                 float gv[8], o[8];
                 cg[u].get(gv);
                 turn.partners(cg[u], gv, o);
+                const bool in = h0 + u * walk.step < limit;
+                if (!again) redo[u] = false;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) gv[e] = __builtin_fmaf(gv[e], turn.c[e], -o[e] * turn.s[e]);
-                if (norm) {   // rows behind the last one are zeros and add nothing
-                    float f[8], sq = 0.0f, dot = 0.0f;
+                if (norm) {   // only rows that this pass stores add to dw
+                    float f[8], dot = 0.0f;
                     cx[u].get(f);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sq = __builtin_fmaf(f[e], f[e], sq);
-                    sq = group_sum<LPR>(sq) * (1.0f / D) + p.eps;
-                    const bool in = h0 + u * walk.step < limit;
-                    const float r = in ? inverse_root(sq) : 0.0f;
+                    if (!again) {
+                        const float m = mean_square<LPR>(f) + p.eps;
+                        r = __builtin_amdgcn_rsqf(m);
+                        redo[u] = in && !in_range(m);
+                    }
+                    r = in && redo[u] == again ? r : 0.0f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         f[e] *= r;
@@ -357,8 +415,25 @@ __global__ __launch_bounds__(THREADS) void rope_bwd_kernel(RopeProblem p, int lo
                     dot = group_sum<LPR>(dot) * (1.0f / D);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) gv[e] = r * __builtin_fmaf(-f[e], dot, gv[e]);
+                    if (again)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) gv[e] = ldexpf(gv[e], -down);
                 }
-                if (h0 + u * walk.step < limit) Chunk<T>::store(to + (h0 + u * walk.step) * stride, gv);
+                if (in && redo[u] == again) Chunk<T>::store(to + (h0 + u * walk.step) * stride, gv);
+            };
+            bool any = false;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                row(u, 1.0f, 0, std::false_type{});
+                any |= redo[u];
+            }
+            if (!wave_any(any)) continue;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float r;
+                int down;
+                divide<LPR>(cx[u], p.eps, r, down);
+                row(u, r, down, std::true_type{});
             }
         }
     }
