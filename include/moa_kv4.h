@@ -62,7 +62,8 @@ size_t moa_kv4_page_bytes(int64_t page, int64_t d);
  * B, Hk, N, d, page, num_pages, max_pages
  *           B, Hk, N >= 0; supported: d in {64, 128}, page a multiple of 64 up to
  *           2^20, max_pages * page < 2^31, num_pages < 2^31, and
- *           B * Hk * (N + 6) < 2^30.
+ *           B * Hk * (N + 6) < 2^30; at d = 128 writing and reading take
+ *           B * Hk * (N + 6) up to 2^30 - 64.
  * Two rows of one call must not be the same token of the same page (which one
  * stays is then undefined).  One kernel.  Returns MOA_OK once the work is
  * enqueued, or when there are no rows.

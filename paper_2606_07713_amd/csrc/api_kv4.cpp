@@ -159,6 +159,7 @@ int moa_kv4_write(const void* K, const void* V, void* cache, const int32_t* seq_
     if (in_dtype != MOA_F32 && in_dtype != MOA_BF16) return MOA_ERR_INVALID_ARG;
     int st = check_dims(s);
     if (st) return st;
+    if (s.any() && kv4_row_blocks(B, Hk, N, d) > kMaxBlocks) return MOA_ERR_UNSUPPORTED;
     const size_t es = in_dtype == MOA_F32 ? 4 : 2;
     const Strides sk = strides_of(k_strides, B, Hk, N, d), sv = strides_of(v_strides, B, Hk, N, d);
     if ((st = check_tensor(K, sk, B, Hk, N, d, es, false)) || (st = check_tensor(V, sv, B, Hk, N, d, es, false))) return st;
@@ -183,6 +184,7 @@ int moa_kv4_read(const void* cache, void* K, void* V, const int32_t* seq_lens,
     if (out_dtype != MOA_F32 && out_dtype != MOA_BF16) return MOA_ERR_INVALID_ARG;
     int st = check_dims(s);
     if (st) return st;
+    if (s.any() && kv4_row_blocks(B, Hk, N, d) > kMaxBlocks) return MOA_ERR_UNSUPPORTED;
     const size_t es = out_dtype == MOA_F32 ? 4 : 2;
     const Strides sk = strides_of(k_strides, B, Hk, N, d), sv = strides_of(v_strides, B, Hk, N, d);
     if ((st = check_tensor(K, sk, B, Hk, N, d, es, true)) || (st = check_tensor(V, sv, B, Hk, N, d, es, true))) return st;

@@ -27,6 +27,15 @@ struct Kv4Rows {
     bool bf16;
 };
 
+// Quads (aligned fours) of tokens that a run of n touches at most: (n + 3) / 4
+// where it begins at one, one more elsewhere.
+inline int kv4_quads(long long n) { return (int)((n + 6) / 4); }
+// Workgroups of a write or read: d/8 of 256 threads for each sequence, head and quad.
+inline long long kv4_row_blocks(long long B, long long hk, long long n, long long d) {
+    const long long per = 256 / (d / 8);
+    return (B * hk * kv4_quads(n) + per - 1) / per;
+}
+
 hipError_t launch_kv4_write(const Kv4Rows& p, hipStream_t stream);
 hipError_t launch_kv4_read(const Kv4Rows& p, hipStream_t stream);
 

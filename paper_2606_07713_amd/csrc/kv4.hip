@@ -16,7 +16,7 @@ namespace {
 
 using namespace kv4;
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 256;   // as kv4_row_blocks counts them
 
 // The quad of one lane group: tokens 4 * quad + j of sequence b, head h.
 template <int D>
@@ -196,15 +196,10 @@ __global__ __launch_bounds__(THREADS) void kv4_read_kernel(Kv4Rows p, int quads)
     }
 }
 
-// Runs of n tokens touch at most (n + 3) / 4 quads when aligned, one more
-// otherwise.
-int quads_of(int n) { return (n + 6) / 4; }
-
 template <typename K>
 hipError_t go(K kernel, const Kv4Rows& p, hipStream_t stream) {
-    const int quads = quads_of(p.c.n), per = THREADS / (p.c.d / 8);
-    const long long groups = (long long)p.c.B * p.c.hk * quads;
-    return launch_kernel(kernel, dim3((unsigned)((groups + per - 1) / per)), dim3(THREADS), stream, p, quads);
+    const long long blocks = kv4_row_blocks(p.c.B, p.c.hk, p.c.n, p.c.d);
+    return launch_kernel(kernel, dim3((unsigned)blocks), dim3(THREADS), stream, p, kv4_quads(p.c.n));
 }
 
 }  // namespace
