@@ -83,7 +83,8 @@ int check_view(const View& v, const Common& c, int i, bool out) {
 size_t bytes(const View& v, const Common& c) { return extent_bytes(v.s, c.B, v.H, c.N, c.d, c.es()); }
 
 // Whether two views certainly share no element: their byte ranges do not meet,
-// or they take turns in one buffer, row by row or batch by batch.
+// or they take turns in one buffer: whole batches, or the heads of one token, be
+// they [B][N][heads] or [N][B][heads].
 bool disjoint(const View& a, const View& b, const Common& c) {
     if (!overlaps(a.p, bytes(a, c), b.p, bytes(b, c))) return true;
     const View &lo = a.p <= b.p ? a : b, &hi = a.p <= b.p ? b : a;
@@ -94,8 +95,11 @@ bool disjoint(const View& a, const View& b, const Common& c) {
         return (v.H - 1) * v.s.h + (rows ? (c.N - 1) * v.s.r : 0) + c.d;
     };
     if (lo.s.b == hi.s.b && inner(lo, true) <= delta && delta + inner(hi, true) <= lo.s.b) return true;
-    return lo.s.r == hi.s.r && inner(lo, false) <= delta && delta + inner(hi, false) <= lo.s.r &&
-           (c.B == 1 || (lo.s.b == hi.s.b && lo.s.b >= c.N * lo.s.r));
+    const int64_t end = delta + inner(hi, false);
+    const bool rows = lo.s.r == hi.s.r, batches = lo.s.b == hi.s.b;
+    if (inner(lo, false) > delta) return false;
+    if (rows && end <= lo.s.r && (c.B == 1 || (batches && lo.s.b >= c.N * lo.s.r))) return true;
+    return rows && batches && end <= lo.s.b && lo.s.r >= c.B * lo.s.b;
 }
 
 bool same(const View& a, const View& b) {
