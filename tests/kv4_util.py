@@ -70,14 +70,14 @@ def attention(q, K, V, seen, scale):
     return o, lse, mag, reach
 
 
-def attention_error(o, lse, ref, keys, d):
+def attention_error(o, lse, ref, keys, d, half=U):
     """The largest shares that O and LSE (fp64) take of their bounds, or a text that says what is
     NaN or infinite where `ref` is not.
 
     A weight goes into the product with V as two bf16 numbers, of which the second leaves half a
     step of 2^-8 of a rest of at most 2^-9: 2^-18 of sum P |V|.  Scores are off by (d + 4) units of
     2^-24 of scale * sum |q k|, which weights and sums have; fp32 sums of n terms add n / 64 + 64
-    units; the output's type adds half a step (given by its own rounding: fp32 here)."""
+    units; the output's type adds half a step, `half` (fp32's)."""
     want, wl, mag, reach = ref
     for name, got, right in (("O", o, want), ("LSE", lse, wl)):
         for what, test in (("NaN", torch.isnan), ("infinite", torch.isinf)):
@@ -85,7 +85,7 @@ def attention_error(o, lse, ref, keys, d):
                 return f"{name}: {what} at {int((test(got) != test(right)).sum())} places"
     ds, sums = (d + 4) * U * reach, (keys / 64 + 64) * U
     live = torch.isfinite(wl)
-    lim = (2.0 ** -18 + 2 * ds[:, None] + sums) * mag + U * want.abs() + 1e-30
+    lim = (2.0 ** -18 + 2 * ds[:, None] + sums) * mag + half * want.abs() + 1e-30
     err = torch.nan_to_num((o - want).abs() / lim).amax().item() if o.numel() else 0.0
     lerr = ((lse - wl).abs() / (ds + sums + 4 * U * wl.abs()))[live]
     return err, lerr.amax().item() if lerr.numel() else 0.0

@@ -1,7 +1,9 @@
-"""The attention over the four-bit cache, with fp32 outputs, against fp64 over the stored values:
-bounds of a few units of fp32 but for the weights' own 2^-18 (``kv4_util.attention_error``)."""
+"""The attention over the four-bit cache against fp64 over the stored values: bounds of a few units of
+fp32 but for the weights' own 2^-18 and the output's rounding (``kv4_util.attention_error``), and
+nothing that is NaN or infinite where the definition is not."""
 import pytest
 
+import test_kv4_gpu
 from kv4_util import attention, attention_error, stored
 from test_kv4_gpu import ATTNS, _cache_of, _ints, _pool
 
@@ -9,8 +11,9 @@ pytestmark = pytest.mark.gpu
 
 
 def check(q, cache, table, page, lens, new, causal, scale, o, lse):
-    """O and LSE (fp32) of every head against fp64."""
+    """O and LSE of every head against fp64."""
     import torch
+    half = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}[o.dtype]
     B, Hq, N, d = q.shape
     G = Hq // cache.shape[1]
     host, tab = cache.cpu(), None if table is None else table.cpu()
@@ -22,7 +25,7 @@ def check(q, cache, table, page, lens, new, causal, scale, o, lse):
         seen = torch.arange(n) + lens[b] - n + 1 if causal else torch.full((n,), lens[b])
         for h in range(Hq):
             ref = attention(q[b, h, :n].cpu().double(), K[h // G], V[h // G], seen, scale)
-            got = attention_error(o[b, h, :n].cpu().double(), lse[b, h, :n].cpu().double(), ref, lens[b], d)
+            got = attention_error(o[b, h, :n].cpu().double(), lse[b, h, :n].cpu().double(), ref, lens[b], d, half)
             assert not isinstance(got, str), (b, h, got)
             worst = [max(x, y) for x, y in zip(worst, got)]
     print(f"  O worst {worst[0]:.2f} of the bound, LSE {worst[1]:.2f}", flush=True)
@@ -88,3 +91,17 @@ def test_scores_that_leave_fp32_do_not_pass_for_rows_that_see_nothing():
         want = torch.tensor(float(-(-n // 3)), dtype=torch.float64).log()
         # equal weights of one: sums exact, a logarithm and its products
         assert (o == 1).all() and ((lse.cpu().double() - want).abs() <= 4 * 2.0 ** -24 * want).all()
+
+
+@pytest.mark.parametrize("test,args", [
+    ("test_no_page_table_and_strided_output", ()),
+    *[("test_nan_blocks_reach_only_the_rows_that_see_them", (n, causal, d))
+      for n, causal in ((1, True), (7, True), (40, True), (5, False)) for d in (64, 128)],
+    ("test_extreme_scores", ()),
+    ("test_norm_rope_write_attend_together", ()),
+    ("test_pool_beyond_four_gigabytes", ()),
+], ids=lambda v: v if isinstance(v, str) else "_".join(map(str, v)))
+def test_no_log_sum_is_nan_where_a_row_sees_a_key(monkeypatch, test, args):
+    # the calls of test_kv4_gpu whose own check takes a NaN log sum for 0
+    monkeypatch.setattr(test_kv4_gpu, "_check_attn", check)
+    getattr(test_kv4_gpu, test)(*args)
