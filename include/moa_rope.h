@@ -31,8 +31,8 @@ extern "C" {
  *           be K (same pointer and strides: in place).
  * wq, wk    norm weights [d] of storage type w_dtype, or NULL: that tensor is
  *           rotated without a norm.
- * positions device int64 [axes][B][N], any values, or NULL: token n is at
- *           position n on every axis.
+ * positions device int64 [axes][B][N], any values (beyond 2^53 rounded to fp64),
+ *           or NULL: token n is at position n on every axis.
  * inv_freq  device fp32 [rot/2] (NULL when rot == 0): radians per position of
  *           each pair.
  * B, Hq, Hk, N, d, rot
@@ -59,8 +59,8 @@ extern "C" {
  * its tensor has no elements.
  *
  * Computation: fp32 from exact inputs, one rounding at the end; angles in
- * fp64, reduced to one turn before sine and cosine are taken in fp32, so that
- * far positions lose nothing.  Rows whose squares leave fp32 (elements of 2^60
+ * fp64 with the products' errors carried along, reduced to one turn before sine
+ * and cosine are taken in fp32, so that far positions lose nothing.  Rows whose squares leave fp32 (elements of 2^60
  * and more, or below 2^-45 with an eps too small to hide them) are divided by a
  * power of two first and lose nothing either, with weights below 2^60; a row of
  * zeros without an eps is 0 / 0, NaN.  One kernel; deterministic.

@@ -93,6 +93,18 @@ struct Chunk<float> {
     }
 };
 
+// at * freq / (2 pi) less the nearest whole number.  Both products' rounding errors
+// and the constant's second half are carried along: of an angle of 2^40 rad
+// fp64's own rounding would be off by 2^-12.
+__device__ __forceinline__ double part_of_turn(double at, double freq) {
+    constexpr double HI = 0x1.45f306dc9c883p-3, LO = -0x1.6b01ec5417056p-57;   // 1 / (2 pi)
+    const double angle = at * freq, rest = fma(at, freq, -angle);
+    double part = fma(angle, HI, -rint(angle * HI));
+    part = fma(angle, LO, part);
+    part = fma(rest, HI, part);
+    return part - rint(part);
+}
+
 // cos and sin of the rot/2 pairs of the workgroup's tokens t0 .. t0 + tb - 1.
 __device__ __forceinline__ void take_angles(const RopeProblem& p, float2* cs, int t0, int tb, int tokens) {
     const int pairs = p.rot >> 1;
@@ -102,9 +114,8 @@ __device__ __forceinline__ void take_angles(const RopeProblem& p, float2* cs, in
         int axis = 0;
         for (int a = 1; a < p.axes; ++a) axis = pr >= p.first[a] ? a : axis;
         const long long at = p.pos ? p.pos[(long long)axis * tokens + tok] : tok % p.N;
-        const double turns = (double)at * (double)p.freq[pr] * 0.15915494309189533577;
         float s, c;
-        sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+        sincospif((float)(2.0 * part_of_turn((double)at, (double)p.freq[pr])), &s, &c);
         cs[i] = make_float2(c, s);
     }
 }
