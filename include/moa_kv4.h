@@ -9,9 +9,10 @@
  * 0..2 the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6.  17 bytes for 32 elements.
  * Written blocks have bytes 2..252, or 255: a block that held an infinity or a
  * NaN, all of whose elements read as NaN.  Of a block with largest magnitude a
- * the byte is the smallest for which a <= 7 * 2^(byte - 127) (no element then
- * is off by more than half the widest step), and every element takes the
- * nearest value, ties to the even code.
+ * the byte is the smallest of 2..252 for which a <= 7 * 2^(byte - 127) (no
+ * element then is off by more than half the widest step; beyond 7 * 2^125 it is
+ * 252, and such elements become 6 * 2^125), and every element takes the nearest
+ * value, ties to the even code.
  *
  * THE CACHE is a pool of pages, [num_pages][Hk][page_bytes] bytes in one
  * buffer.  A page holds `page` tokens (a multiple of 64) of one key/value head:
@@ -77,7 +78,9 @@ int moa_kv4_write(const void* K, const void* V, void* cache, const int32_t* seq_
  * moa_kv4_read -- the reverse: the values that the cache holds for the rows'
  * tokens (exact in bf16 and fp32), into K and V of storage type out_dtype.
  * Rows behind new_lens[b] and rows of skipped tokens are left as they are.  K
- * and V must not write an element twice or overlap each other or an input.
+ * and V must not write an element twice, and the bytes from the first to the
+ * last element of each must not meet the other's or an input's (views that
+ * interleave in one buffer do).
  * (new_lens = seq_lens, with N at least the longest, reads whole sequences:
  * token i to row i.)
  */
@@ -113,7 +116,8 @@ size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t N
  *           (batch, head, row) or NULL; non-negative multiples of 16 bytes.
  * cache     device pool, only read.
  * O         device output of storage type out_dtype (MOA_F32 or MOA_BF16), same
- *           logical shape and stride rules; no element written twice.
+ *           logical shape and stride rules; no element written twice, and its
+ *           bytes from the first to the last overlapping nothing else.
  * LSE       optional device output, fp32 [B][Hq][N] contiguous: the natural log
  *           of the softmax denominator.  NULL: not written.
  * A row without a visible token gets O = 0 and LSE = -inf.  Rows behind

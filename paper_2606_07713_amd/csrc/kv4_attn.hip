@@ -495,9 +495,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
 }
 
 // Exact join of a row's key splits; splits without a visible key have a reference
-// of -inf and sums of 0.  The pass is a chain of load latencies, so W waves share a row (1, or 4
-// for more than 4 splits), each takes U of its splits at a time, and all of
-// these loads are in flight together: up to 32 splits cost one latency.
+// of -inf and sums of 0.  With few rows the pass is a chain of load latencies, so
+// W = 4 waves share a row of more than 4 splits, each takes U of its splits at a
+// time, and all of these loads are in flight together: up to 32 splits cost one
+// latency.  From 2048 rows on there are enough waves with one for each (us by one
+// wave a row and by four, d = 128: 512 rows of 16 splits 4.8 and 3.9, 1024 of 16
+// 5.4 and 4.8, 1024 of 5 4.0 and 4.3; 2048 of 16 5.9 and 6.7, 8192 of 8 7.4 and
+// 17.3; 512 of 4 3.3 and 3.9).
 template <int D, int W>
 __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Attn p) {
     constexpr int PER = D / 64, U = W == 1 ? 4 : 8;
