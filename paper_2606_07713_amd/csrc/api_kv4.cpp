@@ -103,10 +103,10 @@ void put(long long (&to)[3], const Strides& s) { to[0] = s.b; to[1] = s.h; to[2]
 // partial states.  `wave` workgroups run at a time: one per compute unit where
 // up to 16 rows of d = 128 leave it to the memory, two where a tile is half as
 // large or its work twice (measured, splits:us, 32 heads on 8: one query, 4097
-// keys, d = 128 1:22.9 8:10.9 17:9.1 64:11.4; 16384 1:72 16:12.6 32:11.2 64:14.1;
-// 48 queries of 8192 1:75.9 2:72.5 4:74.6, 64 of them 1:91.5 2:93.1; 200 queries
-// of one sequence on 20011 keys 1:113 2:96 4:97 5:84 8:94, 512 on 8192 1:75.5
-// 2:86).
+// keys, d = 128 1:26.1 8:11.3 17:9.1 64:11.4; 16384 1:85 16:13.3 32:11.1 64:14.3;
+// 48 queries of 8192 1:79.0 2:75.9 4:78.1, 64 of them 1:94.0 2:96.3; 200 queries
+// of one sequence on 20011 keys 1:143 2:124 4:123 5:106 8:115, 512 on 8192 1:98
+// 2:108).
 int pick_splits(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d, int64_t max_len, int requested) {
     if (requested > 0) return requested;
     const int64_t rows = N * (Hq / Hk), per = kv4_rows_per_block((int)rows);

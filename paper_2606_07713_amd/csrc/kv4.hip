@@ -1,12 +1,13 @@
 // Quantising keys and values into the pages of the four-bit cache, and reading
 // them back (moa_kv4.h has the format).
 //
-// Both move 2.53 bytes per element and do little else, so device memory bounds
-// them (8192 tokens, 16 heads, d = 128, bf16, 85 MB: written in 17.5 us, 4.9
-// TB/s, read back in 15).  A group of d/8 lanes takes the four tokens of an aligned quad: a lane
-// has the same eight elements of all four, which makes its value codes one
-// 16-byte piece of the page ([d/4][4][2] of the quad) and its key codes 4 bytes
-// of four rows.  A quad of which only some tokens belong to the call (a single
+// Both move 2.53 bytes per element (fp32: 4.53) and do little else, so device
+// memory bounds them (8192 tokens, 16 heads, d = 128, bf16, 85 MB: written in 17.6
+// us, 4.8 TB/s, read back in 15, 5.6, where copies of that mix reach 6.5; fp32, 152
+// MB: 36 and 75).  A group of d/8 lanes takes the four tokens of an aligned quad: a
+// lane has the same eight elements of all four, which makes its value codes one
+// 16-byte piece of the page ([d/4][4][2] of the quad) and its key codes 4 bytes of
+// four rows.  A quad of which only some tokens belong to the call (a single
 // decoded token) writes 2-byte pieces of the quad, never a byte of another
 // token: no read-modify-write, so different calls may fill one quad.
 #include "kv4_common.h"

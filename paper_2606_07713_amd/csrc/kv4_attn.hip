@@ -22,15 +22,17 @@
 // row sees; later tiles are weighed against it without looking for their own
 // maximum, and only a sum beyond 2^20 (scores 16 and more log2 units above the
 // reference; fp32 and bf16 hold such weights as well as small ones) raises it,
-// for the whole wave at once, and so does a tile with values of 2^65 and more.  fp32 sums of the unrounded weights per lane,
-// joined over the lanes once at the end.
+// for the whole wave at once, and so does a tile with values of 2^65 and more.
+// fp32 sums of the unrounded weights per lane, joined over the lanes once at the
+// end.
 //
 // What bounds it: with few rows the memory (64 sequences of 8192 keys, 8 stored
-// heads of d = 128 for 32: 571 MB in 88 us, 6.5 TB/s; reading alone reaches 6.9),
-// with many the sum of vector and matrix instructions, which hardly overlap (a
-// tile of 16 rows takes a SIMD 1860 cycles from the caches, 325 vector and 32
-// matrix instructions; of 32 rows 2950): 32 heads on 8, 8192 causal queries, d =
-// 128, 588 us, 0.94 PFLOP/s.  Short calls are chains of latencies.
+// heads of d = 128 for 32: 571 MB in 91 us, 6.2 TB/s; reading alone reaches 6.9),
+// with many the sum of vector and matrix instructions, which hardly overlap as
+// they are ordered here (a tile of 16 rows takes a SIMD 2600 cycles from the
+// caches, one of 32 rows 3800; 2100 and 2900 with one bf16 number per weight): 32
+// heads on 8, 8192 causal queries, d = 128, 748 us, 0.74 PFLOP/s.  Short calls are
+// chains of latencies.
 #include <cfloat>
 #include <limits>
 
@@ -192,8 +194,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
     // Row tiles last, the last ones first: those of one head and split, which read
     // the same keys, mostly go to one XCD (successive workgroups go to the eight
     // in turn), and under the causal mask the longest begin first (16 heads of 2
-    // sequences of 4096, d = 128: 207 us with row tiles next to each other, 171
-    // so, 175 first to last).
+    // sequences of 4096, d = 128: 266 us with row tiles next to each other, 210
+    // so, 233 first to last).
     int blk = blockIdx.x;
     const int groups = kc.B * kc.hk * p.splits, rt = row_tiles - 1 - blk / groups;
     blk %= groups;

@@ -2,9 +2,9 @@
 // the gradients (moa_rope.h has the formulas).
 //
 // Each row of d elements is read once and written once and takes about ten
-// operations an element, so device memory bounds it (32 heads of 8192 tokens,
-// bf16, d = 128: 134 MB in 25.5 us, 5.2 TB/s, and 201 MB in 41.6 us, 4.8 TB/s,
-// for the gradients; a large copy moves 4.9 TB/s).  A group of d/8 lanes
+// operations an element: mostly memory's (32 heads of 8192 tokens, bf16, d = 128:
+// 134 MB in 26 us, 5.1 TB/s, and 201 MB in 41 us, 4.9 TB/s, for the gradients;
+// copies of as much read and written reach 7.0 and 5.9).  A group of d/8 lanes
 // holds a row, eight elements a lane; the sum of squares is a reduction inside
 // the group.  The rotation is folded with the weight: of a rotated element e
 // with partner e' (the other element of its pair)
@@ -496,8 +496,8 @@ __global__ __launch_bounds__(1024) void rope_dw_kernel(const float* __restrict__
 // Tokens a workgroup takes at a time (a power of two, at most one for each of
 // its groups): as many as leave a workgroup for every compute unit.  What a
 // group does once per token then serves as many heads as there are: 16 heads of
-// 4000 tokens, fp32, d = 64, forward and gradients: 1024 workgroups at least 20.3
-// and 20.7 us, 512 14.6 and 13.4, 256 11.4 and 12.3.
+// 4000 tokens, fp32, d = 64, forward and gradients: 1024 workgroups at least 10.9
+// and 16.6 us, 512 9.3 and 15.2, 256 9.2 and 10.6.
 int pick_log_tb(int tokens, int groups) {
     int l = 0;
     while ((2 << l) <= groups && (tokens >> (l + 1)) >= 256) ++l;
