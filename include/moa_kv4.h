@@ -134,12 +134,14 @@ size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t N
  *
  * Computation: bf16 matrix products with fp32 accumulation of the exact stored
  * values (bf16 holds them); softmax statistics in fp32, from the fp32 weights; a
- * weight multiplies V as the sum of two bf16 numbers, 17 bits.  A score whose
- * product with scale * log2(e) is not below fp32's largest number makes its row
- * NaN, one that is below fp32's lowest weighs nothing, and a row that sees only
- * such is NaN (LSE: infinite, of that sign).  Stored NaN
- * blocks and unset tokens do not touch rows that do not see them.  One kernel,
- * or two when the keys are split; no atomics, deterministic.
+ * weight multiplies V as the sum of two bf16 numbers, 17 bits.  The sums of up to
+ * n visible keys are taken with weights of at most 1 where values are large, so
+ * that values below 2^128 / n cannot overflow.  A score whose product with
+ * scale * log2(e) leaves fp32 upwards makes its row NaN, one that leaves it
+ * downwards weighs nothing, and a row that sees only such is NaN (LSE: infinite,
+ * of that sign).  Stored NaN blocks and unset tokens do not touch rows that do
+ * not see them.  One kernel, or two when the keys are split; no atomics,
+ * deterministic.
  */
 int moa_kv4_attn_fwd(const void* Q, const void* cache, void* O, float* LSE, const int32_t* seq_lens,
                      const int32_t* new_lens, const int32_t* page_table, int64_t B, int64_t Hq,
