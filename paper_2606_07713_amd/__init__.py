@@ -11,9 +11,11 @@ wrapper for torch tensors (torch supplies device memory and the stream).
 
 What stands around the attention of a model has modules of its own, with their
 names here as well: ``rope`` (``include/moa_rope.h``: norms of queries and keys
-for each head with the rotation by position, and the gradients) and ``kv4``
+for each head with the rotation by position, and the gradients), ``kv4``
 (``include/moa_kv4.h``: a key/value cache held in four bits and the attention
-over it).
+over it), ``window`` (``include/moa_window.h``: attention in a sliding window, with
+shared heads) and ``paged`` (``include/moa_paged.h``: a paged cache in bf16 and the
+attention over it).
 
 There is no fallback: if the HIP library has not been built, importing this
 package raises ``ImportError``.
@@ -37,6 +39,9 @@ __all__ = [
     "moa_kv4_page_bytes", "moa_kv4_write", "moa_kv4_read", "moa_kv4_attn_fwd",
     "moa_kv4_attn_num_splits", "moa_kv4_attn_workspace_bytes",
     "kv4_cache", "kv4_write", "kv4_read", "kv4_attn_fwd",
+    "moa_win_attn_fwd", "moa_win_attn_num_splits", "moa_win_attn_workspace_bytes", "win_attn_fwd",
+    "moa_paged_attn_fwd", "moa_paged_attn_num_splits", "moa_paged_attn_workspace_bytes",
+    "paged_cache", "paged_attn_fwd",
 ]
 
 MOA_OK, MOA_ERR_INVALID_ARG, MOA_ERR_UNSUPPORTED, MOA_ERR_WORKSPACE, MOA_ERR_HIP = 0, 1, 2, 3, 4
@@ -383,3 +388,7 @@ from .rope import (  # noqa: E402
 from .kv4 import (  # noqa: E402
     kv4_attn_fwd, kv4_cache, kv4_read, kv4_write, moa_kv4_attn_fwd, moa_kv4_attn_num_splits,
     moa_kv4_attn_workspace_bytes, moa_kv4_page_bytes, moa_kv4_read, moa_kv4_write)
+from .window import (  # noqa: E402
+    moa_win_attn_fwd, moa_win_attn_num_splits, moa_win_attn_workspace_bytes, win_attn_fwd)
+from .paged import (  # noqa: E402
+    moa_paged_attn_fwd, moa_paged_attn_num_splits, moa_paged_attn_workspace_bytes, paged_attn_fwd, paged_cache)

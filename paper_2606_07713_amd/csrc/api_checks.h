@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/moa_attn.h"
+
 namespace moa {
 
 // MOA_OK, or MOA_ERR_HIP with the error's name kept for this thread.
@@ -49,5 +51,35 @@ inline bool injective(const Strides& s, int64_t B, int64_t H, int64_t N, int64_t
     }
     return true;
 }
+
+// A [B][H][N][d] tensor of elements of es bytes: pointer, strides, extent, and of an
+// output that no element is written twice.
+inline int check_tensor(const void* p, const Strides& s, int64_t B, int64_t H, int64_t N, int64_t d, size_t es, bool out) {
+    if (B == 0 || H == 0 || N == 0) return MOA_OK;
+    if (!p || !aligned16(p)) return MOA_ERR_INVALID_ARG;
+    for (int64_t x : {s.b, s.h, s.r}) {
+        if (x < 0) return MOA_ERR_INVALID_ARG;
+        if (x > (int64_t(1) << 40) || (x * (int64_t)es) % 16) return MOA_ERR_UNSUPPORTED;
+    }
+    const __int128 n = (__int128)(B - 1) * s.b + (__int128)(H - 1) * s.h + (__int128)(N - 1) * s.r + d;
+    if (n > ((__int128)1 << 46)) return MOA_ERR_UNSUPPORTED;
+    if (out && !injective(s, B, H, N, d)) return MOA_ERR_INVALID_ARG;
+    return MOA_OK;
+}
+
+// A dimension of size 1 has no stride to keep to.
+inline Strides strides_of(const int64_t* s, int64_t B, int64_t H, int64_t N, int64_t d) {
+    return s ? Strides{B > 1 ? s[0] : 0, H > 1 ? s[1] : 0, N > 1 ? s[2] : 0} : contiguous(H, N, d);
+}
+
+// A range of bytes.
+struct Buf {
+    const void* p;
+    size_t n;
+};
+
+inline bool meet(const Buf& x, const Buf& y) { return overlaps(x.p, x.n, y.p, y.n); }
+
+inline void put(long long (&to)[3], const Strides& s) { to[0] = s.b; to[1] = s.h; to[2] = s.r; }
 
 }  // namespace moa

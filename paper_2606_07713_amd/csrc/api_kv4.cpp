@@ -47,29 +47,6 @@ int check_dims(const Dims& s) {
     return MOA_OK;
 }
 
-int check_tensor(const void* p, const Strides& s, int64_t B, int64_t H, int64_t N, int64_t d, size_t es, bool out) {
-    if (B == 0 || H == 0 || N == 0) return MOA_OK;
-    if (!p || !aligned16(p)) return MOA_ERR_INVALID_ARG;
-    for (int64_t x : {s.b, s.h, s.r}) {
-        if (x < 0) return MOA_ERR_INVALID_ARG;
-        if (x > (int64_t(1) << 40) || (x * (int64_t)es) % 16) return MOA_ERR_UNSUPPORTED;
-    }
-    const __int128 n = (__int128)(B - 1) * s.b + (__int128)(H - 1) * s.h + (__int128)(N - 1) * s.r + d;
-    if (n > ((__int128)1 << 46)) return MOA_ERR_UNSUPPORTED;
-    if (out && !injective(s, B, H, N, d)) return MOA_ERR_INVALID_ARG;
-    return MOA_OK;
-}
-
-// A dimension of size 1 has no stride to keep to.
-Strides strides_of(const int64_t* s, int64_t B, int64_t H, int64_t N, int64_t d) {
-    return s ? Strides{B > 1 ? s[0] : 0, H > 1 ? s[1] : 0, N > 1 ? s[2] : 0} : contiguous(H, N, d);
-}
-
-struct Buf {
-    const void* p;
-    size_t n;
-};
-
 // The arrays that tell where tokens are.
 struct Lists {
     Buf b[3];
@@ -83,8 +60,6 @@ struct Lists {
     }
 };
 
-bool meet(const Buf& x, const Buf& y) { return overlaps(x.p, x.n, y.p, y.n); }
-
 Kv4Cache cache_of(const Dims& s) {
     Kv4Cache c;
     c.base = static_cast<unsigned char*>(const_cast<void*>(s.cache));
@@ -94,8 +69,6 @@ Kv4Cache cache_of(const Dims& s) {
     c.page = (int)s.page; c.num_pages = (int)s.num_pages; c.max_pages = (int)s.max_pages;
     return c;
 }
-
-void put(long long (&to)[3], const Strides& s) { to[0] = s.b; to[1] = s.h; to[2] = s.r; }
 
 // Key splits of the attention.  A workgroup's four waves take its 64-key tiles
 // in steps of four; starting and ending it costs about two steps, and the

@@ -150,8 +150,6 @@ void fill(RopeProblem& p, const Common& c, const void* const (&w)[2]) {
     p.w_bf16 = c.w_dtype == MOA_BF16;
 }
 
-void put(long long (&to)[3], const Strides& s) { to[0] = s.b; to[1] = s.h; to[2] = s.r; }
-
 }  // namespace
 
 extern "C" {

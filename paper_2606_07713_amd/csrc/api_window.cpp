@@ -1,0 +1,285 @@
+// C-ABI front end of the attention with a window, on whole tensors (moa_window.h)
+// and over the paged cache (moa_paged.h): argument validation, split choice and
+// dispatch.  Host code; allocates nothing, never synchronises.
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/moa_paged.h"
+#include "../../include/moa_window.h"
+#include "api_checks.h"
+#include "packed.h"
+#include "win.h"
+
+namespace {
+
+using namespace moa;
+
+constexpr int64_t kMost = int64_t(1) << 30;     // positions and sizes: sums of two stay in 32 bits
+constexpr int64_t kMaxRows = int64_t(1) << 26;  // B * Hq * N: four rows a workgroup when splits are joined
+constexpr int64_t kMaxRowStride = int64_t(1) << 25;   // 16 rows' bytes stay in 32 bits
+constexpr int kMaxSplits = 256;
+constexpr float kMaxScale = 0x1p127f;           // times log2(e) is still finite
+// Workgroups of 256 threads in one launch: its threads are counted in 32 bits.
+constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;
+
+// The sizes of an attention call; Nk: keys of a sequence, at most.
+struct Sizes {
+    int64_t B, Hq, Hk, N, Nk, d, left, right, sinks;
+    int64_t rows() const { return N * (Hq / Hk); }
+    int64_t per() const { return win_rows_per_block(rows()); }
+    int64_t tiles() const { return (rows() + per() - 1) / per(); }
+    int64_t groups() const { return B * Hk * tiles(); }
+    bool any() const { return B > 0 && Hq > 0 && N > 0; }
+};
+
+// MOA_OK, or what is wrong.
+int check_sizes(const Sizes& s, int num_splits) {
+    if (s.B < 0 || s.Hq < 0 || s.Hk < 1 || s.N < 0 || s.Nk < 0 || s.d < 1 || s.Hq % s.Hk || s.sinks < 0) return MOA_ERR_INVALID_ARG;
+    if (num_splits < 0 || num_splits > kMaxSplits) return MOA_ERR_INVALID_ARG;
+    if (s.d != 64 && s.d != 128) return MOA_ERR_UNSUPPORTED;
+    if (s.B >= kMaxRows || s.Hq >= kMaxRows || s.Hk >= kMaxRows || s.N > kMost || s.Nk > kMost) return MOA_ERR_UNSUPPORTED;
+    if (s.B * std::max(s.Hq, s.Hk) >= kMaxRows) return MOA_ERR_UNSUPPORTED;
+    if (s.B * s.Hq > 0 && s.N >= (kMaxRows + s.B * s.Hq - 1) / (s.B * s.Hq)) return MOA_ERR_UNSUPPORTED;
+    if (s.any() && s.groups() > kMaxBlocks / std::max(num_splits, 1)) return MOA_ERR_UNSUPPORTED;
+    return MOA_OK;
+}
+
+// Keys that one row tile walks over, at most.
+int64_t span(const Sizes& s) {
+    if (s.left < 0) return s.Nk;
+    const int64_t positions = std::min(s.N, s.per() / std::max<int64_t>(1, s.Hq / s.Hk) + 1);
+    const int64_t ahead = s.right < 0 ? s.Nk : s.right;
+    return std::min(s.Nk, s.left + ahead + positions + std::min(s.sinks, s.Nk));
+}
+
+// Key splits.  A workgroup of few rows takes steps of 128 keys (four waves, 32
+// each), one of many rows tiles of 64; starting and ending it costs about two of
+// these, and the second pass about three, one more for every 16 splits and for
+// every 6 MB of partial states.  512 workgroups run at a time.
+int pick_splits(const Sizes& s, int requested) {
+    if (!s.any()) return 1;
+    if (requested > 0) return requested;
+    const bool few = s.per() < 128;
+    const int64_t blocks = s.groups(), keys = few ? 128 : 64, all = (span(s) + keys - 1) / keys, wave = 512;
+    const double states = (double)(s.B * s.Hq * s.N) * (double)s.d * sizeof(float) / 6e6;
+    int best = 1;
+    double least = 0;
+    for (int64_t k = 1; k <= kMaxSplits && k <= std::max<int64_t>(all, 1) && (k == 1 || k * blocks <= 4 * wave); ++k) {
+        const int64_t rounds = (k * blocks + wave - 1) / wave, steps = (all + k - 1) / k;
+        const double cost = (double)(rounds * (steps + 2)) + (k > 1 ? 3 + (double)k / 16 + (double)k * states : 0);
+        if (k == 1 || cost < least) {
+            best = (int)k;
+            least = cost;
+        }
+    }
+    return best;
+}
+
+// Partial states of a call with these splits (none with one).
+size_t states_bytes(const Sizes& s, int splits) {
+    if (splits <= 1) return 0;
+    return align256((size_t)(s.B * s.Hq * s.N) * (size_t)splits * (size_t)(s.d + 2) * sizeof(float));
+}
+
+int limit(int64_t x) { return x < 0 || x >= kMost ? kNoLimit : (int)x; }
+
+Window window_of(const Sizes& s) { return {limit(s.left), limit(s.right), (int)std::min(s.sinks, kMost)}; }
+
+// What both entry points check and do once their keys are known.  `keys`: the
+// ranges that the call reads besides Q.
+struct Call {
+    const void* Q;
+    void* O;
+    float* LSE;
+    Strides sq, so;
+    float scale;
+    int out_dtype;
+    void* ws;
+    size_t ws_bytes;
+    int splits;
+    void* stream;
+};
+
+int check_call(const Call& c, const Sizes& s) {
+    const size_t es = c.out_dtype == MOA_F32 ? 4 : 2;
+    int st;
+    if ((st = check_tensor(c.Q, c.sq, s.B, s.Hq, s.N, s.d, 2, false)) || (st = check_tensor(c.O, c.so, s.B, s.Hq, s.N, s.d, es, true))) return st;
+    if (!aligned16(c.ws) || (reinterpret_cast<uintptr_t>(c.LSE) & 3)) return MOA_ERR_INVALID_ARG;
+    if (std::fabs(c.scale) > kMaxScale) return MOA_ERR_UNSUPPORTED;
+    return MOA_OK;
+}
+
+int run(const Call& c, const Sizes& s, const KeySource& src, const Buf* keys, int n_keys) {
+    const size_t es = c.out_dtype == MOA_F32 ? 4 : 2, need = states_bytes(s, c.splits);
+    if (need && (!c.ws || c.ws_bytes < need)) return MOA_ERR_WORKSPACE;
+    const Buf q{c.Q, extent_bytes(c.sq, s.B, s.Hq, s.N, s.d, 2)};
+    const Buf outs[] = {{c.O, extent_bytes(c.so, s.B, s.Hq, s.N, s.d, es)},
+                        {c.LSE, c.LSE ? (size_t)(s.B * s.Hq * s.N) * 4 : 0}, {c.ws, need}};
+    for (int i = 0; i < 3; ++i) {
+        if (meet(outs[i], q)) return MOA_ERR_INVALID_ARG;
+        for (int k = 0; k < n_keys; ++k)
+            if (meet(outs[i], keys[k])) return MOA_ERR_INVALID_ARG;
+        for (int k = i + 1; k < 3; ++k)
+            if (meet(outs[i], outs[k])) return MOA_ERR_INVALID_ARG;
+    }
+    WinAttn p{};
+    p.s = src;
+    p.w = window_of(s);
+    p.q = c.Q; p.o = c.O; p.lse = c.LSE;
+    put(p.qs, c.sq); put(p.os, c.so);
+    p.B = (int)s.B; p.hq = (int)s.Hq; p.hk = (int)s.Hk; p.n = (int)s.N; p.d = (int)s.d;
+    p.scale = c.scale;
+    p.out_bf16 = c.out_dtype == MOA_BF16;
+    p.splits = c.splits;
+    p.ws = static_cast<float*>(c.ws);
+    return hip_status(launch_win_attn(p, static_cast<hipStream_t>(c.stream)));
+}
+
+// The two pools of a paged cache.
+struct Pools {
+    int64_t page, num_pages, max_pages;
+    const int32_t *seq_lens, *new_lens, *table;
+};
+
+int64_t capacity(const Pools& c) { return c.max_pages * c.page; }
+
+int log2_of(int64_t page) {
+    int k = 0;
+    while ((int64_t(1) << k) < page) ++k;
+    return k;
+}
+
+int check_pools(const Pools& c, int64_t B, int64_t N, bool any) {
+    if (c.page < 1 || c.num_pages < 0 || c.max_pages < 0) return MOA_ERR_INVALID_ARG;
+    if (c.page < 16 || c.page > (int64_t(1) << 20) || (c.page & (c.page - 1))) return MOA_ERR_UNSUPPORTED;
+    if (c.num_pages >= kMost || c.max_pages > kMost / c.page || N > kMost) return MOA_ERR_UNSUPPORTED;
+    if (!c.table && any && (c.max_pages != 1 || c.num_pages < B)) return MOA_ERR_INVALID_ARG;
+    if (any && !c.seq_lens) return MOA_ERR_INVALID_ARG;
+    for (const void* p : {c.seq_lens, c.new_lens, c.table})
+        if (reinterpret_cast<uintptr_t>(p) & 3) return MOA_ERR_INVALID_ARG;
+    return MOA_OK;
+}
+
+// A pool of keys or values.
+int check_pool(const void* p, const Strides& s, const Pools& c, int64_t Hk, int64_t d, bool out) {
+    if (s.r > kMaxRowStride) return MOA_ERR_UNSUPPORTED;
+    return check_tensor(p, s, c.num_pages, Hk, c.page, d, 2, out);
+}
+
+}  // namespace
+
+extern "C" {
+
+int moa_win_attn_num_splits(int64_t B, int64_t Hq, int64_t Hk, int64_t Nq, int64_t Nk, int64_t d,
+                            int64_t left, int64_t right, int64_t sinks, int num_splits) {
+    const Sizes s{B, Hq, Hk, Nq, Nk, d, left, right, sinks};
+    return check_sizes(s, num_splits) ? 1 : pick_splits(s, num_splits);
+}
+
+size_t moa_win_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t Nq, int64_t Nk,
+                                    int64_t d, int64_t left, int64_t right, int64_t sinks,
+                                    int num_splits) {
+    const Sizes s{B, Hq, Hk, Nq, Nk, d, left, right, sinks};
+    return check_sizes(s, num_splits) ? 0 : states_bytes(s, pick_splits(s, num_splits));
+}
+
+int moa_win_attn_fwd(const void* Q, const void* K, const void* V, void* O, float* LSE, int64_t B,
+                     int64_t Hq, int64_t Hk, int64_t Nq, int64_t Nk, int64_t d,
+                     const int64_t* q_strides, const int64_t* k_strides, const int64_t* v_strides,
+                     const int64_t* o_strides, int64_t left, int64_t right, int64_t sinks,
+                     float scale, int out_dtype, void* workspace, size_t workspace_bytes,
+                     int num_splits, void* stream) {
+    const Sizes s{B, Hq, Hk, Nq, Nk, d, left, right, sinks};
+    if (out_dtype != MOA_F32 && out_dtype != MOA_BF16) return MOA_ERR_INVALID_ARG;
+    if (!std::isfinite(scale)) return MOA_ERR_INVALID_ARG;
+    int st = check_sizes(s, num_splits);
+    if (st) return st;
+    const Strides sk = strides_of(k_strides, B, Hk, Nk, d), sv = strides_of(v_strides, B, Hk, Nk, d);
+    if ((st = check_tensor(K, sk, B, Hk, Nk, d, 2, false)) || (st = check_tensor(V, sv, B, Hk, Nk, d, 2, false))) return st;
+    if (sk.r > kMaxRowStride || sv.r > kMaxRowStride) return MOA_ERR_UNSUPPORTED;
+    const Call c{Q, O, LSE, strides_of(q_strides, B, Hq, Nq, d), strides_of(o_strides, B, Hq, Nq, d), scale, out_dtype,
+                 workspace, workspace_bytes, pick_splits(s, num_splits), stream};
+    if ((st = check_call(c, s))) return st;
+    if (!s.any()) return MOA_OK;
+    KeySource src{};
+    src.k = K; src.v = V;
+    put(src.ks, sk); put(src.vs, sv);
+    src.len = (int)Nk;
+    src.shift = 31;
+    src.num_pages = (int)B;
+    src.max_pages = 1;
+    const Buf keys[] = {{K, extent_bytes(sk, B, Hk, Nk, d, 2)}, {V, extent_bytes(sv, B, Hk, Nk, d, 2)}};
+    return run(c, s, src, keys, 2);
+}
+
+int moa_paged_attn_num_splits(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d, int64_t page,
+                              int64_t max_pages, int64_t max_len, int64_t left, int64_t right,
+                              int64_t sinks, int num_splits) {
+    const Pools c{page, 0, max_pages, nullptr, nullptr, nullptr};
+    if (max_len < 0 || check_pools(c, B, N, false)) return 1;
+    const int64_t cap = capacity(c);
+    const Sizes s{B, Hq, Hk, N, max_len > 0 && max_len < cap ? max_len : cap, d, left, right, sinks};
+    return check_sizes(s, num_splits) ? 1 : pick_splits(s, num_splits);
+}
+
+size_t moa_paged_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d,
+                                      int64_t page, int64_t max_pages, int64_t max_len,
+                                      int64_t left, int64_t right, int64_t sinks, int num_splits) {
+    const int splits = moa_paged_attn_num_splits(B, Hq, Hk, N, d, page, max_pages, max_len, left, right, sinks, num_splits);
+    return splits <= 1 ? 0 : states_bytes({B, Hq, Hk, N, 0, d, 0, 0, 0}, splits);
+}
+
+int moa_paged_attn_fwd(const void* Q, const void* k_pool, const void* v_pool, void* O, float* LSE,
+                       const int32_t* seq_lens, const int32_t* new_lens, const int32_t* page_table,
+                       int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d, int64_t page,
+                       int64_t num_pages, int64_t max_pages, int64_t max_len,
+                       const int64_t* q_strides, const int64_t* k_strides,
+                       const int64_t* v_strides, const int64_t* o_strides, int64_t left,
+                       int64_t right, int64_t sinks, float scale, int out_dtype, void* workspace,
+                       size_t workspace_bytes, int num_splits, void* stream) {
+    const Pools pools{page, num_pages, max_pages, seq_lens, new_lens, page_table};
+    if (out_dtype != MOA_F32 && out_dtype != MOA_BF16) return MOA_ERR_INVALID_ARG;
+    if (!std::isfinite(scale) || max_len < 0) return MOA_ERR_INVALID_ARG;
+    int st = check_sizes({B, Hq, Hk, N, 0, d, left, right, sinks}, num_splits);
+    if (st) return st;
+    const bool any = B > 0 && Hq > 0 && N > 0;
+    if ((st = check_pools(pools, B, N, any))) return st;
+    const int64_t cap = capacity(pools);
+    const Sizes s{B, Hq, Hk, N, max_len > 0 && max_len < cap ? max_len : cap, d, left, right, sinks};
+    const Strides sk = strides_of(k_strides, num_pages, Hk, page, d), sv = strides_of(v_strides, num_pages, Hk, page, d);
+    if ((st = check_pool(k_pool, sk, pools, Hk, d, false)) || (st = check_pool(v_pool, sv, pools, Hk, d, false))) return st;
+    const Call c{Q, O, LSE, strides_of(q_strides, B, Hq, N, d), strides_of(o_strides, B, Hq, N, d), scale, out_dtype,
+                 workspace, workspace_bytes, pick_splits(s, num_splits), stream};
+    if ((st = check_call(c, s))) return st;
+    if (!any) return MOA_OK;
+    KeySource src{};
+    src.k = k_pool; src.v = v_pool;
+    put(src.ks, sk); put(src.vs, sv);
+    src.seq_lens = seq_lens; src.new_lens = new_lens; src.table = page_table;
+    src.shift = log2_of(page);
+    src.num_pages = (int)num_pages;
+    src.max_pages = (int)max_pages;
+    const Buf keys[] = {{k_pool, extent_bytes(sk, num_pages, Hk, page, d, 2)}, {v_pool, extent_bytes(sv, num_pages, Hk, page, d, 2)},
+                        {seq_lens, (size_t)B * 4}, {new_lens, new_lens ? (size_t)B * 4 : 0},
+                        {page_table, page_table ? (size_t)B * (size_t)max_pages * 4 : 0}};
+    return run(c, s, src, keys, 5);
+}
+
+// Words: the arguments in their order, but 4 for each tensor's strides (the last
+// not read).
+int moa_packed_win_attn_fwd(const int64_t* a) {
+    using packed::Ptr;
+    return moa_win_attn_fwd(Ptr{a[0]}, Ptr{a[1]}, Ptr{a[2]}, Ptr{a[3]}, Ptr{a[4]}, a[5], a[6], a[7], a[8], a[9], a[10],
+                            a + 11, a + 15, a + 19, a + 23, a[27], a[28], a[29], packed::real(a[30]), (int)a[31], Ptr{a[32]},
+                            (size_t)a[33], (int)a[34], Ptr{a[35]});
+}
+
+int moa_packed_paged_attn_fwd(const int64_t* a) {
+    using packed::Ptr;
+    return moa_paged_attn_fwd(Ptr{a[0]}, Ptr{a[1]}, Ptr{a[2]}, Ptr{a[3]}, Ptr{a[4]}, Ptr{a[5]}, Ptr{a[6]}, Ptr{a[7]},
+                              a[8], a[9], a[10], a[11], a[12], a[13], a[14], a[15], a[16], a + 17, a + 21, a + 25, a + 29,
+                              a[33], a[34], a[35], packed::real(a[36]), (int)a[37], Ptr{a[38]}, (size_t)a[39], (int)a[40],
+                              Ptr{a[41]});
+}
+
+}  // extern "C"

@@ -38,6 +38,7 @@
 
 #include "kv4_common.h"
 #include "prefill_bf16_common.h"
+#include "split_join.h"
 
 namespace moa {
 namespace {
@@ -496,88 +497,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void kv4_attn_kernel(Kv4Attn p, floa
     }
 }
 
-// Exact join of a row's key splits; splits without a visible key have a reference
-// of -inf and sums of 0.  With few rows the pass is a chain of load latencies, so
-// W = 4 waves share a row of more than 4 splits, each takes U of its splits at a
-// time, and all of these loads are in flight together: up to 32 splits cost one
-// latency.  From 2048 rows on there are enough waves with one for each (us by one
-// wave a row and by four, d = 128: 512 rows of 16 splits 4.8 and 3.9, 1024 of 16
-// 5.4 and 4.8, 1024 of 5 4.0 and 4.3; 2048 of 16 5.9 and 6.7, 8192 of 8 7.4 and
-// 17.3; 512 of 4 3.3 and 3.9).
-template <int D, int W>
-__global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Attn p) {
-    constexpr int PER = D / 64, U = W == 1 ? 4 : 8;
-    typedef float vec __attribute__((ext_vector_type(PER)));
-    __shared__ vec part[4][64];
-    __shared__ float part_m[4], part_l[4];
-    const Kv4Cache& kc = p.c;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const long long row = (long long)blockIdx.x * (4 / W) + (W == 1 ? wave : 0);
-    if (row >= (long long)kc.B * p.hq * kc.n) return;
-    const int i = (int)(row % kc.n);
-    const long long bh = row / kc.n;
-    const int b = (int)(bh / p.hq), hh = (int)(bh - (long long)b * p.hq);
-    const vec* acc = reinterpret_cast<const vec*>(p.ws + (size_t)row * p.splits * D) + lane;
-    const float* ml = p.ws + (size_t)kc.B * p.hq * kc.n * p.splits * D + (size_t)row * p.splits * 2;
-    float M = kNegInf, L = 0.0f;
-    vec o = 0.0f;
-    for (int s0 = W == 1 ? 0 : wave; s0 < p.splits; s0 += U * W) {
-        float ms[U], ls[U], top = M;
-        vec a[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int s = min(s0 + u * W, p.splits - 1);
-            ms[u] = ml[2 * s];
-            ls[u] = ml[2 * s + 1];
-            a[u] = acc[(size_t)s * 64];
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (s0 + u * W >= p.splits) ms[u] = kNegInf;
-            top = fmaxf(top, ms[u]);
-        }
-        const float alpha = M == kNegInf ? 0.0f : exp2_hw(M - top);
-        M = top;
-        L *= alpha;
-        o *= alpha;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (ms[u] == kNegInf) continue;
-            const float w = exp2_hw(ms[u] - M);
-            L += w * ls[u];
-            o += w * a[u];
-        }
-    }
-    if (i >= new_tokens(kc, b)) return;   // nothing was written for this row, and nothing is
-    if constexpr (W > 1) {
-        part[wave][lane] = o;
-        if (lane == 0) { part_m[wave] = M; part_l[wave] = L; }
-        __syncthreads();
-        if (wave != 0) return;
-        const float top = fmaxf(fmaxf(part_m[0], part_m[1]), fmaxf(part_m[2], part_m[3]));
-        L = 0.0f;
-        o = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if (part_m[w] == kNegInf) continue;
-            const float f = exp2_hw(part_m[w] - top);
-            L += f * part_l[w];
-            o += f * part[w][lane];
-        }
-        M = top;
-    }
-    const bool none = M == kNegInf;   // no visible key
-    o *= none ? 0.0f : 1.0f / L;
-    const long long to = b * p.os[0] + hh * p.os[1] + i * p.os[2] + PER * lane;
-    if (p.out_bf16) {
-        typedef __bf16 out __attribute__((ext_vector_type(PER)));
-        *reinterpret_cast<out*>(static_cast<__bf16*>(p.o) + to) = __builtin_convertvector(o, out);
-    } else {
-        *reinterpret_cast<vec*>(static_cast<float*>(p.o) + to) = o;
-    }
-    if (p.lse && lane == 0) p.lse[row] = none ? kNegInf : (M + __log2f(L)) * kLn2;
-}
-
 template <int D, int RT>
 hipError_t go(const Kv4Attn& p, hipStream_t stream) {
     const int rows = p.c.n * (p.hq / p.c.hk), tiles = (rows + 16 * RT - 1) / (16 * RT);
@@ -594,9 +513,8 @@ hipError_t go(const Kv4Attn& p, hipStream_t stream) {
     };
     const hipError_t e = tiles == 1 ? run(kv4_attn_kernel<D, RT, true>) : run(kv4_attn_kernel<D, RT, false>);
     if (e != hipSuccess || p.splits == 1) return e;
-    const long long all = (long long)p.c.B * p.hq * p.c.n;
-    if (p.splits <= 4 || all >= 2048) return launch_kernel(kv4_combine_kernel<D, 1>, dim3((unsigned)((all + 3) / 4)), dim3(256), stream, p);
-    return launch_kernel(kv4_combine_kernel<D, 4>, dim3((unsigned)all), dim3(256), stream, p);
+    const SplitJoin j{p.ws, p.o, p.lse, p.c.new_lens, {p.os[0], p.os[1], p.os[2]}, p.c.B, p.hq, p.c.n, p.splits, p.out_bf16};
+    return launch_split_join<D>(j, stream);
 }
 
 }  // namespace

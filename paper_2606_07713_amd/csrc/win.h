@@ -1,0 +1,72 @@
+// Internal launch interface of the attention with a window and first visible
+// tokens, on whole tensors (moa_window.h) and over the paged cache (moa_paged.h).
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+#include <stdint.h>
+
+namespace moa {
+
+// Where the keys and values of (sequence, head) are.  Token t is row t mod 2^shift
+// of page table[b][t >> shift]; without a table sequence b is page b, and shift is
+// 31 on whole tensors, whose batches are the pages.
+struct KeySource {
+    const void *k, *v;
+    long long ks[3], vs[3];    // element strides (page, head, row)
+    const int* seq_lens;       // or null: len tokens each
+    const int* new_lens;       // or null: all rows of the call
+    const int* table;          // [B][max_pages], or null
+    int len, shift, num_pages, max_pages;
+};
+
+// Limits of what one row sees: keys j < hi with j >= lo or j < sinks, where
+// hi = position + right + 1 and lo = position - left.
+struct Window {
+    int left, right, sinks;    // left, right: kNoLimit where there is none
+};
+constexpr int kNoLimit = 1 << 30;
+
+struct WinAttn {
+    KeySource s;
+    Window w;
+    const void* q;
+    void* o;
+    float* lse;                // nullable
+    long long qs[3], os[3];    // element strides (batch, head, row)
+    int B, hq, hk, n, d;
+    float scale;
+    bool out_bf16;
+    // Key splits (1 = none) and their partial states: [B][hq][n][splits][d]
+    // fp32, then [B][hq][n][splits][2] (reference in log2 units, sum).
+    int splits;
+    float* ws;
+};
+
+// Rows (queries times the query heads of a key/value head) that a workgroup
+// takes: 16 or 32 in the kernel of few rows, 128 in that of many.
+inline int win_rows_per_block(long long rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 128; }
+
+hipError_t launch_win_attn(const WinAttn& p, hipStream_t stream);
+// The two kernels behind it.
+hipError_t launch_win_few(const WinAttn& p, hipStream_t stream);
+hipError_t launch_win_many(const WinAttn& p, hipStream_t stream);
+
+// Gradients on whole tensors.
+struct WinGrad {
+    Window w;
+    const void *q, *k, *v, *o, *dout;
+    const float* lse;
+    void *dq, *dk, *dv;
+    // element strides (batch, head, row)
+    long long qs[3], ks[3], vs[3], os[3], gs[3], dqs[3], dks[3], dvs[3];
+    int B, hq, hk, nq, nk, d;
+    float scale;
+    bool o_bf16;
+    float* dsum;               // [B][hq][nq]: <dO, O> of every row
+    float* part;               // partial sums of dK and dV of the keys that far queries see
+    int chunks;                // of the queries behind the first keys' windows
+};
+
+hipError_t launch_win_bwd(const WinGrad& p, hipStream_t stream);
+
+}  // namespace moa

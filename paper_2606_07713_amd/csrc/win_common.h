@@ -1,0 +1,205 @@
+// Device-side pieces of the attention with a window: which keys a row sees, the
+// walk over the key tiles that any of some rows see, and a row's result by its
+// definition.
+#pragma once
+
+#include "device_common.h"
+#include "win.h"
+
+namespace moa {
+namespace win {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Max and sum over the four lanes with the same lane % 16.
+__device__ __forceinline__ float column_max(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return half_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float column_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const bf16x2 t = {(__bf16)lo, (__bf16)hi};
+    return __builtin_bit_cast(uint32_t, t);
+}
+
+// a and b as sums of TERMS bf16 numbers each, every one the nearest to what the ones
+// before it leave (8 bits and a sign: 2^-9, 2^-18, 2^-27 of a weight at most is lost).
+template <int TERMS>
+__device__ __forceinline__ void bf16_terms(float a, float b, uint32_t (&w)[TERMS]) {
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t) {
+        w[t] = pack2(a, b);
+        if (t + 1 < TERMS) {
+            a -= bf16lo_to_f32(w[t]);
+            b -= bf16hi_to_f32(w[t]);
+        }
+    }
+}
+
+// New tokens of sequence b, its length, and the tokens that the pages have room
+// for at most.
+__device__ __forceinline__ int new_tokens(const int* new_lens, int b, int n) {
+    return new_lens ? min(max(new_lens[b], 0), n) : n;
+}
+__device__ __forceinline__ int length(const KeySource& s, int b) { return s.seq_lens ? s.seq_lens[b] : s.len; }
+__device__ __forceinline__ int capacity(const KeySource& s) {
+    return s.seq_lens ? (s.num_pages ? s.max_pages << s.shift : 0) : s.len;
+}
+
+// The page of key `key` of sequence b, or -1.
+__device__ __forceinline__ int page_of(const KeySource& s, int b, int key) {
+    if (!s.table) return b;
+    const int index = key >> s.shift;
+    if (index >= s.max_pages) return -1;
+    const int id = s.table[(size_t)b * s.max_pages + index];
+    return id >= 0 && id < s.num_pages ? id : -1;
+}
+
+// Element offset of key `key` in its page of a pool with strides st.
+__device__ __forceinline__ long long key_offset(const long long (&st)[3], int shift, int page, int head, int key) {
+    const int row = shift < 31 ? key & ((1 << shift) - 1) : key;
+    return page * st[0] + head * st[1] + row * st[2];
+}
+
+// Keys that a row sees: j < hi with j >= lo or j < sinks (0 <= lo).
+struct Seen {
+    int lo, hi;
+};
+
+// Of a row at position pos of a sequence with `end` keys.
+__device__ __forceinline__ Seen seen_from(const Window& w, long long pos, int end) {
+    Seen s;
+    s.hi = w.right == kNoLimit ? end : (int)max(0ll, min((long long)end, pos + w.right + 1));
+    s.lo = w.left == kNoLimit ? 0 : (int)min((long long)end, max(0ll, pos - w.left));
+    return s;
+}
+__device__ __forceinline__ bool sees(const Seen& s, int sinks, int key) {
+    return key < s.hi && (key >= s.lo || key < sinks);
+}
+__device__ __forceinline__ bool sees_any(const Seen& s, int sinks) { return s.hi > 0 && (s.lo < s.hi || sinks > 0); }
+
+// The tiles of T keys that any of the rows from `first` to `last` (positions in
+// order) see: those of the first keys, then those of the windows.
+template <int T>
+struct Tiles {
+    int head, skip, count;
+    __device__ __forceinline__ Tiles(const Seen& first, const Seen& last, int sinks) {
+        const int end = (last.hi + T - 1) / T, from = first.lo / T;
+        head = (min(sinks, last.hi) + T - 1) / T;
+        const int begin = max(from, head);
+        skip = begin - head;
+        count = head + max(0, end - begin);
+    }
+    __device__ __forceinline__ int at(int v) const { return v < head ? v : v + skip; }
+};
+
+// One row by its definition, by one wave, over the keys of tiles begin .. end - 1:
+// scores in fp64, weights of at most 1, nothing of a key that the row does not
+// see.  For the rows whose sums in the tile kernels did not come out finite: a
+// value that is infinite or NaN (which a product with a weight of 0 spreads to
+// rows that do not see it), or a score or a sum beyond fp32.  o: this lane's
+// elements D/64 lane ..; without `partial` divided by the sum, with it the state
+// of a split.
+template <int D, int T>
+__device__ void row_by_definition(const WinAttn& p, int b, int h, const u16* q, const Seen& seen, const Tiles<T>& tiles,
+                                  int begin, int end, bool partial, float (&o)[D / 64], float& ref, float& sum) {
+    // Both walks have to see the same scores, bit for bit: of one of 2^100 a single
+    // rounding is 2^47.
+#pragma clang fp contract(off)
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+    const double c = (double)p.scale * 1.4426950408889634;
+    const auto score = [&](int key, int page) {
+#pragma clang fp contract(off)
+        const u16* k = static_cast<const u16*>(p.s.k) + key_offset(p.s.ks, p.s.shift, page, h, key);
+        double x = 0.0;
+        for (int e = 0; e < D; e += 2) {
+            const uint32_t a = *reinterpret_cast<const uint32_t*>(q + e), y = *reinterpret_cast<const uint32_t*>(k + e);
+            x += (double)bf16lo_to_f32(a) * (double)bf16lo_to_f32(y) + (double)bf16hi_to_f32(a) * (double)bf16hi_to_f32(y);
+        }
+        return x * c;
+    };
+    const auto walk = [&](auto f) {
+        for (int v = begin; v < end; ++v)
+            for (int k0 = tiles.at(v) * T; k0 < (tiles.at(v) + 1) * T; k0 += 64) {
+                const int key = k0 + lane;
+                const bool in = lane < T && sees(seen, p.w.sinks, key);
+                const int page = in ? page_of(p.s, b, key) : -1;
+                if (wave_any(page >= 0)) f(k0, key, page);
+            }
+    };
+    double M = -__builtin_inf(), L = 0.0;
+    bool any = false;
+    walk([&](int, int key, int page) {
+#pragma clang fp contract(off)
+        double x = page >= 0 ? score(key, page) : -__builtin_inf();
+        double m = x;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) m = fmax(m, __shfl_xor(m, s));
+        any = true;
+        const double top = fmax(M, m);
+        double w = page >= 0 ? exp2(x - top) : 0.0;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) w += __shfl_xor(w, s);
+        L = (M == -__builtin_inf() ? 0.0 : L * exp2(M - top)) + w;
+        M = top;
+    });
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.0f;
+    ref = kNegInf;
+    sum = 0.0f;
+    if (!any) return;
+    const double inv = partial ? 1.0 : 1.0 / L;
+    walk([&](int k0, int key, int page) {
+#pragma clang fp contract(off)
+        const float w = page >= 0 ? (float)(exp2(score(key, page) - M) * inv) : 0.0f;
+        for (int j = 0; j < 64; ++j) {
+            const int pj = __shfl(page, j);
+            if (pj < 0) continue;
+            const float wj = __shfl(w, j);
+            const u16* v = static_cast<const u16*>(p.s.v) + key_offset(p.s.vs, p.s.shift, pj, h, k0 + j) + E * lane;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(wj, __uint_as_float((uint32_t)v[e] << 16), o[e]);
+        }
+    });
+    // A reference that is not finite would drop out of a join.
+    const bool finite = M > -3e38 && M < 3e38;
+    ref = finite || !partial ? (float)M : 0.0f;
+    sum = finite ? (float)L : __builtin_nanf("");
+    if (!finite && partial)
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = __builtin_nanf("");
+}
+
+// Stores such a row: O and LSE, or the state of split sp.
+template <int D>
+__device__ __forceinline__ void store_row(const WinAttn& p, int b, int hh, int qi, int sp, const float (&o)[D / 64],
+                                          float ref, float sum) {
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+    const size_t at = ((size_t)b * p.hq + hh) * p.n + qi;
+    if (p.splits > 1) {
+        float* ml = p.ws + (size_t)p.B * p.hq * p.n * p.splits * D + (at * p.splits + sp) * 2;
+#pragma unroll
+        for (int e = 0; e < E; ++e) p.ws[(at * p.splits + sp) * D + E * lane + e] = o[e];
+        if (lane == 0) {
+            ml[0] = ref;
+            ml[1] = sum;
+        }
+        return;
+    }
+    const long long to = b * p.os[0] + hh * p.os[1] + qi * p.os[2] + E * lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if (p.out_bf16) static_cast<__bf16*>(p.o)[to + e] = (__bf16)o[e];
+        else static_cast<float*>(p.o)[to + e] = o[e];
+    }
+    if (p.lse && lane == 0) p.lse[at] = ref == kNegInf ? kNegInf : (ref + __log2f(sum)) * kLn2;
+}
+
+}  // namespace win
+}  // namespace moa

@@ -1,0 +1,378 @@
+// Attention with a window for many rows (moa_window.h, moa_paged.h).
+//
+// One workgroup = 4 waves x 32 rows of one key/value head, a row being a query and
+// one of the G = Hq/Hk heads that share it, query by query: keys and values are
+// read once for all of them, and 128 rows are only 128/G positions wide, so that
+// a window's ragged ends cost little.  K and V stream through a two-stage LDS ring
+// in 64-key tiles, one barrier per tile, in the layout and with the products of
+// the prefill kernels (prefill_bf16_common.h).  Each wave loads 16 of a tile's
+// rows, which lie in one page whatever its size.  Only tiles that a row of the
+// workgroup sees are walked: those of the first visible keys, then the windows'.
+//
+// Softmax: a running reference per row, the maximum of the first tile that it
+// sees; later ones are weighed against it as they come, and it is raised where a
+// lane's sum of 32 keys exceeds 2^20.  The sums are of the fp32 weights.  A weight
+// meets V as one bf16 number for a bf16 output (2^-9 each, which leaves the error
+// of a bf16 output at 1.4 times its own rounding's), as three for an fp32 output
+// (two left it at 2.3e-6, nine times what fp32 sums alone make).
+#include <limits>
+
+#include "prefill_bf16_common.h"
+#include "split_join.h"
+#include "win_common.h"
+
+namespace moa {
+namespace {
+
+using namespace win;
+using pf::BN;
+using pf::Cfg;
+using pf::dv_of;
+using pf::lds_v4s;
+using pf::swz;
+using pf::v4s;
+
+constexpr int MW = 4;            // waves
+constexpr int MROWS = MW * 32;   // rows per workgroup
+
+// How O leaves: bf16, fp32, or the fp32 state of a split.
+enum { TO_BF16, TO_F32, TO_STATE };
+
+template <int D, int OUT, int TERMS>
+__global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(WinAttn p, float c, uint32_t qflip, int row_tiles) {
+    using C = Cfg<D>;
+    constexpr uint32_t RB = C::ROW_BYTES;
+    constexpr int SN = 32;                                // keys per step
+    constexpr int LPW = C::TILE_BYTES / (MW * 1024);      // 16-byte loads per lane per tile
+    // One array per ring stage: the compiler tracks direct-to-LDS loads per object.
+    __shared__ __attribute__((aligned(1024))) unsigned char k_st0[C::TILE_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char k_st1[C::TILE_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_st0[C::TILE_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_st1[C::TILE_BYTES];
+    using S0 = std::integral_constant<int, 0>;
+    using S1 = std::integral_constant<int, 1>;
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const KeySource& src = p.s;
+    const int G = p.hq / p.hk;
+    // Row tiles last, those of the highest positions first; the heads next to each
+    // other, so that the row tiles of a head mostly go to one XCD.
+    int blk = blockIdx.x;
+    const int groups = p.B * p.hk * p.splits, rt = row_tiles - 1 - blk / groups;
+    blk %= groups;
+    const int sp = blk % p.splits; blk /= p.splits;
+    const int h = blk % p.hk, b = blk / p.hk;
+
+    const int count = new_tokens(src.new_lens, b, p.n), rows = count * G, row0 = rt * MROWS;
+    if (row0 >= rows) return;
+    const int len = length(src, b), end = max(0, min(len, capacity(src)));
+    const long long first = (long long)len - count;   // position of query 0
+    const auto seen_of = [&](int row) { return seen_from(p.w, first + row / G, end); };
+    const auto uniform = [](Seen s) {
+        return Seen{__builtin_amdgcn_readfirstlane(s.lo), __builtin_amdgcn_readfirstlane(s.hi)};
+    };
+    const Seen low = uniform(seen_of(row0)), high = uniform(seen_of(min(row0 + MROWS, rows) - 1));
+    const Tiles<BN> tiles(low, high, p.w.sinks);
+    const int per = (tiles.count + p.splits - 1) / p.splits, begin = sp * per, stop = min(tiles.count, begin + per);
+
+    // This wave's rows.
+    const int w0 = row0 + wave * 32, row = w0 + col;
+    const bool live = w0 < rows, in = row < rows;
+    const Seen wl = uniform(seen_of(min(w0, rows - 1))), wh = uniform(seen_of(min(w0 + 32, rows) - 1));
+    const Seen seen = seen_of(min(row, rows - 1));
+
+    bf16x8 qf[D / 16];
+    {
+        const int qi = in ? row / G : 0, hh = h * G + (in ? row - qi * G : 0);
+        const u16* at = static_cast<const u16*>(p.q) + b * p.qs[0] + hh * p.qs[1] + qi * p.qs[2] + half * 8;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            u32x4 w = {0, 0, 0, 0};
+            if (in) w = *reinterpret_cast<const u32x4*>(at + 16 * s);
+            qf[s] = __builtin_bit_cast(bf16x8, w ^ qflip);
+        }
+    }
+
+    const uint32_t krb = (uint32_t)src.ks[2] * 2u, vrb = (uint32_t)src.vs[2] * 2u;
+    uint32_t ld_koff[LPW], ld_voff[LPW];
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+        const int slot = (wave * LPW + i) * 64 + lane;
+        const int r = slot / C::CHUNKS, ch = slot % C::CHUNKS;
+        const uint32_t chunk = (uint32_t)((ch ^ swz<D>(r)) * 16);
+        ld_koff[i] = (uint32_t)(r & 15) * krb + chunk;   // this wave's 16 rows of the tile
+        ld_voff[i] = (uint32_t)(r & 15) * vrb + chunk;
+    }
+    // Lane 4 i + t holds the page of 16-key group t of the i-th tile from `known` on.
+    int pages = 0, known = begin;
+    const auto look = [&]() {
+        const int v = known + (lane >> 2), key = tiles.at(v) * BN + 16 * (lane & 3);
+        pages = v < stop && key < end ? page_of(src, b, key) : -1;
+    };
+    // Starts the loads of the v-th tile; bit t of the result: group t has a page.
+    // Tokens behind the last, and those without a page, become zeros.
+    auto issue = [&](int v, auto stage) __attribute__((always_inline)) -> int {
+        unsigned char* ks = decltype(stage)::value == 0 ? k_st0 : k_st1;
+        unsigned char* vs = decltype(stage)::value == 0 ? v_st0 : v_st1;
+        if (v - known == 16) {
+            known = v;
+            look();
+        }
+        const int i = v - known, key = tiles.at(v) * BN + 16 * wave;
+        const int page = __builtin_amdgcn_readlane(pages, 4 * i + wave);
+        const int n = page >= 0 ? max(0, min(16, end - key)) : 0;
+        const u16* kb = static_cast<const u16*>(src.k) + (n ? key_offset(src.ks, src.shift, page, h, key) : 0);
+        const u16* vb = static_cast<const u16*>(src.v) + (n ? key_offset(src.vs, src.shift, page, h, key) : 0);
+        const auto rk = make_rsrc(kb, rows_extent(n, krb, RB)), rv = make_rsrc(vb, rows_extent(n, vrb, RB));
+#pragma unroll
+        for (int j = 0; j < LPW; ++j) buffer_load16_to_lds(rk, ks + (wave * LPW + j) * 1024, ld_koff[j]);
+#pragma unroll
+        for (int j = 0; j < LPW; ++j) buffer_load16_to_lds(rv, vs + (wave * LPW + j) * 1024, ld_voff[j]);
+        return (int)(__ballot(pages >= 0) >> (4 * i)) & 15;
+    };
+    uint32_t kaddr[D / 16], vaddr[D / 32][2];
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+        kaddr[s] = (uint32_t)col * RB + (uint32_t)(((2 * s + half) ^ swz<D>(col)) * 16);
+    {
+        const int g = lane >> 4, j = (lane >> 2) & 3, q = lane & 3;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int h8 = 0; h8 < 2; ++h8) {
+                const int r = 4 * (g >> 1) + j + 8 * h8, dv = dv_of<D>(d, 16 * (g & 1) + 4 * q);
+                vaddr[d][h8] = (uint32_t)r * RB + (uint32_t)((((dv >> 3) ^ swz<D>(r)) * 16) + (dv & 7) * 2);
+            }
+    }
+
+    f32x16 oacc[D / 32];
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) oacc[d] = f32x16{};
+    float ref = kNegInf;     // log2 units
+    float neg = 0.0f;        // -ref, or 0 while it is -inf
+    float l = 0.0f;          // sum over this half-wave's keys
+
+    auto tile = [&](int v, int have, auto stage) __attribute__((always_inline)) {
+        const unsigned char* ks = decltype(stage)::value == 0 ? k_st0 : k_st1;
+        unsigned char* vs = decltype(stage)::value == 0 ? v_st0 : v_st1;
+        const int k0 = tiles.at(v) * BN;
+        // Nothing for this wave's rows, or no row hides a key of it.
+        if (!live || k0 >= wh.hi || (k0 + BN <= wl.lo && k0 >= p.w.sinks)) return;
+        const bool need_mask = have != 15 || k0 + BN > wl.hi || (k0 < wh.lo && k0 + BN > p.w.sinks);
+#pragma unroll
+        for (int sb = 0; sb < BN / SN; ++sb) {
+            f32x16 s = f32x16{};
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    *reinterpret_cast<const bf16x8*>(ks + kaddr[k] + sb * SN * RB), qf[k], s, 0, 0, 0);
+            if (need_mask) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int in_tile = sb * SN + (i >> 2) * 8 + half * 4 + (i & 3);
+                    if (!((have >> (in_tile >> 4)) & 1) || !sees(seen, p.w.sinks, k0 + in_tile)) s[i] = kNegInf;
+                }
+            }
+            const auto raise = [&]() __attribute__((always_inline)) {
+                float m = kNegInf;
+                asm volatile("" : "+v"(m));   // not hoisted onto the fast path
+#pragma unroll
+                for (int i = 0; i < 16; ++i) m = fmaxf(m, s[i]);
+                m = fmaxf(ref, half_max(m) * c);
+                const float a = ref == kNegInf ? 0.0f : exp2_hw(ref - m);
+                l *= a;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) oacc[d] *= a;
+                ref = m;
+                neg = m == kNegInf ? 0.0f : -m;
+            };
+            u32x4 pt[SN / 16][TERMS];
+            const auto weights = [&]() __attribute__((always_inline)) {
+                float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int g = 0; g < SN / 16; ++g) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int i = g * 8 + 2 * j;
+                        const float a = exp2_hw(__builtin_fmaf(s[i], c, neg)), d = exp2_hw(__builtin_fmaf(s[i + 1], c, neg));
+                        sum[0] += a;
+                        sum[1] += d;
+                        uint32_t x[TERMS];
+                        bf16_terms<TERMS>(a, d, x);
+#pragma unroll
+                        for (int k = 0; k < TERMS; ++k) pt[g][k][j] = x[k];
+                    }
+                }
+                return sum[0] + sum[1];
+            };
+            if (wave_any(ref == kNegInf)) raise();
+            float part = weights();
+            if (wave_any(!(part <= pf::kFastSumLimit))) {
+                raise();
+                part = weights();
+            }
+            l += part;
+#pragma unroll
+            for (int cc = 0; cc < SN / 16; ++cc)
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) {
+                    const int r = (sb * (SN / 16) + cc) * 16;
+                    const v4s both[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(vs + vaddr[d][0] + r * RB)),
+                                         __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(vs + vaddr[d][1] + r * RB))};
+                    const bf16x8 a = __builtin_bit_cast(bf16x8, both);
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k)
+                        oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, pt[cc][k]), oacc[d], 0, 0, 0);
+                }
+        }
+    };
+
+    // The v-th tile sits in stage v - begin & 1.  After the barrier at its start
+    // every wave has its part of it in LDS and is done with the tile before, into
+    // whose stage the next one is loaded while this one is worked on.
+    if (begin < stop) {
+        look();
+        int have0 = issue(begin, S0{}), have1 = 0;
+        for (int v = begin; v < stop; v += 2) {
+            pf::wait_vmcnt<0>();
+            __syncthreads();
+            if (v + 1 < stop) have1 = issue(v + 1, S1{});
+            tile(v, have0, S0{});
+            if (v + 1 >= stop) break;
+            pf::wait_vmcnt<0>();
+            __syncthreads();
+            if (v + 2 < stop) have0 = issue(v + 2, S0{});
+            tile(v + 1, have1, S1{});
+        }
+    }
+    __syncthreads();   // every wave is done with the stages
+    if (!live) return;
+
+    // O = acc / l (or the sums as they are) through a 32-row slice of the stages,
+    // whole rows per store.
+    unsigned char* stg = (wave < 2 ? k_st0 : k_st1) + (wave & 1) * 32 * RB;
+    const float total = half_sum(l);
+    const bool none = ref == kNegInf;   // no visible key
+    const float inv = OUT == TO_STATE ? 1.0f : none ? 0.0f : 1.0f / total;
+    // Sums that are not finite, or none at all in a row that sees keys.
+    float zero = 0.0f * total;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(oacc[d][i], 0.0f, zero);
+    zero = half_sum(zero);
+    const bool odd = in && (!(zero == 0.0f) || (total == 0.0f && begin < stop && sees_any(seen, p.w.sinks)));
+    int ln = lane;
+    asm volatile("" : "+v"(ln));   // staging addresses are formed here, not above the loop
+    const int cl = ln & 31, hf = ln >> 5;
+    // Row r of this wave's 32: its query head and query.
+    const auto place = [&](int r, int& hh, int& qi) {
+        qi = (w0 + r) / G;
+        hh = h * G + (w0 + r) - qi * G;
+    };
+    if constexpr (OUT == TO_BF16) {
+        constexpr int CHK = C::CHUNKS, RPI = 64 / CHK;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int dv = dv_of<D>(d, g * 8 + hf * 4);
+                *reinterpret_cast<uint2*>(stg + (uint32_t)cl * RB + (uint32_t)((((dv >> 3) ^ (cl & (CHK - 1))) * 16) + (dv & 7) * 2)) =
+                    make_uint2(pack2(oacc[d][g * 4 + 0] * inv, oacc[d][g * 4 + 1] * inv),
+                               pack2(oacc[d][g * 4 + 2] * inv, oacc[d][g * 4 + 3] * inv));
+            }
+        pf::wait_lgkmcnt0();   // only this wave reads its rows
+        const int rr = ln / CHK, ch = ln % CHK;
+#pragma unroll
+        for (int i = 0; i < 32 / RPI; ++i) {
+            const int r = i * RPI + rr;
+            const uint4 x = *reinterpret_cast<const uint4*>(stg + (uint32_t)r * RB + (uint32_t)((ch ^ (r & (CHK - 1))) * 16));
+            if (w0 + r >= rows) continue;
+            int hh, qi;
+            place(r, hh, qi);
+            *reinterpret_cast<uint4*>(static_cast<u16*>(p.o) + b * p.os[0] + hh * p.os[1] + qi * p.os[2] + ch * 8) = x;
+        }
+    } else {
+        // fp32 rows in two passes of D / 2 columns
+        constexpr int HB = D * 2, HCH = HB / 16, RPI = 64 / HCH;
+        const int rr = ln / HCH, ch = ln % HCH;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    if (dv_of<D>(d, g * 8) / (D / 2) != u) continue;
+                    const int cc = (dv_of<D>(d, g * 8 + hf * 4) - u * (D / 2)) / 4;
+                    *reinterpret_cast<float4*>(stg + (uint32_t)cl * HB + (uint32_t)((cc ^ (cl & (HCH - 1))) * 16)) =
+                        make_float4(oacc[d][g * 4 + 0] * inv, oacc[d][g * 4 + 1] * inv, oacc[d][g * 4 + 2] * inv, oacc[d][g * 4 + 3] * inv);
+                }
+            pf::wait_lgkmcnt0();
+#pragma unroll
+            for (int i = 0; i < 32 / RPI; ++i) {
+                const int r = i * RPI + rr;
+                const float4 x = *reinterpret_cast<const float4*>(stg + (uint32_t)r * HB + (uint32_t)((ch ^ (r & (HCH - 1))) * 16));
+                if (w0 + r >= rows) continue;
+                int hh, qi;
+                place(r, hh, qi);
+                float* to;
+                if constexpr (OUT == TO_STATE) to = p.ws + ((((size_t)b * p.hq + hh) * p.n + qi) * p.splits + sp) * D;
+                else to = static_cast<float*>(p.o) + b * p.os[0] + hh * p.os[1] + qi * p.os[2];
+                *reinterpret_cast<float4*>(to + u * (D / 2) + ch * 4) = x;
+            }
+            pf::wait_lgkmcnt0();
+        }
+    }
+    if (half == 0 && in) {
+        int hh, qi;
+        place(col, hh, qi);
+        const size_t at = ((size_t)b * p.hq + hh) * p.n + qi;
+        if constexpr (OUT == TO_STATE) {
+            float* ml = p.ws + (size_t)p.B * p.hq * p.n * p.splits * D + (at * p.splits + sp) * 2;
+            ml[0] = ref;
+            ml[1] = total;
+        } else {
+            if (p.lse) p.lse[at] = none ? kNegInf : (ref + __log2f(total)) * kLn2;
+        }
+    }
+    // Rows that have to be done by their definition.
+    for (uint32_t left = (uint32_t)__ballot(odd); left; left &= left - 1) {
+        int hh, qi;
+        const int r = __builtin_ctz(left);
+        place(r, hh, qi);
+        float f[D / 64], M, L;
+        row_by_definition<D, BN>(p, b, h, static_cast<const u16*>(p.q) + b * p.qs[0] + hh * p.qs[1] + qi * p.qs[2],
+                                 seen_of(w0 + r), tiles, begin, stop, OUT == TO_STATE, f, M, L);
+        store_row<D>(p, b, hh, qi, sp, f, M, L);
+    }
+}
+
+template <int D>
+hipError_t go(const WinAttn& p, hipStream_t stream) {
+    const long long rows = (long long)p.n * (p.hq / p.hk);
+    const int tiles = (int)((rows + MROWS - 1) / MROWS);
+    // As in the kernel of few rows.
+    float c = p.scale * kLog2e;
+    const uint32_t flip = c < 0.0f ? 0x80008000u : 0u;
+    c = c < 0.0f ? -c : c;
+    if (c == 0.0f) c = std::numeric_limits<float>::denorm_min();
+    const long long blocks = (long long)p.B * p.hk * tiles * p.splits;
+    const auto run = [&](auto kernel) {
+        return launch_kernel(kernel, dim3((unsigned)blocks), dim3(MW * 64), stream, p, c, flip, tiles);
+    };
+    if (p.splits == 1) return p.out_bf16 ? run(win_many_kernel<D, TO_BF16, 1>) : run(win_many_kernel<D, TO_F32, 3>);
+    const hipError_t e = p.out_bf16 ? run(win_many_kernel<D, TO_STATE, 1>) : run(win_many_kernel<D, TO_STATE, 3>);
+    if (e != hipSuccess) return e;
+    const SplitJoin j{p.ws, p.o, p.lse, p.s.new_lens, {p.os[0], p.os[1], p.os[2]}, p.B, p.hq, p.n, p.splits, p.out_bf16};
+    return launch_split_join<D>(j, stream);
+}
+
+}  // namespace
+
+hipError_t launch_win_many(const WinAttn& p, hipStream_t stream) {
+    return p.d == 64 ? go<64>(p, stream) : go<128>(p, stream);
+}
+
+}  // namespace moa
