@@ -34,6 +34,46 @@ extern "C" {
 #endif
 
 /*
+ * moa_paged_append -- new tokens into the cache.  Every head row of Q and K is normed
+ * (where there is a weight) and turned by its token's position, exactly as
+ * moa_qk_norm_rope does, and rounded to bf16 once: Q's into Qo, K's into k_pool; V's
+ * rows go into v_pool as they are, rounded to bf16.
+ *
+ * Q, K, V   device inputs of storage type dtype (MOA_F32 or MOA_BF16), logical shapes
+ *           [B][Hq][N][d], [B][Hk][N][d] and [B][Hk][N][d].  Input rows may overlap.
+ * Qo        device output, bf16, [B][Hq][N][d].  May be Q (bf16, same pointer and
+ *           strides: in place).
+ * k_pool, v_pool
+ *           the cache, written: 16-byte aligned, no element of the two twice.
+ * wq, wk    norm weights [d] of storage type w_dtype, or NULL: no norm.
+ * positions device int64 [axes][B][N], any values, or NULL: every token's place in its
+ *           sequence, seq_lens[b] - new_lens[b] + i, on every axis.
+ * inv_freq, rot, axes, sections, interleaved, eps
+ *           as for moa_qk_norm_rope (rot = 0: no rotation).
+ * B, Hq, Hk, N, d, page, num_pages, max_pages
+ *           all may be 0 but d and page; supported: d in {64, 128}, max_pages * page
+ *           <= 2^30, num_pages < 2^30, B * N < 2^27, Hq + Hk < 2^30, B * N * (Hq + 2 Hk) <
+ *           2^31.
+ * *_strides element strides (batch, head, row), of the pools (page, head, row), or
+ *           NULL: contiguous.  Non-negative multiples of 16 bytes.
+ *
+ * Two rows of one call must not be the same token of the same page (which one stays
+ * is then undefined).  Qo and the inputs may be views that interleave in one buffer
+ * of bf16 (heads of a packed projection output), and so may the two pools, where
+ * their rows or their batches (pages) take turns in it; nothing else may overlap.
+ * Queries of skipped tokens are turned all the same.  One kernel; deterministic.
+ */
+int moa_paged_append(const void* Q, const void* K, const void* V, void* Qo, void* k_pool,
+                     void* v_pool, const void* wq, const void* wk, const int64_t* positions,
+                     const float* inv_freq, const int32_t* seq_lens, const int32_t* new_lens,
+                     const int32_t* page_table, int64_t B, int64_t Hq, int64_t Hk, int64_t N,
+                     int64_t d, int64_t rot, int64_t page, int64_t num_pages, int64_t max_pages,
+                     const int64_t* q_strides, const int64_t* k_strides, const int64_t* v_strides,
+                     const int64_t* qo_strides, const int64_t* k_pool_strides,
+                     const int64_t* v_pool_strides, int axes, const int64_t* sections,
+                     int interleaved, float eps, int dtype, int w_dtype, void* stream);
+
+/*
  * moa_paged_attn_num_splits, moa_paged_attn_workspace_bytes -- the key splits that a
  * moa_paged_attn_fwd call with these arguments uses, and the device workspace it
  * then needs in bytes (0 when it does not split).  num_splits: 0 = the library's

@@ -14,8 +14,8 @@ names here as well: ``rope`` (``include/moa_rope.h``: norms of queries and keys
 for each head with the rotation by position, and the gradients), ``kv4``
 (``include/moa_kv4.h``: a key/value cache held in four bits and the attention
 over it), ``window`` (``include/moa_window.h``: attention in a sliding window, with
-shared heads) and ``paged`` (``include/moa_paged.h``: a paged cache in bf16 and the
-attention over it).
+shared heads) and ``paged`` (``include/moa_paged.h``: a paged cache in bf16,
+appending to it with norms and rotation, and the attention over it).
 
 There is no fallback: if the HIP library has not been built, importing this
 package raises ``ImportError``.
@@ -41,7 +41,7 @@ __all__ = [
     "kv4_cache", "kv4_write", "kv4_read", "kv4_attn_fwd",
     "moa_win_attn_fwd", "moa_win_attn_num_splits", "moa_win_attn_workspace_bytes", "win_attn_fwd",
     "moa_paged_attn_fwd", "moa_paged_attn_num_splits", "moa_paged_attn_workspace_bytes",
-    "paged_cache", "paged_attn_fwd",
+    "moa_paged_append", "paged_cache", "paged_append", "paged_attn_fwd",
 ]
 
 MOA_OK, MOA_ERR_INVALID_ARG, MOA_ERR_UNSUPPORTED, MOA_ERR_WORKSPACE, MOA_ERR_HIP = 0, 1, 2, 3, 4
@@ -391,4 +391,5 @@ from .kv4 import (  # noqa: E402
 from .window import (  # noqa: E402
     moa_win_attn_fwd, moa_win_attn_num_splits, moa_win_attn_workspace_bytes, win_attn_fwd)
 from .paged import (  # noqa: E402
-    moa_paged_attn_fwd, moa_paged_attn_num_splits, moa_paged_attn_workspace_bytes, paged_attn_fwd, paged_cache)
+    moa_paged_append, moa_paged_attn_fwd, moa_paged_attn_num_splits, moa_paged_attn_workspace_bytes, paged_append,
+    paged_attn_fwd, paged_cache)

@@ -6,7 +6,7 @@
 
 #include "../../include/moa_paged.h"
 #include "../../include/moa_window.h"
-#include "api_checks.h"
+#include "api_pools.h"
 #include "packed.h"
 #include "win.h"
 
@@ -14,9 +14,7 @@ namespace {
 
 using namespace moa;
 
-constexpr int64_t kMost = int64_t(1) << 30;     // positions and sizes: sums of two stay in 32 bits
 constexpr int64_t kMaxRows = int64_t(1) << 26;  // B * Hq * N: four rows a workgroup when splits are joined
-constexpr int64_t kMaxRowStride = int64_t(1) << 25;   // 16 rows' bytes stay in 32 bits
 constexpr int kMaxSplits = 256;
 constexpr float kMaxScale = 0x1p127f;           // times log2(e) is still finite
 // Workgroups of 256 threads in one launch: its threads are counted in 32 bits.
@@ -135,37 +133,6 @@ int run(const Call& c, const Sizes& s, const KeySource& src, const Buf* keys, in
     return hip_status(launch_win_attn(p, static_cast<hipStream_t>(c.stream)));
 }
 
-// The two pools of a paged cache.
-struct Pools {
-    int64_t page, num_pages, max_pages;
-    const int32_t *seq_lens, *new_lens, *table;
-};
-
-int64_t capacity(const Pools& c) { return c.max_pages * c.page; }
-
-int log2_of(int64_t page) {
-    int k = 0;
-    while ((int64_t(1) << k) < page) ++k;
-    return k;
-}
-
-int check_pools(const Pools& c, int64_t B, int64_t N, bool any) {
-    if (c.page < 1 || c.num_pages < 0 || c.max_pages < 0) return MOA_ERR_INVALID_ARG;
-    if (c.page < 16 || c.page > (int64_t(1) << 20) || (c.page & (c.page - 1))) return MOA_ERR_UNSUPPORTED;
-    if (c.num_pages >= kMost || c.max_pages > kMost / c.page || N > kMost) return MOA_ERR_UNSUPPORTED;
-    if (!c.table && any && (c.max_pages != 1 || c.num_pages < B)) return MOA_ERR_INVALID_ARG;
-    if (any && !c.seq_lens) return MOA_ERR_INVALID_ARG;
-    for (const void* p : {c.seq_lens, c.new_lens, c.table})
-        if (reinterpret_cast<uintptr_t>(p) & 3) return MOA_ERR_INVALID_ARG;
-    return MOA_OK;
-}
-
-// A pool of keys or values.
-int check_pool(const void* p, const Strides& s, const Pools& c, int64_t Hk, int64_t d, bool out) {
-    if (s.r > kMaxRowStride) return MOA_ERR_UNSUPPORTED;
-    return check_tensor(p, s, c.num_pages, Hk, c.page, d, 2, out);
-}
-
 }  // namespace
 
 extern "C" {
@@ -252,17 +219,10 @@ int moa_paged_attn_fwd(const void* Q, const void* k_pool, const void* v_pool, vo
                  workspace, workspace_bytes, pick_splits(s, num_splits), stream};
     if ((st = check_call(c, s))) return st;
     if (!any) return MOA_OK;
-    KeySource src{};
-    src.k = k_pool; src.v = v_pool;
-    put(src.ks, sk); put(src.vs, sv);
-    src.seq_lens = seq_lens; src.new_lens = new_lens; src.table = page_table;
-    src.shift = log2_of(page);
-    src.num_pages = (int)num_pages;
-    src.max_pages = (int)max_pages;
+    const Lists lists(pools, B);
     const Buf keys[] = {{k_pool, extent_bytes(sk, num_pages, Hk, page, d, 2)}, {v_pool, extent_bytes(sv, num_pages, Hk, page, d, 2)},
-                        {seq_lens, (size_t)B * 4}, {new_lens, new_lens ? (size_t)B * 4 : 0},
-                        {page_table, page_table ? (size_t)B * (size_t)max_pages * 4 : 0}};
-    return run(c, s, src, keys, 5);
+                        lists.b[0], lists.b[1], lists.b[2]};
+    return run(c, s, source_of(pools, k_pool, v_pool, sk, sv), keys, 5);
 }
 
 // Words: the arguments in their order, but 4 for each tensor's strides (the last

@@ -1,4 +1,4 @@
-"""A paged key/value cache in bf16: the attention over it (``include/moa_paged.h``).
+"""A paged key/value cache in bf16: appending to it and the attention over it (``include/moa_paged.h``).
 
 A cache is two bf16 tensors [num_pages, heads, page, d] (``paged_cache``; any views with contiguous
 heads), page a power of two from 16 on.  ``seq_lens`` int32 [B] counts the tokens of every sequence,
@@ -14,13 +14,17 @@ import math
 from . import MOA_BF16, MOA_F32, _DTYPE_CODES, _stream_handle, _torch as torch
 from ._call import (Function, Packed, check_list, check_rows, ci, f32, i64, is_list, new_like, on_stream, run, sz, vp,
                     workspace as _workspace)
+from .rope import _HOW, _common
 
 _SPLIT = [i64] * 11 + [ci]
 moa_paged_attn_num_splits = Function("moa_paged_attn_num_splits", _SPLIT)
 moa_paged_attn_workspace_bytes = Function("moa_paged_attn_workspace_bytes", _SPLIT, sz)
 moa_paged_attn_fwd = Function(
     "moa_paged_attn_fwd", [vp] * 8 + [i64] * 9 + [vp] * 4 + [i64] * 3 + [f32, ci, vp, sz, ci, vp])
+moa_paged_append = Function(
+    "moa_paged_append", [vp] * 13 + [i64] * 9 + [vp] * 6 + [ci, vp, ci, f32, ci, ci, vp])
 
+_append = Packed("moa_packed_paged_append", "13q 9q 24q" + _HOW + "q")
 _attn = Packed("moa_packed_paged_attn_fwd", "8q 9q 16q 3q d 5q")
 _ws_bytes = functools.lru_cache(maxsize=1024)(moa_paged_attn_workspace_bytes)
 if torch is not None:   # the C functions above need none
@@ -59,6 +63,49 @@ def _place(k_pool, v_pool, d, B, seq_lens, new_lens, page_table, device):
     elif n[0] < B:
         raise ValueError("a cache without a page table needs a page for every sequence")
     return (n[1], n[2], n[0], max_pages, ks, vs, k_pool.data_ptr(), v_pool.data_ptr(), seq_lens.data_ptr(), new, table)
+
+
+def paged_append(q, k, v, k_pool, v_pool, seq_lens, page_table=None, new_lens=None, positions=None, inv_freq=None,
+                 q_weight=None, k_weight=None, eps=1e-6, interleaved=False, sections=None, q_out=None, stream=None):
+    """New tokens into the cache: head rows of q [B, Hq, N, d] and k [B, heads, N, d] normed with
+    ``q_weight`` and ``k_weight`` and turned by position as ``qk_norm_rope`` does (None: no norm, no
+    rotation), keys and values v [B, heads, N, d] written to their pages.  q, k, v are bf16 or fp32,
+    any views with contiguous heads; q may be None.  ``positions``: contiguous int64 [B, N], or
+    [axes, B, N] with ``sections``; None: every token's place in its sequence.  Returns the turned
+    queries, bf16 ``q_out`` (which may be a bf16 q); rows behind ``new_lens`` are left as they are
+    (in a new tensor: unset).  Raises ``MoaAttnError`` on a rejected call."""
+    if stream is not None:
+        with on_stream(stream, k):
+            return paged_append(q, k, v, k_pool, v_pool, seq_lens, page_table, new_lens, positions, inv_freq, q_weight,
+                                k_weight, eps, interleaved, sections, q_out)
+    if q is None:
+        if q_weight is not None or q_out is not None:
+            raise ValueError("q_weight and q_out go with q")
+        kn, _, ks, _, device, rot, axes, sec, wcode, (kp, _, wk, _, pos, freq) = _common(
+            k, None, positions, inv_freq, k_weight, None, sections)
+        Hq, qs, qos, qp, qop, wq = 0, ks, ks, 0, 0, 0
+    else:
+        qn, kn, qs, ks, device, rot, axes, sec, wcode, (qp, kp, wq, wk, pos, freq) = _common(
+            q, k, positions, inv_freq, q_weight, k_weight, sections)
+        Hq = qn[1]
+        if q_out is None:
+            q_out = new_like(q) if q.dtype is _bf16 else q.new_empty(qn, dtype=_bf16)
+        qos = q_out.stride()
+        if q_out.shape != qn or q_out.dtype is not _bf16 or q_out.get_device() != device or qos[3] != 1:
+            check_rows("q_out", q_out, qn, _bf16, device)
+        qop = q_out.data_ptr()
+    vs = v.stride()
+    if v.shape != kn or v.dtype is not k.dtype or v.get_device() != device or vs[-1] != 1:
+        check_rows("v", v, kn, k.dtype, device)
+    B, Hk, N, d = kn
+    heads, page, num_pages, max_pages, kps, vps, kpp, vpp, lens, new, table = _place(
+        k_pool, v_pool, d, B, seq_lens, new_lens, page_table, device)
+    if Hk != heads:
+        raise ValueError(f"k has {Hk} heads, the cache {heads}")
+    run(_append, device, qp, kp, v.data_ptr(), qop, kpp, vpp, wq, wk, pos, freq, lens, new, table, B, Hq, Hk, N, d, rot, page,
+        num_pages, max_pages, *qs, *ks, *vs, *qos, *kps, *vps, axes, *sec, interleaved, eps, _DTYPE_CODES[k.dtype], wcode,
+        _stream_handle(None, k))
+    return q_out
 
 
 def paged_attn_fwd(q, k_pool, v_pool, seq_lens, page_table=None, new_lens=None, left=-1, right=-1, sinks=0, scale=None,

@@ -94,6 +94,8 @@ class Exact:
 def close(got, want, bound, odd=None):
     """Asserts |got - want| <= bound wherever a value is expected (odd: where none is finite)."""
     got = got.double()
+    if not got.numel():
+        return
     if odd is not None:
         odd = odd.expand(got.shape)
         got, want, bound = torch.where(odd, 0.0, got), torch.where(odd, 0.0, want), torch.where(odd, 1.0, bound)
