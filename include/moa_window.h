@@ -78,6 +78,54 @@ int moa_win_attn_fwd(const void* Q, const void* K, const void* V, void* O, float
                      float scale, int out_dtype, void* workspace, size_t workspace_bytes,
                      int num_splits, void* stream);
 
+/*
+ * moa_win_attn_bwd_workspace_bytes -- device workspace of a moa_win_attn_bwd call, in
+ * bytes (0 for invalid dimensions): a sum for every query row, and, where first keys
+ * stay visible behind a window, partial sums of their gradients.
+ */
+size_t moa_win_attn_bwd_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t Nq, int64_t Nk,
+                                        int64_t d, int64_t left, int64_t right, int64_t sinks);
+
+/*
+ * moa_win_attn_bwd -- gradients of moa_win_attn_fwd.  With P the forward's weights,
+ * D_i = <dO_i, O_i> and dS_ij = P_ij (<dO_i, V_j> - D_i) over the pairs of which query i
+ * sees key j,
+ *
+ *   dQ_i = scale * sum_j dS_ij K_j
+ *   dK_j = scale * sum_i dS_ij Q_i,   dV_j = sum_i P_ij dO_i
+ *
+ * the last two over the queries of all heads that share the key/value head.
+ *
+ * Q, K, V   the forward's inputs.
+ * O, LSE    its outputs: O of storage type o_dtype (MOA_F32 or MOA_BF16), LSE required.
+ * dO        device input, bf16, [B][Hq][Nq][d].
+ * dQ, dK, dV
+ *           device outputs, bf16, written as a whole: no element written twice, the
+ *           bytes from the first to the last of each overlapping nothing else.
+ * *_strides as for the forward; here rows of all tensors are at most 2^23 elements
+ *           apart.
+ * B, Hq, Hk, Nq, Nk, d, left, right, sinks, scale
+ *           the forward's; supported besides: B * Hk * Nk < 2^26 and fewer than 2^23
+ *           workgroups of 512 threads (of 128 keys of one key/value head).
+ * workspace, workspace_bytes
+ *           at least moa_win_attn_bwd_workspace_bytes(...) bytes, 16-byte aligned,
+ *           overlapping nothing.
+ *
+ * Computation: bf16 matrix products with fp32 accumulation; P and dS enter them as one
+ * bf16 number each, one rounding at the end.  Rows and keys that do not see each
+ * other have no part in each other's gradients, whatever they hold: sums that do not
+ * come out finite are done again by the definition.  Two kernels, or three with
+ * first keys behind a window; no atomics, deterministic.
+ */
+int moa_win_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                     const float* LSE, void* dQ, void* dK, void* dV, int64_t B, int64_t Hq,
+                     int64_t Hk, int64_t Nq, int64_t Nk, int64_t d, const int64_t* q_strides,
+                     const int64_t* k_strides, const int64_t* v_strides, const int64_t* o_strides,
+                     const int64_t* do_strides, const int64_t* dq_strides,
+                     const int64_t* dk_strides, const int64_t* dv_strides, int64_t left,
+                     int64_t right, int64_t sinks, float scale, int o_dtype, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

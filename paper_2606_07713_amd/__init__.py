@@ -14,7 +14,7 @@ names here as well: ``rope`` (``include/moa_rope.h``: norms of queries and keys
 for each head with the rotation by position, and the gradients), ``kv4``
 (``include/moa_kv4.h``: a key/value cache held in four bits and the attention
 over it), ``window`` (``include/moa_window.h``: attention in a sliding window, with
-shared heads) and ``paged`` (``include/moa_paged.h``: a paged cache in bf16,
+shared heads, and the gradients) and ``paged`` (``include/moa_paged.h``: a paged cache in bf16,
 appending to it with norms and rotation, and the attention over it).
 
 There is no fallback: if the HIP library has not been built, importing this
@@ -40,6 +40,7 @@ __all__ = [
     "moa_kv4_attn_num_splits", "moa_kv4_attn_workspace_bytes",
     "kv4_cache", "kv4_write", "kv4_read", "kv4_attn_fwd",
     "moa_win_attn_fwd", "moa_win_attn_num_splits", "moa_win_attn_workspace_bytes", "win_attn_fwd",
+    "moa_win_attn_bwd", "moa_win_attn_bwd_workspace_bytes", "win_attn_bwd",
     "moa_paged_attn_fwd", "moa_paged_attn_num_splits", "moa_paged_attn_workspace_bytes",
     "moa_paged_append", "paged_cache", "paged_append", "paged_attn_fwd",
 ]
@@ -389,7 +390,8 @@ from .kv4 import (  # noqa: E402
     kv4_attn_fwd, kv4_cache, kv4_read, kv4_write, moa_kv4_attn_fwd, moa_kv4_attn_num_splits,
     moa_kv4_attn_workspace_bytes, moa_kv4_page_bytes, moa_kv4_read, moa_kv4_write)
 from .window import (  # noqa: E402
-    moa_win_attn_fwd, moa_win_attn_num_splits, moa_win_attn_workspace_bytes, win_attn_fwd)
+    moa_win_attn_bwd, moa_win_attn_bwd_workspace_bytes, moa_win_attn_fwd, moa_win_attn_num_splits,
+    moa_win_attn_workspace_bytes, win_attn_bwd, win_attn_fwd)
 from .paged import (  # noqa: E402
     moa_paged_append, moa_paged_attn_fwd, moa_paged_attn_num_splits, moa_paged_attn_workspace_bytes, paged_append,
     paged_attn_fwd, paged_cache)

@@ -21,7 +21,7 @@ ARCH = "gfx950"
 SOURCES = ["api.cpp", "prefill_bf16.hip", "prefill_bf16_indep.hip", "prefill_f32.hip", "prefill_f32_mfma.hip", "decode.hip",
            "combine.hip", "bwd.hip", "proj.hip", "noalloc.hip", "prefill_gather.hip",
            "api_rope.cpp", "rope.hip", "api_kv4.cpp", "kv4.hip", "kv4_attn.hip",
-           "api_window.cpp", "win_few.hip", "win_fwd.hip", "api_paged.cpp", "paged.hip"]
+           "api_window.cpp", "win_few.hip", "win_fwd.hip", "win_bwd.hip", "api_paged.cpp", "paged.hip"]
 
 # Packed fp32 instructions are disabled for all device code on purpose.
 COMMON_FLAGS = [

@@ -15,6 +15,7 @@ namespace {
 using namespace moa;
 
 constexpr int64_t kMaxRows = int64_t(1) << 26;  // B * Hq * N: four rows a workgroup when splits are joined
+constexpr int64_t kMaxStageStride = int64_t(1) << 23;   // 64 rows' bytes stay in 32 bits
 constexpr int kMaxSplits = 256;
 constexpr float kMaxScale = 0x1p127f;           // times log2(e) is still finite
 // Workgroups of 256 threads in one launch: its threads are counted in 32 bits.
@@ -133,6 +134,37 @@ int run(const Call& c, const Sizes& s, const KeySource& src, const Buf* keys, in
     return hip_status(launch_win_attn(p, static_cast<hipStream_t>(c.stream)));
 }
 
+// Chunks of the queries that see only the first keys of a sequence, 0 if there are
+// none: so many that one is about as long as what the windows reach, and at most 64
+// over all tiles of such keys.
+int far_chunks(const Sizes& s) {
+    if (s.left < 0 || !s.any() || s.Nk == 0) return 0;
+    const int tiles = win_sink_tiles(window_of(s), (int)s.Nk);
+    if (tiles == 0) return 0;
+    // the first tile's windows end here
+    const int64_t near = std::clamp<int64_t>(std::min<int64_t>(kWinKeyTile, s.Nk) - (s.Nk - s.N) + s.left, 0, s.N);
+    const int64_t behind = (s.N - near + kWinStage - 1) / kWinStage;
+    if (behind == 0) return 0;
+    const int64_t reach = (std::min(s.left + std::max<int64_t>(s.right, 0), s.N) + kWinKeyTile) / kWinStage + 1;
+    return (int)std::clamp<int64_t>((behind + reach - 1) / reach, 1, std::max(1, 64 / tiles));
+}
+
+size_t far_bytes(const Sizes& s, int chunks) {
+    if (!chunks) return 0;
+    return (size_t)(s.B * s.Hk) * (size_t)win_sink_tiles(window_of(s), (int)s.Nk) * (size_t)(chunks + 1) * 2 * kWinKeyTile * (size_t)s.d * 4;
+}
+
+// Sizes of a gradient call.
+int check_bwd(const Sizes& s) {
+    int st = check_sizes(s, 0);
+    if (st) return st;
+    if (s.B * s.Hk > 0 && s.Nk >= (kMaxRows + s.B * s.Hk - 1) / (s.B * s.Hk)) return MOA_ERR_UNSUPPORTED;
+    const int64_t tiles = (s.Nk + kWinKeyTile - 1) / kWinKeyTile;
+    const int64_t more = s.left < 0 ? 0 : 64 + tiles;   // chunks, of one tile or of many with one each
+    if (s.B * s.Hk * (tiles + more) > kMaxBlocks / 2) return MOA_ERR_UNSUPPORTED;   // of 512 threads
+    return MOA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -177,6 +209,70 @@ int moa_win_attn_fwd(const void* Q, const void* K, const void* V, void* O, float
     src.max_pages = 1;
     const Buf keys[] = {{K, extent_bytes(sk, B, Hk, Nk, d, 2)}, {V, extent_bytes(sv, B, Hk, Nk, d, 2)}};
     return run(c, s, src, keys, 2);
+}
+
+size_t moa_win_attn_bwd_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t Nq, int64_t Nk,
+                                        int64_t d, int64_t left, int64_t right, int64_t sinks) {
+    const Sizes s{B, Hq, Hk, Nq, Nk, d, left, right, sinks};
+    return check_bwd(s) ? 0 : align256((size_t)(B * Hq * Nq) * 4) + far_bytes(s, far_chunks(s));
+}
+
+int moa_win_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                     const float* LSE, void* dQ, void* dK, void* dV, int64_t B, int64_t Hq,
+                     int64_t Hk, int64_t Nq, int64_t Nk, int64_t d, const int64_t* q_strides,
+                     const int64_t* k_strides, const int64_t* v_strides, const int64_t* o_strides,
+                     const int64_t* do_strides, const int64_t* dq_strides,
+                     const int64_t* dk_strides, const int64_t* dv_strides, int64_t left,
+                     int64_t right, int64_t sinks, float scale, int o_dtype, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+    const Sizes s{B, Hq, Hk, Nq, Nk, d, left, right, sinks};
+    if (o_dtype != MOA_F32 && o_dtype != MOA_BF16) return MOA_ERR_INVALID_ARG;
+    if (!std::isfinite(scale)) return MOA_ERR_INVALID_ARG;
+    int st = check_bwd(s);
+    if (st) return st;
+    if (std::fabs(scale) > kMaxScale) return MOA_ERR_UNSUPPORTED;
+    struct Tensor {
+        const void* p;
+        const int64_t* strides;
+        int64_t H, N;
+        size_t es;
+        bool out;
+        Strides s;
+    } t[] = {{Q, q_strides, Hq, Nq, 2, false, {}}, {K, k_strides, Hk, Nk, 2, false, {}}, {V, v_strides, Hk, Nk, 2, false, {}},
+             {O, o_strides, Hq, Nq, o_dtype == MOA_F32 ? size_t(4) : size_t(2), false, {}}, {dO, do_strides, Hq, Nq, 2, false, {}},
+             {dQ, dq_strides, Hq, Nq, 2, true, {}}, {dK, dk_strides, Hk, Nk, 2, true, {}}, {dV, dv_strides, Hk, Nk, 2, true, {}}};
+    for (Tensor& x : t) {
+        x.s = strides_of(x.strides, B, x.H, x.N, d);
+        if ((st = check_tensor(x.p, x.s, B, x.H, x.N, d, x.es, x.out))) return st;
+        if (x.s.r > kMaxStageStride) return MOA_ERR_UNSUPPORTED;
+    }
+    if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(LSE) & 3)) return MOA_ERR_INVALID_ARG;
+    if (s.any() && !LSE) return MOA_ERR_INVALID_ARG;
+    if (B == 0 || (!s.any() && Nk == 0)) return MOA_OK;
+    const size_t stats = (size_t)(B * Hq * Nq) * 4;
+    const int chunks = far_chunks(s);
+    const size_t need = align256(stats) + far_bytes(s, chunks);
+    if (need && (!workspace || workspace_bytes < need)) return MOA_ERR_WORKSPACE;
+    Buf all[10];
+    for (int i = 0; i < 8; ++i) all[i] = {t[i].p, extent_bytes(t[i].s, B, t[i].H, t[i].N, d, t[i].es)};
+    all[8] = {LSE, stats};
+    all[9] = {workspace, need};
+    for (int i : {5, 6, 7, 9})
+        for (int k = 0; k < 10; ++k)
+            if (k != i && meet(all[i], all[k])) return MOA_ERR_INVALID_ARG;
+    WinGrad p{};
+    p.w = window_of(s);
+    p.q = Q; p.k = K; p.v = V; p.o = O; p.dout = dO; p.lse = LSE;
+    p.dq = dQ; p.dk = dK; p.dv = dV;
+    put(p.qs, t[0].s); put(p.ks, t[1].s); put(p.vs, t[2].s); put(p.os, t[3].s); put(p.gs, t[4].s);
+    put(p.dqs, t[5].s); put(p.dks, t[6].s); put(p.dvs, t[7].s);
+    p.B = (int)B; p.hq = (int)Hq; p.hk = (int)Hk; p.nq = (int)Nq; p.nk = (int)Nk; p.d = (int)d;
+    p.scale = scale;
+    p.o_bf16 = o_dtype == MOA_BF16;
+    p.dsum = static_cast<float*>(workspace);
+    p.part = chunks ? reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(stats)) : nullptr;
+    p.chunks = chunks;
+    return hip_status(launch_win_bwd(p, static_cast<hipStream_t>(stream)));
 }
 
 int moa_paged_attn_num_splits(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d, int64_t page,
@@ -232,6 +328,13 @@ int moa_packed_win_attn_fwd(const int64_t* a) {
     return moa_win_attn_fwd(Ptr{a[0]}, Ptr{a[1]}, Ptr{a[2]}, Ptr{a[3]}, Ptr{a[4]}, a[5], a[6], a[7], a[8], a[9], a[10],
                             a + 11, a + 15, a + 19, a + 23, a[27], a[28], a[29], packed::real(a[30]), (int)a[31], Ptr{a[32]},
                             (size_t)a[33], (int)a[34], Ptr{a[35]});
+}
+
+int moa_packed_win_attn_bwd(const int64_t* a) {
+    using packed::Ptr;
+    return moa_win_attn_bwd(Ptr{a[0]}, Ptr{a[1]}, Ptr{a[2]}, Ptr{a[3]}, Ptr{a[4]}, Ptr{a[5]}, Ptr{a[6]}, Ptr{a[7]}, Ptr{a[8]},
+                            a[9], a[10], a[11], a[12], a[13], a[14], a + 15, a + 19, a + 23, a + 27, a + 31, a + 35, a + 39,
+                            a + 43, a[47], a[48], a[49], packed::real(a[50]), (int)a[51], Ptr{a[52]}, (size_t)a[53], Ptr{a[54]});
 }
 
 int moa_packed_paged_attn_fwd(const int64_t* a) {

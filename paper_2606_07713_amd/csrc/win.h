@@ -67,6 +67,15 @@ struct WinGrad {
     int chunks;                // of the queries behind the first keys' windows
 };
 
+// Keys of a workgroup of the dK, dV kernel, and queries of one of its stages.
+constexpr int kWinKeyTile = 128, kWinStage = 64;
+
+// Key tiles that hold first keys which stay visible behind the window.
+inline int win_sink_tiles(const Window& w, int nk) {
+    const int sinks = w.sinks < nk ? w.sinks : nk;
+    return w.left == kNoLimit ? 0 : (sinks + kWinKeyTile - 1) / kWinKeyTile;
+}
+
 hipError_t launch_win_bwd(const WinGrad& p, hipStream_t stream);
 
 }  // namespace moa

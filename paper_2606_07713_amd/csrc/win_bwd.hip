@@ -1,0 +1,637 @@
+// Gradients of the attention with a window (moa_window.h) on gfx950 matrix cores,
+// the weights recomputed from the forward's LSE.
+//
+// With s = <q_i, k_j>, c = scale * log2(e) and lse2_i = LSE_i * log2(e), over the pairs
+// of which query i sees key j:
+//   P_ij  = 2^(s_ij c - lse2_i),   dP_ij = <dO_i, v_j>,   D_i = <dO_i, O_i>
+//   dS_ij = P_ij (dP_ij - D_i)
+//   dQ_i  = scale * sum_j dS_ij k_j
+//   dK_j  = scale * sum_i dS_ij q_i,   dV_j = sum_i P_ij dO_i     (i over the queries of
+//           all heads that share the key/value head)
+//
+// * win_dq: one workgroup = 4 waves x 32 rows of one key/value head, a row being a
+//   query and one of the G = Hq/Hk heads that share it; K and V tiles of 64 keys
+//   stream through LDS as in the forward, only those that a row sees.  D_i of its
+//   rows comes first, for the other kernel too.
+// * win_dkdv: one workgroup = 128 keys; Q and dO of the queries that see one of them
+//   stream through LDS, 64 queries of one head at a time, head after head, so that
+//   shared heads meet in the same sums.  A pair of waves on one SIMD owns 32 keys:
+//   one forms S and P and sums dV, the other forms dP and dS with the partner's P and
+//   sums dK, one stage behind.
+// * The first keys stay visible to all later queries, so their sums would be as long
+//   as the sequence where all others are as long as the window.  The queries behind
+//   their windows are cut into chunks with workgroups of their own, which leave fp32
+//   sums that win_join adds in a fixed order.
+// No atomics; deterministic.  P and dS are rounded to bf16 for the matrix products.
+// Rows whose sums do not come out finite are done again by the definition.
+#include <algorithm>
+#include <type_traits>
+
+#include "prefill_bf16_common.h"
+#include "stage_common.h"
+#include "win_common.h"
+
+namespace moa {
+namespace {
+
+using namespace win;
+using pf::BN;
+using pf::Cfg;
+using pf::dv_of;
+using pf::pack16;
+using pf::stage_rows;
+using pf::stage_tr;
+using pf::swz;
+using pf::TileAddr;
+
+// Element offset of row i of head hh of sequence b.
+__device__ __forceinline__ long long at_row(const long long (&s)[3], int b, int hh, int i) {
+    return b * s[0] + hh * s[1] + i * s[2];
+}
+
+__device__ __forceinline__ Seen seen_by(const WinGrad& p, int i) {
+    return seen_from(p.w, (long long)i + p.nk - p.nq, p.nk);
+}
+
+// What of a row's gradient one pair gives: P and dS.
+template <int D>
+__device__ __forceinline__ void pair_by_definition(const u16* q, const u16* k, const u16* g, const u16* v, double c, float lse2,
+                                                   float dsum, float& w, float& ds) {
+    double s = 0.0, t = 0.0;
+    for (int e = 0; e < D; e += 2) {
+        const auto two = [&](const u16* x) { return *reinterpret_cast<const uint32_t*>(x + e); };
+        const uint32_t a = two(q), y = two(k), m = two(g), z = two(v);
+        s += (double)bf16lo_to_f32(a) * (double)bf16lo_to_f32(y) + (double)bf16hi_to_f32(a) * (double)bf16hi_to_f32(y);
+        t += (double)bf16lo_to_f32(m) * (double)bf16lo_to_f32(z) + (double)bf16hi_to_f32(m) * (double)bf16hi_to_f32(z);
+    }
+    w = (float)exp2(s * c - (double)lse2);
+    ds = w * (float)(t - (double)dsum);
+}
+
+// Adds w * row to o, this lane's D/64 elements.
+template <int D>
+__device__ __forceinline__ void add_row(float (&o)[D / 64], float w, const u16* row) {
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(w, __uint_as_float((uint32_t)row[E * lane + e] << 16), o[e]);
+}
+
+template <int D>
+__device__ __forceinline__ void store_lane(u16* to, const float (&o)[D / 64], float mul) {
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int e = 0; e < E; ++e) reinterpret_cast<__bf16*>(to)[E * lane + e] = (__bf16)(o[e] * mul);
+}
+
+// A lane's row of D elements from an accumulator in the transposed layout.
+template <int D>
+__device__ __forceinline__ void store_row16(u16* to, int half, const f32x16 (&acc)[D / 32], float mul) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<uint2*>(to + dv_of<D>(d, g * 8 + half * 4)) =
+                make_uint2(pack2(acc[d][g * 4 + 0] * mul, acc[d][g * 4 + 1] * mul), pack2(acc[d][g * 4 + 2] * mul, acc[d][g * 4 + 3] * mul));
+}
+template <int D>
+__device__ __forceinline__ void store_row16(float* to, int half, const f32x16 (&acc)[D / 32], float mul) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<float4*>(to + dv_of<D>(d, g * 8 + half * 4)) =
+                make_float4(acc[d][g * 4 + 0] * mul, acc[d][g * 4 + 1] * mul, acc[d][g * 4 + 2] * mul, acc[d][g * 4 + 3] * mul);
+}
+
+// Whether a lane's row has an element that is not finite (the two halves of a row
+// are lanes l and l ^ 32).
+template <int D>
+__device__ __forceinline__ bool not_finite(const f32x16 (&acc)[D / 32]) {
+    float zero = 0.0f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(acc[d][i], 0.0f, zero);
+    return !(half_sum(zero) == 0.0f);
+}
+
+// ---- dQ ----------------------------------------------------------------------
+
+constexpr int QW = 4;            // waves
+constexpr int QROWS = QW * 32;   // rows per workgroup
+
+template <int D>
+__global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, int row_tiles) {
+    using C = Cfg<D>;
+    constexpr uint32_t RB = C::ROW_BYTES;
+    constexpr int LPW = C::TILE_BYTES / (QW * 1024);
+    __shared__ __attribute__((aligned(1024))) unsigned char k_st0[C::TILE_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char k_st1[C::TILE_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_st0[C::TILE_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_st1[C::TILE_BYTES];
+    using S0 = std::integral_constant<int, 0>;
+    using S1 = std::integral_constant<int, 1>;
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int G = p.hq / p.hk, groups = p.B * p.hk, rt = row_tiles - 1 - blockIdx.x / groups;
+    const int bh = blockIdx.x % groups, b = bh / p.hk, h = bh - b * p.hk;
+    const int rows = p.nq * G, row0 = rt * QROWS;
+    const auto uniform = [](Seen s) {
+        return Seen{__builtin_amdgcn_readfirstlane(s.lo), __builtin_amdgcn_readfirstlane(s.hi)};
+    };
+    const Tiles<BN> tiles(uniform(seen_by(p, row0 / G)), uniform(seen_by(p, (min(row0 + QROWS, rows) - 1) / G)), p.w.sinks);
+
+    // This wave's rows; this lane's row, its Q and dO fragments, LSE and D.
+    const int w0 = row0 + wave * 32, row = w0 + col;
+    const bool live = w0 < rows, in = row < rows;
+    const Seen wl = uniform(seen_by(p, min(w0, rows - 1) / G)), wh = uniform(seen_by(p, (min(w0 + 32, rows) - 1) / G));
+    const int qi = min(row, rows - 1) / G, hh = h * G + min(row, rows - 1) - qi * G;
+    const Seen seen = seen_by(p, qi);
+    const u16* qr = static_cast<const u16*>(p.q) + at_row(p.qs, b, hh, qi);
+    const u16* gr = static_cast<const u16*>(p.dout) + at_row(p.gs, b, hh, qi);
+    bf16x8 qf[D / 16], gf[D / 16];
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+        u32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+        if (in) {
+            x = *reinterpret_cast<const u32x4*>(qr + 16 * s + 8 * half);
+            y = *reinterpret_cast<const u32x4*>(gr + 16 * s + 8 * half);
+        }
+        qf[s] = __builtin_bit_cast(bf16x8, x);
+        gf[s] = __builtin_bit_cast(bf16x8, y);
+    }
+    const size_t stat = ((size_t)b * p.hq + hh) * p.nq + qi;
+    float lse2 = in ? p.lse[stat] * kLog2e : 0.0f;
+    if (lse2 == kNegInf) lse2 = 0.0f;   // a row that sees nothing: all its weights are masked
+    float dsum = 0.0f;
+    if (in) {
+        const long long o0 = at_row(p.os, b, hh, qi) + 8 * half;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            float o[8];
+            if (p.o_bf16) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const u16*>(p.o) + o0 + 16 * s);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { o[2 * j] = bf16lo_to_f32(x[j]); o[2 * j + 1] = bf16hi_to_f32(x[j]); }
+            } else {
+                const f32x4* x = reinterpret_cast<const f32x4*>(static_cast<const float*>(p.o) + o0 + 16 * s);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { o[j] = x[0][j]; o[4 + j] = x[1][j]; }
+            }
+            const u32x4 y = __builtin_bit_cast(u32x4, gf[s]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                dsum = __builtin_fmaf(bf16lo_to_f32(y[j]), o[2 * j], dsum);
+                dsum = __builtin_fmaf(bf16hi_to_f32(y[j]), o[2 * j + 1], dsum);
+            }
+        }
+    }
+    dsum = half_sum(dsum);
+    if (in && half == 0) p.dsum[stat] = dsum;
+
+    const u16* Kh = static_cast<const u16*>(p.k) + at_row(p.ks, b, h, 0);
+    const u16* Vh = static_cast<const u16*>(p.v) + at_row(p.vs, b, h, 0);
+    const uint32_t krb = (uint32_t)p.ks[2] * 2u, vrb = (uint32_t)p.vs[2] * 2u;
+    uint32_t koff[LPW], voff[LPW];
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+        const int slot = (wave * LPW + i) * 64 + lane, r = slot / C::CHUNKS, ch = slot % C::CHUNKS;
+        const uint32_t chunk = (uint32_t)((ch ^ swz<D>(r)) * 16);
+        koff[i] = (uint32_t)(r & 15) * krb + chunk;   // this wave's 16 rows of the tile
+        voff[i] = (uint32_t)(r & 15) * vrb + chunk;
+    }
+    auto issue = [&](int v, auto stage) __attribute__((always_inline)) {
+        unsigned char* ks = decltype(stage)::value == 0 ? k_st0 : k_st1;
+        unsigned char* vs = decltype(stage)::value == 0 ? v_st0 : v_st1;
+        const int key = tiles.at(v) * BN + 16 * wave, n = max(0, min(16, p.nk - key));
+        const auto rk = make_rsrc(Kh + (n ? key * p.ks[2] : 0), rows_extent(n, krb, RB));
+        const auto rv = make_rsrc(Vh + (n ? key * p.vs[2] : 0), rows_extent(n, vrb, RB));
+#pragma unroll
+        for (int j = 0; j < LPW; ++j) buffer_load16_to_lds(rk, ks + (wave * LPW + j) * 1024, koff[j]);
+#pragma unroll
+        for (int j = 0; j < LPW; ++j) buffer_load16_to_lds(rv, vs + (wave * LPW + j) * 1024, voff[j]);
+    };
+    const TileAddr<D> ta(lane);
+    f32x16 acc[D / 32];
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
+    auto tile = [&](int v, auto stage) __attribute__((always_inline)) {
+        const unsigned char* ks = decltype(stage)::value == 0 ? k_st0 : k_st1;
+        const unsigned char* vs = decltype(stage)::value == 0 ? v_st0 : v_st1;
+        const int k0 = tiles.at(v) * BN;
+        if (!live || k0 >= wh.hi || (k0 + BN <= wl.lo && k0 >= p.w.sinks)) return;
+        const bool need_mask = k0 + BN > wl.hi || (k0 < wh.lo && k0 + BN > p.w.sinks);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_rows<D>(ks, ta, u, k), qf[k], s, 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_rows<D>(vs, ta, u, k), gf[k], dp, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], c, -lse2);
+            if (need_mask) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!sees(seen, p.w.sinks, k0 + 32 * u + (i >> 2) * 8 + half * 4 + (i & 3))) s[i] = kNegInf;
+            }
+            float ds[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ds[i] = exp2_hw(s[i]) * (dp[i] - dsum);
+            bf16x8 dsb[2];
+            pack16(ds, dsb);
+#pragma unroll
+            for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_tr<D>(ks, ta, d, 2 * u + c2), dsb[c2], acc[d], 0, 0, 0);
+        }
+    };
+    if (tiles.count > 0) {
+        issue(0, S0{});
+        for (int v = 0; v < tiles.count; v += 2) {
+            pf::wait_vmcnt<0>();
+            __syncthreads();
+            if (v + 1 < tiles.count) issue(v + 1, S1{});
+            tile(v, S0{});
+            if (v + 1 >= tiles.count) break;
+            pf::wait_vmcnt<0>();
+            __syncthreads();
+            if (v + 2 < tiles.count) issue(v + 2, S0{});
+            tile(v + 1, S1{});
+        }
+    }
+    if (!live) return;
+    const bool odd = not_finite<D>(acc) && in;
+    if (in) store_row16<D>(static_cast<u16*>(p.dq) + at_row(p.dqs, b, hh, qi), half, acc, p.scale);
+    for (uint32_t left = (uint32_t)__ballot(odd); left; left &= left - 1) {
+        const int r = __builtin_ctz(left), i = (w0 + r) / G, head = h * G + (w0 + r) - i * G;
+        const Seen see = seen_by(p, i);
+        const u16* q = static_cast<const u16*>(p.q) + at_row(p.qs, b, head, i);
+        const u16* g = static_cast<const u16*>(p.dout) + at_row(p.gs, b, head, i);
+        const float l = __shfl(lse2, r), dd = __shfl(dsum, r);
+        float o[D / 64] = {};
+        for (int v = 0; v < tiles.count; ++v) {
+            const int key = tiles.at(v) * BN + lane;
+            const bool mine = sees(see, p.w.sinks, key);
+            float w = 0.0f, ds = 0.0f;
+            if (mine) pair_by_definition<D>(q, Kh + key * p.ks[2], g, Vh + key * p.vs[2], (double)p.scale * 1.4426950408889634, l, dd, w, ds);
+            const uint64_t all = __ballot(mine);
+            for (int j = 0; j < 64; ++j)
+                if ((all >> j) & 1) add_row<D>(o, __shfl(ds, j), Kh + (long long)(key - lane + j) * p.ks[2]);
+        }
+        store_lane<D>(static_cast<u16*>(p.dq) + at_row(p.dqs, b, head, i), o, p.scale);
+    }
+}
+
+// ---- dK, dV ------------------------------------------------------------------
+
+constexpr int KW = 8;       // waves
+constexpr int KT = kWinKeyTile;   // keys per workgroup
+constexpr int SR = kWinStage;     // queries per stage
+
+// The queries that see a key: lo .. hi.
+struct Span {
+    int lo, hi;
+};
+__device__ __forceinline__ Span seen_of_key(const WinGrad& p, int key) {
+    const long long off = (long long)p.nk - p.nq;
+    Span s;
+    s.lo = p.w.right == kNoLimit ? 0 : (int)max(0ll, min((long long)p.nq, key - off - p.w.right));
+    s.hi = p.w.left == kNoLimit || key < p.w.sinks ? p.nq - 1 : (int)max(-1ll, min((long long)p.nq - 1, key - off + p.w.left));
+    return s;
+}
+
+// The stages of one workgroup: `count` of the list that has, head after head, the
+// stages first .. first + each - 1.
+struct Stages {
+    int first, each, begin, count;
+};
+
+template <int D>
+__global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c, int key_tiles, int sink_tiles) {
+    using C = Cfg<D>;
+    constexpr uint32_t RB = C::ROW_BYTES;
+    constexpr int U = SR / 32;                             // steps per stage
+    constexpr int LPS = SR * C::ROW_BYTES / (KW * 1024);   // 16-byte loads per lane per stage of Q or dO
+    // One array per ring slot: the compiler tracks direct-to-LDS loads per object.
+    __shared__ __attribute__((aligned(1024))) unsigned char q_0[SR * C::ROW_BYTES], q_1[SR * C::ROW_BYTES], q_2[SR * C::ROW_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char g_0[SR * C::ROW_BYTES], g_1[SR * C::ROW_BYTES], g_2[SR * C::ROW_BYTES];
+    // Exchanged weights: [stage parity][pair][step][chunk][lane].
+    __shared__ __attribute__((aligned(1024))) uint4 p_x[2][4][U][2][64];
+    __shared__ __attribute__((aligned(16))) float l_r[3][2][SR];   // [slot][lse2, D][query]
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int role = wave >> 2, pair = wave & 3;   // role 0: P and dV; role 1: dS and dK
+    const int col = lane & 31, half = lane >> 5;
+    const int G = p.hq / p.hk, groups = p.B * p.hk;
+    const int bh = blockIdx.x % groups, b = bh / p.hk, h = bh - b * p.hk;
+    // Items of a head: the chunks of the far queries of the first keys' tiles, then
+    // every tile with the queries whose windows reach it.
+    const int item = blockIdx.x / groups, far_items = sink_tiles * p.chunks;
+    const bool far = item < far_items;
+    const int kt = far ? item / p.chunks : item - far_items, chunk = far ? item % p.chunks : -1;
+    const int k0 = kt * KT, k1 = min(k0 + KT, p.nk) - 1;
+    const bool partial = kt < sink_tiles && p.chunks > 0;
+
+    Stages st;
+    {
+        // Windows alone decide of the near queries where the far ones have chunks.
+        const long long off = (long long)p.nk - p.nq;
+        const int lo = seen_of_key(p, k0).lo;
+        int hi = seen_of_key(p, k1).hi;
+        const int near_hi = (int)max(-1ll, min((long long)p.nq - 1, k1 - off + (long long)p.w.left));
+        if (k0 < p.w.sinks) hi = partial ? near_hi : p.nq - 1;
+        int first = lo / SR, end = hi < lo ? first : hi / SR + 1;
+        if (far) {
+            first = max(lo / SR, (near_hi + SR) / SR);   // the stage behind near_hi's
+            end = max(first, (p.nq + SR - 1) / SR);
+        }
+        st.first = first;
+        st.each = end - first;
+        const int all = st.each * G, per = far ? (all + p.chunks - 1) / p.chunks : all;
+        st.begin = far ? min(all, chunk * per) : 0;
+        st.count = min(per, all - st.begin);
+    }
+    const int n_stages = st.count;
+
+    const int w0 = k0 + pair * 32, key = w0 + col;   // this pair's keys, this lane's
+    const Span mine = seen_of_key(p, min(key, p.nk - 1));
+    // Queries that a key of the pair's is seen by, and those that see all of them.
+    // (the first key behind the sinks has the earliest end)
+    const Span wa = seen_of_key(p, min(w0, p.nk - 1)), wb = seen_of_key(p, min(w0 + 31, p.nk - 1));
+    const Span wc = seen_of_key(p, min(min(max(w0, p.w.sinks), w0 + 31), p.nk - 1));
+    const int some_lo = __builtin_amdgcn_readfirstlane(wa.lo), all_lo = __builtin_amdgcn_readfirstlane(wb.lo);
+    const int some_hi = __builtin_amdgcn_readfirstlane(max(wa.hi, wb.hi));
+    const int all_hi = __builtin_amdgcn_readfirstlane(min(wa.hi, wc.hi));
+    const bool live = w0 < p.nk;
+
+    const uint32_t qrb = (uint32_t)p.qs[2] * 2u, grb = (uint32_t)p.gs[2] * 2u;
+    uint32_t qoff[LPS], goff[LPS];
+#pragma unroll
+    for (int i = 0; i < LPS; ++i) {
+        const int slot = (wave * LPS + i) * 64 + lane, r = slot / C::CHUNKS, ch = slot % C::CHUNKS;
+        const uint32_t at = (uint32_t)((ch ^ swz<D>(r)) * 16);
+        qoff[i] = (uint32_t)r * qrb + at;
+        goff[i] = (uint32_t)r * grb + at;
+    }
+    const TileAddr<D> ta(lane);
+
+    // K (role 0) or V (role 1) of this lane's key: B operands.
+    bf16x8 kvf[D / 16];
+    {
+        const u16* src = role == 0 ? static_cast<const u16*>(p.k) + at_row(p.ks, b, h, 0) + key * p.ks[2]
+                                   : static_cast<const u16*>(p.v) + at_row(p.vs, b, h, 0) + key * p.vs[2];
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            u32x4 x = {0, 0, 0, 0};
+            if (key < p.nk) x = *reinterpret_cast<const u32x4*>(src + 16 * s + 8 * half);
+            kvf[s] = __builtin_bit_cast(bf16x8, x);
+        }
+    }
+    f32x16 acc[D / 32];     // dV^T (role 0) or dK^T (role 1)
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
+
+    // Whether the pair has anything to do in the 32 queries from q0 on.
+    const auto wanted = [&](int q0) { return live && q0 <= some_hi && q0 + 31 >= some_lo; };
+
+    auto step_a = [&](const unsigned char* qs, const unsigned char* gs, const float* ls, uint4* px, int u, int q0)
+                      __attribute__((always_inline)) {
+        f32x16 s = f32x16{};
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_rows<D>(qs, ta, u, k), kvf[k], s, 0, 0, 0);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4 l4 = *reinterpret_cast<const float4*>(ls + 32 * u + 8 * g + 4 * half);
+            const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[4 * g + r] = __builtin_fmaf(s[4 * g + r], c, -lv[r]);
+        }
+        if (q0 < all_lo || q0 + 31 > all_hi) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int qi = q0 + (i >> 2) * 8 + 4 * half + (i & 3);
+                if (qi < mine.lo || qi > mine.hi) s[i] = kNegInf;
+            }
+        }
+        float w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = exp2_hw(s[i]);
+        bf16x8 pb[2];
+        pack16(w, pb);
+#pragma unroll
+        for (int c2 = 0; c2 < 2; ++c2) px[c2 * 64 + lane] = __builtin_bit_cast(uint4, pb[c2]);
+#pragma unroll
+        for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_tr<D>(gs, ta, d, 2 * u + c2), pb[c2], acc[d], 0, 0, 0);
+    };
+    auto step_b = [&](const unsigned char* qs, const unsigned char* gs, const float* dv, const uint4* px, int u)
+                      __attribute__((always_inline)) {
+        f32x16 dp = f32x16{};
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_rows<D>(gs, ta, u, k), kvf[k], dp, 0, 0, 0);
+        const uint4 x0 = px[lane], x1 = px[64 + lane];
+        const uint32_t pw[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+        float ds[16];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4 d4 = *reinterpret_cast<const float4*>(dv + 32 * u + 8 * g + 4 * half);
+            const float dd[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 4 * g + r;
+                ds[i] = ((i & 1) ? bf16hi_to_f32(pw[i >> 1]) : bf16lo_to_f32(pw[i >> 1])) * (dp[i] - dd[r]);
+            }
+        }
+        bf16x8 dsb[2];
+        pack16(ds, dsb);
+#pragma unroll
+        for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_tr<D>(qs, ta, d, 2 * u + c2), dsb[c2], acc[d], 0, 0, 0);
+    };
+
+    // The list's stages one after the other: head `hh`, stage `at`.
+    struct Cursor {
+        int hh, at;
+    };
+    const auto start = [&]() {
+        const int g = st.each ? st.begin / st.each : 0;
+        return Cursor{h * G + g, st.first + st.begin - g * st.each};
+    };
+    const auto next = [&](Cursor& x) {
+        if (++x.at == st.first + st.each) {
+            x.at = st.first;
+            ++x.hh;
+        }
+    };
+    Cursor load = start(), work = load;
+    float sx = 0.0f;
+    auto issue = [&](unsigned char* qd, unsigned char* gd) __attribute__((always_inline)) {
+        const int q0 = load.at * SR, n = min(SR, p.nq - q0);
+        const auto rq = make_rsrc(static_cast<const u16*>(p.q) + at_row(p.qs, b, load.hh, q0), rows_extent(n, qrb, RB));
+        const auto rg = make_rsrc(static_cast<const u16*>(p.dout) + at_row(p.gs, b, load.hh, q0), rows_extent(n, grb, RB));
+#pragma unroll
+        for (int i = 0; i < LPS; ++i) buffer_load16_to_lds(rq, qd + (wave * LPS + i) * 1024, qoff[i]);
+#pragma unroll
+        for (int i = 0; i < LPS; ++i) buffer_load16_to_lds(rg, gd + (wave * LPS + i) * 1024, goff[i]);
+        // LSE and D of the stage's queries: one of each wave pair's, a query a lane.
+        sx = 0.0f;
+        if (pair == 0 && q0 + lane < p.nq) {
+            const size_t stat = ((size_t)b * p.hq + load.hh) * p.nq + q0 + lane;
+            sx = role == 0 ? p.lse[stat] * kLog2e : p.dsum[stat];
+        }
+        next(load);
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2>;
+    const auto q_slot = [&](auto s) -> unsigned char* { return decltype(s)::value == 0 ? q_0 : decltype(s)::value == 1 ? q_1 : q_2; };
+    const auto g_slot = [&](auto s) -> unsigned char* { return decltype(s)::value == 0 ? g_0 : decltype(s)::value == 1 ? g_1 : g_2; };
+    // Iteration j: stage j is in slot j % 3 after the barrier.  Role 0 works on it,
+    // role 1 on the one before, whose weights role 0 wrote in iteration j - 1; the
+    // loads of stage j + 1 start into the slot whose last reader is done.
+    auto advance = [&](int j, auto slot, auto after) __attribute__((always_inline)) {
+        if (j < n_stages && pair == 0) l_r[decltype(slot)::value][role][lane] = sx;
+        pf::wait_vmcnt<0>();
+        pf::wait_lgkmcnt0();
+        pf::barrier_no_fence();
+        if (j + 1 < n_stages) issue(q_slot(after), g_slot(after));
+    };
+    auto iteration_a = [&](int j, auto slot, auto after) __attribute__((always_inline)) {
+        advance(j, slot, after);
+        if (j >= n_stages) return;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (wanted(work.at * SR + 32 * u))
+                step_a(q_slot(slot), g_slot(slot), l_r[decltype(slot)::value][0], &p_x[j & 1][pair][u][0][0], u, work.at * SR + 32 * u);
+        next(work);
+    };
+    auto iteration_b = [&](int j, auto slot, auto after, auto before) __attribute__((always_inline)) {
+        advance(j, slot, after);
+        if (j == 0) return;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (wanted(work.at * SR + 32 * u))
+                step_b(q_slot(before), g_slot(before), l_r[decltype(before)::value][1], &p_x[(j - 1) & 1][pair][u][0][0], u);
+        next(work);
+    };
+    if (n_stages > 0) {
+        issue(q_0, g_0);
+        if (role == 0) {
+            for (int j = 0; j <= n_stages; j += 3) {
+                iteration_a(j, I0{}, I1{});
+                if (j + 1 > n_stages) break;
+                iteration_a(j + 1, I1{}, I2{});
+                if (j + 2 > n_stages) break;
+                iteration_a(j + 2, I2{}, I0{});
+            }
+        } else {
+            for (int j = 0; j <= n_stages; j += 3) {
+                iteration_b(j, I0{}, I1{}, I2{});
+                if (j + 1 > n_stages) break;
+                iteration_b(j + 1, I1{}, I2{}, I0{});
+                if (j + 2 > n_stages) break;
+                iteration_b(j + 2, I2{}, I0{}, I1{});
+            }
+        }
+    }
+    if (!live) return;
+
+    // Where this wave's rows go: the gradient, or a chunk's sums [2][KT][D] (dV first).
+    float* part = nullptr;
+    if (partial) part = p.part + ((((size_t)bh * sink_tiles + kt) * (p.chunks + 1) + chunk + 1) * 2 + role) * KT * D;
+    u16* out = role == 0 ? static_cast<u16*>(p.dv) + at_row(p.dvs, b, h, 0) : static_cast<u16*>(p.dk) + at_row(p.dks, b, h, 0);
+    const long long out_row = role == 0 ? p.dvs[2] : p.dks[2];
+    const float mul = role == 0 ? 1.0f : p.scale;
+    const bool odd = not_finite<D>(acc) && key < p.nk;
+    if (key < p.nk) {
+        if (partial) store_row16<D>(part + (size_t)(key - k0) * D, half, acc, mul);
+        else store_row16<D>(out + key * out_row, half, acc, mul);
+    }
+    for (uint32_t left = (uint32_t)__ballot(odd); left; left &= left - 1) {
+        const int at = w0 + __builtin_ctz(left);
+        const Span span = seen_of_key(p, at);
+        const u16* k = static_cast<const u16*>(p.k) + at_row(p.ks, b, h, at);
+        const u16* v = static_cast<const u16*>(p.v) + at_row(p.vs, b, h, at);
+        float o[D / 64] = {};
+        Cursor x = start();
+        for (int j = 0; j < n_stages; ++j, next(x)) {
+            const int qi = x.at * SR + lane;
+            const bool seen = qi < p.nq && qi >= span.lo && qi <= span.hi;
+            const u16* q0 = static_cast<const u16*>(p.q) + at_row(p.qs, b, x.hh, x.at * SR);
+            const u16* g0 = static_cast<const u16*>(p.dout) + at_row(p.gs, b, x.hh, x.at * SR);
+            float w = 0.0f, ds = 0.0f;
+            if (seen) {
+                const size_t stat = ((size_t)b * p.hq + x.hh) * p.nq + qi;
+                pair_by_definition<D>(q0 + lane * p.qs[2], k, g0 + lane * p.gs[2], v, (double)p.scale * 1.4426950408889634,
+                                      p.lse[stat] * kLog2e, p.dsum[stat], w, ds);
+            }
+            const uint64_t all = __ballot(seen);
+            for (int i = 0; i < 64; ++i)
+                if ((all >> i) & 1) add_row<D>(o, __shfl(role == 0 ? w : ds, i), role == 0 ? g0 + i * p.gs[2] : q0 + i * p.qs[2]);
+        }
+        if (partial) {
+            for (int e = 0; e < D / 64; ++e) part[(size_t)(at - k0) * D + (D / 64) * lane + e] = o[e] * mul;
+        } else {
+            store_lane<D>(out + at * out_row, o, mul);
+        }
+    }
+}
+
+// Adds the chunks' sums of the first keys' tiles, in their order: four elements a
+// thread.
+template <int D>
+__global__ __launch_bounds__(256) void win_join_kernel(WinGrad p, int sink_tiles) {
+    const int per = KT * D / 4 / 256;   // workgroups per tile and tensor
+    int x = blockIdx.x;
+    const int e4 = (x % per) * 256 + threadIdx.x; x /= per;
+    const int role = x & 1; x >>= 1;
+    const int kt = x % sink_tiles, bh = x / sink_tiles, b = bh / p.hk, h = bh - b * p.hk;
+    const int key = kt * KT + e4 / (D / 4), e = e4 % (D / 4) * 4;
+    if (key >= p.nk) return;
+    const size_t step = (size_t)2 * KT * D;
+    const float* at = p.part + ((((size_t)bh * sink_tiles + kt) * (p.chunks + 1)) * 2 + role) * KT * D + (size_t)e4 * 4;
+    f32x4 sum = *reinterpret_cast<const f32x4*>(at);
+    for (int i = 1; i <= p.chunks; ++i) sum += *reinterpret_cast<const f32x4*>(at + i * step);
+    u16* out = role == 0 ? static_cast<u16*>(p.dv) + at_row(p.dvs, b, h, key) : static_cast<u16*>(p.dk) + at_row(p.dks, b, h, key);
+    *reinterpret_cast<uint2*>(out + e) = make_uint2(pack2(sum[0], sum[1]), pack2(sum[2], sum[3]));
+}
+
+template <int D>
+hipError_t go(const WinGrad& p, hipStream_t stream) {
+    const int groups = p.B * p.hk;
+    const float c = p.scale * kLog2e;
+    if (p.nq > 0 && p.hq > 0) {
+        const long long rows = (long long)p.nq * (p.hq / p.hk);
+        const int tiles = (int)((rows + QROWS - 1) / QROWS);
+        const hipError_t e = launch_kernel(win_dq_kernel<D>, dim3((unsigned)groups * tiles), dim3(QW * 64), stream, p, c, tiles);
+        if (e != hipSuccess) return e;
+    }
+    if (p.nk == 0) return hipSuccess;
+    const int key_tiles = (p.nk + KT - 1) / KT, sink_tiles = p.chunks ? win_sink_tiles(p.w, p.nk) : 0;
+    hipError_t e = launch_kernel(win_dkdv_kernel<D>, dim3((unsigned)groups * (key_tiles + sink_tiles * p.chunks)), dim3(KW * 64),
+                                 stream, p, c, key_tiles, sink_tiles);
+    if (e != hipSuccess || !sink_tiles) return e;
+    return launch_kernel(win_join_kernel<D>, dim3((unsigned)groups * sink_tiles * 2 * (KT * D / 4 / 256)), dim3(256), stream, p, sink_tiles);
+}
+
+}  // namespace
+
+hipError_t launch_win_bwd(const WinGrad& p, hipStream_t stream) {
+    return p.d == 64 ? go<64>(p, stream) : go<128>(p, stream);
+}
+
+}  // namespace moa
