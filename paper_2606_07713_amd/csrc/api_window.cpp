@@ -51,21 +51,33 @@ int64_t span(const Sizes& s) {
     return std::min(s.Nk, s.left + ahead + positions + std::min(s.sinks, s.Nk));
 }
 
-// Key splits.  A workgroup of few rows takes steps of 128 keys (four waves, 32
-// each), one of many rows tiles of 64; starting and ending it costs about two of
-// these, and the second pass about three, one more for every 16 splits and for
-// every 6 MB of partial states.  512 workgroups run at a time.
+// Key splits, by an estimate of the call's microseconds.  A workgroup walks over
+// `steps` tiles (of 64 keys with many rows; of 128, four waves' 32, with few), and
+// beginning and ending cost it two more.  A tile takes the longer the more workgroups
+// share a compute unit; more than `most` run one after the other.  Few rows also wait
+// for the memory.  The join reads what the splits wrote, a latency more beyond 32 of
+// them.  (Measured, splits:us.  Many rows: 32 heads on 8, 200 of 20011 keys, d = 128
+// 1:694 4:195 8:126 9:116 12:153; 8 on 2, 4 x 1000, d = 64 1:27 2:33 4:32; 8 heads, 500
+// of 4096, d = 128 4:51 8:36 12:39; 12 on 4, 2 x 700 of 5000, d = 64 1:113 3:60 5:52
+// 6:61.  Few: 32 on 8, one query of 4097, d = 128 1:41 8:17 17:12 32:11 64:14; of 16384
+// 1:193 16:24 32:17 43:23; 8 on 1, 32 x 3 of 9000 4:47 8:35 15:44; 12 on 4, 16 x 4 in
+// a window of 1024, d = 64 1:12.7 4:11.3 5:13.3 16:15.)
 int pick_splits(const Sizes& s, int requested) {
     if (!s.any()) return 1;
     if (requested > 0) return requested;
-    const bool few = s.per() < 128;
-    const int64_t blocks = s.groups(), keys = few ? 128 : 64, all = (span(s) + keys - 1) / keys, wave = 512;
-    const double states = (double)(s.B * s.Hq * s.N) * (double)s.d * sizeof(float) / 6e6;
+    const bool few = s.per() < 128, wide = s.d == 128;
+    const int64_t blocks = s.groups(), keys = few ? 128 : 64, all = std::max<int64_t>(1, (span(s) + keys - 1) / keys);
+    const int64_t most = few ? (s.per() == 32 ? (wide ? 1 : 2) : (wide ? 2 : 4)) : wide ? 2 : 3;
+    const double one = few ? 1.3 : wide ? 2.2 : 1.5, more = few ? 0.4 : wide ? 0.27 : 0.23;   // us, and share of it for each further workgroup
+    const double rows = (double)(s.B * s.Hq * s.N), memory = few ? (double)(s.B * s.Hk * span(s)) * (double)s.d * 4 / 6.5e6 : 0;
+    const auto tile = [&](int64_t at_once) { return at_once ? one * (1 + more * (double)(at_once - 1)) : 0.0; };
     int best = 1;
     double least = 0;
-    for (int64_t k = 1; k <= kMaxSplits && k <= std::max<int64_t>(all, 1) && (k == 1 || k * blocks <= 4 * wave); ++k) {
-        const int64_t rounds = (k * blocks + wave - 1) / wave, steps = (all + k - 1) / k;
-        const double cost = (double)(rounds * (steps + 2)) + (k > 1 ? 3 + (double)k / 16 + (double)k * states : 0);
+    for (int64_t k = 1; k <= kMaxSplits && k <= all && (k == 1 || k * blocks <= 2048); ++k) {
+        const int64_t each = (k * blocks + 255) / 256;   // workgroups of a compute unit
+        const double walk = (double)(each / most) * tile(most) + tile(each % most);
+        double cost = few ? walk * ((double)all / (double)k + 2.5) + memory : walk * (double)((all + k - 1) / k + 2);
+        if (k > 1) cost += 3 + rows * ((double)k * (double)(s.d + 2) * 8 / 5e6 + 1.0 / 8000) + 3 * (double)((k - 1) / 32);
         if (k == 1 || cost < least) {
             best = (int)k;
             least = cost;
@@ -135,23 +147,46 @@ int run(const Call& c, const Sizes& s, const KeySource& src, const Buf* keys, in
 }
 
 // Chunks of the queries that see only the first keys of a sequence, 0 if there are
-// none: so many that one is about as long as what the windows reach, and at most 64
-// over all tiles of such keys.
+// none: as many as fill the GPU once, of six stages at least, and at most 64.
 int far_chunks(const Sizes& s) {
     if (s.left < 0 || !s.any() || s.Nk == 0) return 0;
-    const int tiles = win_sink_tiles(window_of(s), (int)s.Nk);
+    const int64_t tiles = win_sink_tiles(window_of(s), (int)s.Nk);
     if (tiles == 0) return 0;
     // the first tile's windows end here
     const int64_t near = std::clamp<int64_t>(std::min<int64_t>(kWinKeyTile, s.Nk) - (s.Nk - s.N) + s.left, 0, s.N);
-    const int64_t behind = (s.N - near + kWinStage - 1) / kWinStage;
+    const int64_t behind = (s.N - near + kWinStage - 1) / kWinStage * (s.Hq / s.Hk);
     if (behind == 0) return 0;
-    const int64_t reach = (std::min(s.left + std::max<int64_t>(s.right, 0), s.N) + kWinKeyTile) / kWinStage + 1;
-    return (int)std::clamp<int64_t>((behind + reach - 1) / reach, 1, std::max(1, 64 / tiles));
+    const int64_t fill = 256 / (s.B * s.Hk * tiles);
+    return (int)std::clamp<int64_t>(std::min(fill, behind / 6), 1, std::max<int64_t>(1, 64 / tiles));
 }
 
-size_t far_bytes(const Sizes& s, int chunks) {
-    if (!chunks) return 0;
-    return (size_t)(s.B * s.Hk) * (size_t)win_sink_tiles(window_of(s), (int)s.Nk) * (size_t)(chunks + 1) * 2 * kWinKeyTile * (size_t)s.d * 4;
+// Parts of the queries of every key tile, where the tiles alone do not fill the GPU: a
+// workgroup takes a stage of 64 queries in about 1.5 us (256 run at a time), starting
+// and ending it costs about four of these, joining about two and one for every 12 MB
+// of partial sums.
+int near_parts(const Sizes& s) {
+    if (!s.any() || s.Nk == 0) return 1;
+    const int64_t tiles = (s.Nk + kWinKeyTile - 1) / kWinKeyTile, items = s.B * s.Hk * tiles, G = s.Hq / s.Hk;
+    const int64_t reach = s.left < 0 || s.right < 0 ? s.N : std::min(s.N, s.left + s.right + kWinKeyTile);
+    const int64_t all = ((reach + kWinStage - 1) / kWinStage) * G;
+    const double sums = (double)items * kWinKeyTile * (double)s.d * 8 / 12e6;
+    int best = 1;
+    double least = 0;
+    for (int64_t k = 1; k <= 16 && k <= all; ++k) {
+        const int64_t rounds = (k * items + 255) / 256;
+        const double cost = (double)(rounds * ((all + k - 1) / k + 4)) + (k > 1 ? 2 + (double)k * sums : 0);
+        if (k == 1 || cost < least) {
+            best = (int)k;
+            least = cost;
+        }
+    }
+    return best;
+}
+
+size_t part_bytes(const Sizes& s, int parts, int chunks) {
+    const int64_t tiles = (s.Nk + kWinKeyTile - 1) / kWinKeyTile, sinks = chunks ? win_sink_tiles(window_of(s), (int)s.Nk) : 0;
+    const int64_t sums = sinks * (parts + chunks) + (parts > 1 ? (tiles - sinks) * parts : 0);
+    return (size_t)(s.B * s.Hk) * (size_t)sums * 2 * kWinKeyTile * (size_t)s.d * 4;
 }
 
 // Sizes of a gradient call.
@@ -161,7 +196,7 @@ int check_bwd(const Sizes& s) {
     if (s.B * s.Hk > 0 && s.Nk >= (kMaxRows + s.B * s.Hk - 1) / (s.B * s.Hk)) return MOA_ERR_UNSUPPORTED;
     const int64_t tiles = (s.Nk + kWinKeyTile - 1) / kWinKeyTile;
     const int64_t more = s.left < 0 ? 0 : 64 + tiles;   // chunks, of one tile or of many with one each
-    if (s.B * s.Hk * (tiles + more) > kMaxBlocks / 2) return MOA_ERR_UNSUPPORTED;   // of 512 threads
+    if (s.B * s.Hk * (tiles * near_parts(s) + more) > kMaxBlocks / 2) return MOA_ERR_UNSUPPORTED;   // of 512 threads
     return MOA_OK;
 }
 
@@ -214,7 +249,7 @@ int moa_win_attn_fwd(const void* Q, const void* K, const void* V, void* O, float
 size_t moa_win_attn_bwd_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t Nq, int64_t Nk,
                                         int64_t d, int64_t left, int64_t right, int64_t sinks) {
     const Sizes s{B, Hq, Hk, Nq, Nk, d, left, right, sinks};
-    return check_bwd(s) ? 0 : align256((size_t)(B * Hq * Nq) * 4) + far_bytes(s, far_chunks(s));
+    return check_bwd(s) ? 0 : align256((size_t)(B * Hq * Nq) * 4) + part_bytes(s, near_parts(s), far_chunks(s));
 }
 
 int moa_win_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO,
@@ -250,8 +285,8 @@ int moa_win_attn_bwd(const void* Q, const void* K, const void* V, const void* O,
     if (s.any() && !LSE) return MOA_ERR_INVALID_ARG;
     if (B == 0 || (!s.any() && Nk == 0)) return MOA_OK;
     const size_t stats = (size_t)(B * Hq * Nq) * 4;
-    const int chunks = far_chunks(s);
-    const size_t need = align256(stats) + far_bytes(s, chunks);
+    const int parts = near_parts(s), chunks = far_chunks(s);
+    const size_t need = align256(stats) + part_bytes(s, parts, chunks);
     if (need && (!workspace || workspace_bytes < need)) return MOA_ERR_WORKSPACE;
     Buf all[10];
     for (int i = 0; i < 8; ++i) all[i] = {t[i].p, extent_bytes(t[i].s, B, t[i].H, t[i].N, d, t[i].es)};
@@ -270,7 +305,8 @@ int moa_win_attn_bwd(const void* Q, const void* K, const void* V, const void* O,
     p.scale = scale;
     p.o_bf16 = o_dtype == MOA_BF16;
     p.dsum = static_cast<float*>(workspace);
-    p.part = chunks ? reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(stats)) : nullptr;
+    p.part = need > align256(stats) ? reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(stats)) : nullptr;
+    p.parts = parts;
     p.chunks = chunks;
     return hip_status(launch_win_bwd(p, static_cast<hipStream_t>(stream)));
 }

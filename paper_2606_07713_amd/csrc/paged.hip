@@ -16,6 +16,47 @@ namespace {
 
 using namespace rope;
 
+// The heads that one lane group takes of its token: heads first, first + step, ..
+// below end, counted over Q's, K's and V's, one tensor at a time.
+struct Walk {
+    int start[4];          // the first head of each tensor, and the end
+    int step, first, end;
+    int ts, h;             // head h of tensor ts; ts = 3: none left
+    __device__ __forceinline__ Walk(int hq, int hk, int step_, int first_, int end_)
+        : start{0, hq, hq + hk, hq + 2 * hk}, step(step_), first(first_), end(end_) { enter(0); }
+    __device__ __forceinline__ int limit() const { return min(end, start[1]) - start[0]; }
+    // The first head of this group's in tensor t or a later one.  (The tensor's own
+    // limits move to the front, so that no array is indexed.)
+    __device__ __forceinline__ void enter(int t) {
+        ts = t;
+        while (ts < 3) {
+            const int from = first >= start[0] ? first : first + (start[0] - first + step - 1) / step * step;
+            h = from - start[0];
+            if (h < limit()) return;
+            leave();
+        }
+    }
+    __device__ __forceinline__ void leave() {
+        ++ts;
+        start[0] = start[1];
+        start[1] = start[2];
+        start[2] = start[3];
+    }
+    // U heads on
+    template <int U>
+    __device__ __forceinline__ void next() {
+        h += U * step;
+        if (h < limit()) return;
+        leave();
+        enter(ts);
+    }
+};
+
+// One of three values.  (Their places in the arguments or in a closure to choose from
+// sent these to scratch memory.)
+template <typename V>
+__device__ __forceinline__ V pick(int i, V a, V b, V c) { return i == 0 ? a : i == 1 ? b : c; }
+
 template <typename T, int D, bool IL>
 __global__ __launch_bounds__(THREADS) void paged_append_kernel(AppendProblem a, int log_tb, int heads_per_block) {
     constexpr int LPR = D / 8, GROUPS = THREADS / LPR, U = sizeof(T) == 2 ? 4 : 2;   // rows in flight per group
@@ -25,7 +66,7 @@ __global__ __launch_bounds__(THREADS) void paged_append_kernel(AppendProblem a, 
     const int j = threadIdx.x % LPR, grp = threadIdx.x / LPR, lane = threadIdx.x & 63;
     const int t = grp & (tb - 1), tok = min(t0 + t, tokens - 1);
     const int b = tok / p.N, n = tok - b * p.N;
-    const int hq = p.H[0], hk = p.H[1], step = GROUPS >> log_tb;
+    const int hq = p.H[0], hk = p.H[1];
     const int y0 = blockIdx.y * heads_per_block, y1 = min(y0 + heads_per_block, hq + 2 * hk);
     // Token n of sequence b is its token `at`.
     const auto place = [&](int tok) {
@@ -35,29 +76,27 @@ __global__ __launch_bounds__(THREADS) void paged_append_kernel(AppendProblem a, 
     const bool real = t0 + t < tokens && n < win::new_tokens(a.to.new_lens, b, p.N);
     const long long at = place(tok);
     const int page = at >= 0 && at < win::capacity(a.to) ? win::page_of(a.to, b, (int)at) : -1;
-    // Heads are counted over Q's, K's and V's.
-    const auto part = [&](int h) { return h < hq ? 0 : h < hq + hk ? 1 : 2; };
-    const auto row_of = [&](int h) -> const T* {
-        const int ts = part(h);
-        const void* base = ts == 0 ? p.x[0] : ts == 1 ? p.x[1] : a.v;
-        const int head = h - (ts == 0 ? 0 : ts == 1 ? hq : hq + hk);
-        const long long s0 = ts == 0 ? p.xs[0][0] : ts == 1 ? p.xs[1][0] : a.vs[0];
-        const long long s1 = ts == 0 ? p.xs[0][1] : ts == 1 ? p.xs[1][1] : a.vs[1];
-        const long long s2 = ts == 0 ? p.xs[0][2] : ts == 1 ? p.xs[1][2] : a.vs[2];
-        return static_cast<const T*>(base) + b * s0 + head * s1 + n * s2 + 8 * j;
-    };
-    int h = y0 + (grp >> log_tb);
+    const T* const xq = static_cast<const T*>(p.x[0]) + b * p.xs[0][0] + n * p.xs[0][2] + 8 * j;
+    const T* const xk = static_cast<const T*>(p.x[1]) + b * p.xs[1][0] + n * p.xs[1][2] + 8 * j;
+    const T* const xv = static_cast<const T*>(a.v) + b * a.vs[0] + n * a.vs[2] + 8 * j;
+    u16* const yq = static_cast<u16*>(p.y[0]) + b * p.ys[0][0] + n * p.ys[0][2] + 8 * j;
+    u16* const yk = static_cast<u16*>(const_cast<void*>(a.to.k)) + (page >= 0 ? win::key_offset(a.to.ks, a.to.shift, page, 0, (int)at) : 0) + 8 * j;
+    u16* const yv = static_cast<u16*>(const_cast<void*>(a.to.v)) + (page >= 0 ? win::key_offset(a.to.vs, a.to.shift, page, 0, (int)at) : 0) + 8 * j;
+    Walk w(hq, hk, GROUPS >> log_tb, y0 + (grp >> log_tb), y1);
     // Keys and values of a token without a page are not read.
-    const auto wanted = [&](int h) { return real && h < y1 && (h < hq || page >= 0); };
-    const auto load = [&](Chunk<T> (&c)[U], int h) {
+    const auto wanted = [&](int ts) { return real && ts < 3 && (ts == 0 || page >= 0); };
+    const auto load = [&](Chunk<T> (&c)[U]) {
+        const T* base = pick(w.ts, xq, xk, xv);
+        const long long stride = pick(w.ts, p.xs[0][1], p.xs[1][1], a.vs[1]);
+        const int limit = wanted(w.ts) ? w.limit() : 0;
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (wanted(h + u * step)) c[u].load(row_of(h + u * step));
+            if (w.h + u * w.step < limit) c[u].load(base + (w.h + u * w.step) * stride);
             else c[u].zero();
     };
     // The first rows and the weights are on their way while the angles are taken.
     Chunk<T> next[U];
-    load(next, h);
+    load(next);
     float wq[8], wk[8];
     load_weights(p, 0, j, wq);
     load_weights(p, 1, j, wk);
@@ -68,50 +107,51 @@ __global__ __launch_bounds__(THREADS) void paged_append_kernel(AppendProblem a, 
     turn.set(p, cs + t * (p.rot >> 1), j, lane);
     float A[8], Bp[8];
     int have = -1;
-    while (h < y1) {
+    while (w.ts < 3) {
+        const int ts = w.ts, h = w.h, limit = wanted(ts) ? w.limit() : 0, step = w.step;
         Chunk<T> c[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) c[u] = next[u];
-        const int h0 = h;
-        h += U * step;
-        load(next, h);
+        w.template next<U>();
+        load(next);
+        u16* to = pick(ts, yq, yk, yv);
+        const long long stride = pick(ts, p.ys[0][1], a.to.ks[1], a.to.vs[1]);
+        if (ts == 2) {   // values go over as they are
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float f[8];
+                c[u].get(f);
+                if (h + u * step < limit) Chunk<u16>::store(to + (h + u * step) * stride, f);
+            }
+            continue;
+        }
+        if (ts != have) {
+            have = ts;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) A[e] = ts ? wk[e] : wq[e];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) Bp[e] = IL ? A[e ^ 1] : __shfl(A[e], turn.partner);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { A[e] *= turn.c[e]; Bp[e] = turn.turned ? Bp[e] * turn.s[e] : 0.0f; }
+        }
+        const bool norm = pick(ts, p.w[0], p.w[1], p.w[1]) != nullptr;
         bool redo[U];
         const auto row = [&](int u, float r, auto again) {
-            const int hu = h0 + u * step, ts = part(hu);
-            // Partners move between lanes, so every lane of the group takes part.
-            if (ts < 2 && ts != have) {
-                have = ts;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) A[e] = ts == 1 ? wk[e] : wq[e];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) Bp[e] = IL ? A[e ^ 1] : __shfl(A[e], turn.partner);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) { A[e] *= turn.c[e]; Bp[e] = turn.turned ? Bp[e] * turn.s[e] : 0.0f; }
-            }
             float f[8], o[8];
             c[u].get(f);
             turn.partners(c[u], f, o);
-            if (!again) redo[u] = false;
-            if (ts < 2) {
-                if (!again && p.w[ts ? 1 : 0] != nullptr) {
+            const bool in = h + u * step < limit;
+            if (!again) {
+                redo[u] = false;
+                if (norm) {
                     const float m = mean_square<LPR>(f) + p.eps;
                     r = __builtin_amdgcn_rsqf(m);
-                    redo[u] = wanted(hu) && !in_range(m);
+                    redo[u] = in && !in_range(m);
                 }
+            }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = r * __builtin_fmaf(f[e], A[e], o[e] * Bp[e]);
-            }
-            if (!wanted(hu) || redo[u] != again) return;
-            u16* to;
-            if (ts == 0) {
-                to = static_cast<u16*>(p.y[0]) + b * p.ys[0][0] + hu * p.ys[0][1] + n * p.ys[0][2];
-            } else {
-                const int head = hu - (ts == 1 ? hq : hq + hk);
-                to = static_cast<u16*>(const_cast<void*>(ts == 1 ? a.to.k : a.to.v)) +
-                     (ts == 1 ? win::key_offset(a.to.ks, a.to.shift, page, head, (int)at)
-                              : win::key_offset(a.to.vs, a.to.shift, page, head, (int)at));
-            }
-            Chunk<u16>::store(to + 8 * j, f);
+            for (int e = 0; e < 8; ++e) f[e] = r * __builtin_fmaf(f[e], A[e], o[e] * Bp[e]);
+            if (in && redo[u] == again) Chunk<u16>::store(to + (h + u * step) * stride, f);
         };
         bool any = false;
 #pragma unroll

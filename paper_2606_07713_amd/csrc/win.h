@@ -63,8 +63,9 @@ struct WinGrad {
     float scale;
     bool o_bf16;
     float* dsum;               // [B][hq][nq]: <dO, O> of every row
-    float* part;               // partial sums of dK and dV of the keys that far queries see
-    int chunks;                // of the queries behind the first keys' windows
+    float* part;               // partial sums of dK and dV
+    int parts;                 // of every key tile's queries (1: whole)
+    int chunks;                // of the queries behind the first keys' windows (0: none)
 };
 
 // Keys of a workgroup of the dK, dV kernel, and queries of one of its stages.

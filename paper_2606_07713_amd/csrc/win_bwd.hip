@@ -17,11 +17,14 @@
 //   stream through LDS, 64 queries of one head at a time, head after head, so that
 //   shared heads meet in the same sums.  A pair of waves on one SIMD owns 32 keys:
 //   one forms S and P and sums dV, the other forms dP and dS with the partner's P and
-//   sums dK, one stage behind.
+//   sums dK, one stage behind.  P crosses with the upper 24 bits of its fp32 number,
+//   four in three registers.  (In bf16 its rounding made dK's error 2.9e-3, with these
+//   2.4e-3.)
 // * The first keys stay visible to all later queries, so their sums would be as long
 //   as the sequence where all others are as long as the window.  The queries behind
-//   their windows are cut into chunks with workgroups of their own, which leave fp32
-//   sums that win_join adds in a fixed order.
+//   their windows are cut into chunks with workgroups of their own, and where there
+//   are few key tiles the queries of every tile into parts; they leave fp32 sums that
+//   win_join adds in a fixed order.
 // No atomics; deterministic.  P and dS are rounded to bf16 for the matrix products.
 // Rows whose sums do not come out finite are done again by the definition.
 #include <algorithm>
@@ -223,10 +226,10 @@ __global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, 
         const unsigned char* ks = decltype(stage)::value == 0 ? k_st0 : k_st1;
         const unsigned char* vs = decltype(stage)::value == 0 ? v_st0 : v_st1;
         const int k0 = tiles.at(v) * BN;
-        if (!live || k0 >= wh.hi || (k0 + BN <= wl.lo && k0 >= p.w.sinks)) return;
-        const bool need_mask = k0 + BN > wl.hi || (k0 < wh.lo && k0 + BN > p.w.sinks);
+        if (!live) return;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
+            if (!any_of(wl, wh, p.w.sinks, k0 + 32 * u)) continue;
             f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
@@ -235,11 +238,8 @@ __global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, 
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], c, -lse2);
-            if (need_mask) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!sees(seen, p.w.sinks, k0 + 32 * u + (i >> 2) * 8 + half * 4 + (i & 3))) s[i] = kNegInf;
-            }
+            const int how = mask_of(wl, wh, p.w.sinks, k0 + 32 * u);
+            if (how) mask_scores(s, how, 3, seen, p.w.sinks, k0 + 32 * u, half);
             float ds[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) ds[i] = exp2_hw(s[i]) * (dp[i] - dsum);
@@ -291,7 +291,21 @@ __global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, 
 
 // ---- dK, dV ------------------------------------------------------------------
 
-constexpr int KW = 8;       // waves
+constexpr int KW = 8;             // waves
+
+// Four numbers with their upper 24 bits in three registers: the fourth in the others'
+// low bytes, which are left there when the three are used (2^-16 of them).
+__device__ __forceinline__ void pack24(const float (&w)[4], uint32_t (&x)[3]) {
+    const uint32_t last = __float_as_uint(w[3]);
+    x[0] = __builtin_amdgcn_perm(last, __float_as_uint(w[0]), 0x03020107u);
+    x[1] = __builtin_amdgcn_perm(last, __float_as_uint(w[1]), 0x03020106u);
+    x[2] = __builtin_amdgcn_perm(last, __float_as_uint(w[2]), 0x03020105u);
+}
+__device__ __forceinline__ void unpack24(const uint32_t (&x)[3], float (&w)[4]) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) w[i] = __uint_as_float(x[i]);
+    w[3] = __uint_as_float(__builtin_amdgcn_perm(__builtin_amdgcn_perm(x[0], x[1], 0x04000c0cu), x[2], 0x0706000cu));
+}
 constexpr int KT = kWinKeyTile;   // keys per workgroup
 constexpr int SR = kWinStage;     // queries per stage
 
@@ -313,8 +327,17 @@ struct Stages {
     int first, each, begin, count;
 };
 
+// Partial sums: of every tile those of its parts, of the first keys' tiles those of
+// their chunks behind them; none of a tile with one part and no chunks.  The first
+// ones of tile kt of key/value head bh.
+__device__ __forceinline__ size_t first_part(const WinGrad& p, int sink_tiles, int bh, int kt) {
+    const int key_tiles = (p.nk + KT - 1) / KT, far = p.parts + p.chunks, near = p.parts > 1 ? p.parts : 0;
+    const size_t all = (size_t)sink_tiles * far + (size_t)(key_tiles - sink_tiles) * near;
+    return bh * all + (kt < sink_tiles ? (size_t)kt * far : (size_t)sink_tiles * far + (size_t)(kt - sink_tiles) * near);
+}
+
 template <int D>
-__global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c, int key_tiles, int sink_tiles) {
+__global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c, int sink_tiles) {
     using C = Cfg<D>;
     constexpr uint32_t RB = C::ROW_BYTES;
     constexpr int U = SR / 32;                             // steps per stage
@@ -322,8 +345,8 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
     // One array per ring slot: the compiler tracks direct-to-LDS loads per object.
     __shared__ __attribute__((aligned(1024))) unsigned char q_0[SR * C::ROW_BYTES], q_1[SR * C::ROW_BYTES], q_2[SR * C::ROW_BYTES];
     __shared__ __attribute__((aligned(1024))) unsigned char g_0[SR * C::ROW_BYTES], g_1[SR * C::ROW_BYTES], g_2[SR * C::ROW_BYTES];
-    // Exchanged weights: [stage parity][pair][step][chunk][lane].
-    __shared__ __attribute__((aligned(1024))) uint4 p_x[2][4][U][2][64];
+    // Exchanged weights: [stage parity][pair][step][register quad][lane].
+    __shared__ __attribute__((aligned(1024))) u32x4 p_x[2][4][U][3][64];
     __shared__ __attribute__((aligned(16))) float l_r[3][2][SR];   // [slot][lse2, D][query]
 
     const int lane = threadIdx.x & 63;
@@ -332,13 +355,15 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
     const int col = lane & 31, half = lane >> 5;
     const int G = p.hq / p.hk, groups = p.B * p.hk;
     const int bh = blockIdx.x % groups, b = bh / p.hk, h = bh - b * p.hk;
-    // Items of a head: the chunks of the far queries of the first keys' tiles, then
-    // every tile with the queries whose windows reach it.
-    const int item = blockIdx.x / groups, far_items = sink_tiles * p.chunks;
-    const bool far = item < far_items;
-    const int kt = far ? item / p.chunks : item - far_items, chunk = far ? item % p.chunks : -1;
+    // Items of a head: the parts of every tile's queries whose windows reach it, then
+    // the chunks of the far queries of the first keys' tiles, short ones that fill up
+    // the last round.
+    const int item = blockIdx.x / groups, near_items = (p.nk + KT - 1) / KT * p.parts;
+    const bool far = item >= near_items;
+    const int kt = far ? (item - near_items) / p.chunks : item / p.parts;
+    const int cuts = far ? p.chunks : p.parts, cut = far ? (item - near_items) % p.chunks : item % p.parts;
     const int k0 = kt * KT, k1 = min(k0 + KT, p.nk) - 1;
-    const bool partial = kt < sink_tiles && p.chunks > 0;
+    const bool split = kt < sink_tiles && p.chunks > 0;
 
     Stages st;
     {
@@ -347,7 +372,7 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
         const int lo = seen_of_key(p, k0).lo;
         int hi = seen_of_key(p, k1).hi;
         const int near_hi = (int)max(-1ll, min((long long)p.nq - 1, k1 - off + (long long)p.w.left));
-        if (k0 < p.w.sinks) hi = partial ? near_hi : p.nq - 1;
+        if (k0 < p.w.sinks) hi = split ? near_hi : p.nq - 1;
         int first = lo / SR, end = hi < lo ? first : hi / SR + 1;
         if (far) {
             first = max(lo / SR, (near_hi + SR) / SR);   // the stage behind near_hi's
@@ -355,8 +380,8 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
         }
         st.first = first;
         st.each = end - first;
-        const int all = st.each * G, per = far ? (all + p.chunks - 1) / p.chunks : all;
-        st.begin = far ? min(all, chunk * per) : 0;
+        const int all = st.each * G, per = (all + cuts - 1) / cuts;
+        st.begin = min(all, cut * per);
         st.count = min(per, all - st.begin);
     }
     const int n_stages = st.count;
@@ -370,7 +395,7 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
     const int some_lo = __builtin_amdgcn_readfirstlane(wa.lo), all_lo = __builtin_amdgcn_readfirstlane(wb.lo);
     const int some_hi = __builtin_amdgcn_readfirstlane(max(wa.hi, wb.hi));
     const int all_hi = __builtin_amdgcn_readfirstlane(min(wa.hi, wc.hi));
-    const bool live = w0 < p.nk;
+    const bool live = w0 < p.nk && !(far && w0 >= p.w.sinks);
 
     const uint32_t qrb = (uint32_t)p.qs[2] * 2u, grb = (uint32_t)p.gs[2] * 2u;
     uint32_t qoff[LPS], goff[LPS];
@@ -399,10 +424,11 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
 
-    // Whether the pair has anything to do in the 32 queries from q0 on.
-    const auto wanted = [&](int q0) { return live && q0 <= some_hi && q0 + 31 >= some_lo; };
+    // Whether the pair has anything to do in the stage from query q0 on.  (Tested for
+    // each half of it, the steps did not overlap.)
+    const auto wanted = [&](int q0) { return live && q0 <= some_hi && q0 + SR > some_lo; };
 
-    auto step_a = [&](const unsigned char* qs, const unsigned char* gs, const float* ls, uint4* px, int u, int q0)
+    auto step_a = [&](const unsigned char* qs, const unsigned char* gs, const float* ls, u32x4* px, int u, int q0)
                       __attribute__((always_inline)) {
         f32x16 s = f32x16{};
 #pragma unroll
@@ -425,34 +451,46 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
         float w[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) w[i] = exp2_hw(s[i]);
+        u32x4 x[3];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float four[4] = {w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]};
+            uint32_t y[3];
+            pack24(four, y);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) x[(3 * g + i) / 4][(3 * g + i) % 4] = y[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i) px[i * 64 + lane] = x[i];
         bf16x8 pb[2];
         pack16(w, pb);
-#pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2) px[c2 * 64 + lane] = __builtin_bit_cast(uint4, pb[c2]);
 #pragma unroll
         for (int c2 = 0; c2 < 2; ++c2)
 #pragma unroll
             for (int d = 0; d < D / 32; ++d)
                 acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_tr<D>(gs, ta, d, 2 * u + c2), pb[c2], acc[d], 0, 0, 0);
     };
-    auto step_b = [&](const unsigned char* qs, const unsigned char* gs, const float* dv, const uint4* px, int u)
+    auto step_b = [&](const unsigned char* qs, const unsigned char* gs, const float* dv, const u32x4* px, int u)
                       __attribute__((always_inline)) {
         f32x16 dp = f32x16{};
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
             dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_rows<D>(gs, ta, u, k), kvf[k], dp, 0, 0, 0);
-        const uint4 x0 = px[lane], x1 = px[64 + lane];
-        const uint32_t pw[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+        u32x4 x[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) x[i] = px[i * 64 + lane];
         float ds[16];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
+            uint32_t y[3];
+#pragma unroll
+            for (int i = 0; i < 3; ++i) y[i] = x[(3 * g + i) / 4][(3 * g + i) % 4];
+            float w[4];
+            unpack24(y, w);
             const float4 d4 = *reinterpret_cast<const float4*>(dv + 32 * u + 8 * g + 4 * half);
             const float dd[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 4 * g + r;
-                ds[i] = ((i & 1) ? bf16hi_to_f32(pw[i >> 1]) : bf16lo_to_f32(pw[i >> 1])) * (dp[i] - dd[r]);
-            }
+            for (int r = 0; r < 4; ++r) ds[4 * g + r] = w[r] * (dp[4 * g + r] - dd[r]);
         }
         bf16x8 dsb[2];
         pack16(ds, dsb);
@@ -478,6 +516,7 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
         }
     };
     Cursor load = start(), work = load;
+    const float* stats = role == 0 ? p.lse : p.dsum;
     float sx = 0.0f;
     auto issue = [&](unsigned char* qd, unsigned char* gd) __attribute__((always_inline)) {
         const int q0 = load.at * SR, n = min(SR, p.nq - q0);
@@ -487,12 +526,8 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
         for (int i = 0; i < LPS; ++i) buffer_load16_to_lds(rq, qd + (wave * LPS + i) * 1024, qoff[i]);
 #pragma unroll
         for (int i = 0; i < LPS; ++i) buffer_load16_to_lds(rg, gd + (wave * LPS + i) * 1024, goff[i]);
-        // LSE and D of the stage's queries: one of each wave pair's, a query a lane.
-        sx = 0.0f;
-        if (pair == 0 && q0 + lane < p.nq) {
-            const size_t stat = ((size_t)b * p.hq + load.hh) * p.nq + q0 + lane;
-            sx = role == 0 ? p.lse[stat] * kLog2e : p.dsum[stat];
-        }
+        // LSE or D of the stage's queries, a query a lane (behind the last: masked).
+        sx = stats[((size_t)b * p.hq + load.hh) * p.nq + min(q0 + lane, p.nq - 1)];
         next(load);
     };
     using I0 = std::integral_constant<int, 0>;
@@ -504,7 +539,7 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
     // role 1 on the one before, whose weights role 0 wrote in iteration j - 1; the
     // loads of stage j + 1 start into the slot whose last reader is done.
     auto advance = [&](int j, auto slot, auto after) __attribute__((always_inline)) {
-        if (j < n_stages && pair == 0) l_r[decltype(slot)::value][role][lane] = sx;
+        if (j < n_stages && pair == 0) l_r[decltype(slot)::value][role][lane] = role == 0 ? sx * kLog2e : sx;
         pf::wait_vmcnt<0>();
         pf::wait_lgkmcnt0();
         pf::barrier_no_fence();
@@ -513,18 +548,18 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
     auto iteration_a = [&](int j, auto slot, auto after) __attribute__((always_inline)) {
         advance(j, slot, after);
         if (j >= n_stages) return;
+        if (wanted(work.at * SR))
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (wanted(work.at * SR + 32 * u))
+            for (int u = 0; u < U; ++u)
                 step_a(q_slot(slot), g_slot(slot), l_r[decltype(slot)::value][0], &p_x[j & 1][pair][u][0][0], u, work.at * SR + 32 * u);
         next(work);
     };
     auto iteration_b = [&](int j, auto slot, auto after, auto before) __attribute__((always_inline)) {
         advance(j, slot, after);
         if (j == 0) return;
+        if (wanted(work.at * SR))
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (wanted(work.at * SR + 32 * u))
+            for (int u = 0; u < U; ++u)
                 step_b(q_slot(before), g_slot(before), l_r[decltype(before)::value][1], &p_x[(j - 1) & 1][pair][u][0][0], u);
         next(work);
     };
@@ -550,9 +585,11 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
     }
     if (!live) return;
 
-    // Where this wave's rows go: the gradient, or a chunk's sums [2][KT][D] (dV first).
+    // Where this wave's rows go: the gradient, or the sums [2][KT][D] (dV first) of a
+    // part or chunk.
+    const bool partial = p.parts > 1 || split;
     float* part = nullptr;
-    if (partial) part = p.part + ((((size_t)bh * sink_tiles + kt) * (p.chunks + 1) + chunk + 1) * 2 + role) * KT * D;
+    if (partial) part = p.part + ((first_part(p, sink_tiles, bh, kt) + (far ? p.parts : 0) + cut) * 2 + role) * KT * D;
     u16* out = role == 0 ? static_cast<u16*>(p.dv) + at_row(p.dvs, b, h, 0) : static_cast<u16*>(p.dk) + at_row(p.dks, b, h, 0);
     const long long out_row = role == 0 ? p.dvs[2] : p.dks[2];
     const float mul = role == 0 ? 1.0f : p.scale;
@@ -591,21 +628,28 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
     }
 }
 
-// Adds the chunks' sums of the first keys' tiles, in their order: four elements a
-// thread.
+// Adds the sums of a tile's parts and chunks, in their order: four elements a thread.
 template <int D>
-__global__ __launch_bounds__(256) void win_join_kernel(WinGrad p, int sink_tiles) {
-    const int per = KT * D / 4 / 256;   // workgroups per tile and tensor
+__global__ __launch_bounds__(256) void win_join_kernel(WinGrad p, int tiles, int sink_tiles) {
+    constexpr int PER = KT * D / 4 / 256;   // workgroups per tile and tensor
     int x = blockIdx.x;
-    const int e4 = (x % per) * 256 + threadIdx.x; x /= per;
+    const int e4 = (x % PER) * 256 + threadIdx.x; x /= PER;
     const int role = x & 1; x >>= 1;
-    const int kt = x % sink_tiles, bh = x / sink_tiles, b = bh / p.hk, h = bh - b * p.hk;
+    const int kt = x % tiles, bh = x / tiles, b = bh / p.hk, h = bh - b * p.hk;
     const int key = kt * KT + e4 / (D / 4), e = e4 % (D / 4) * 4;
     if (key >= p.nk) return;
-    const size_t step = (size_t)2 * KT * D;
-    const float* at = p.part + ((((size_t)bh * sink_tiles + kt) * (p.chunks + 1)) * 2 + role) * KT * D + (size_t)e4 * 4;
-    f32x4 sum = *reinterpret_cast<const f32x4*>(at);
-    for (int i = 1; i <= p.chunks; ++i) sum += *reinterpret_cast<const f32x4*>(at + i * step);
+    // chunks hold sums of the first keys alone
+    const int n = p.parts + (kt < sink_tiles && key < p.w.sinks ? p.chunks : 0);
+    const float* at = p.part + (first_part(p, sink_tiles, bh, kt) * 2 + role) * KT * D + (size_t)e4 * 4;
+    f32x4 sum = {0, 0, 0, 0};
+    for (int i = 0; i < n; i += 4) {
+        f32x4 y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const f32x4*>(at + (size_t)min(i + u, n - 1) * 2 * KT * D);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + u < n) sum += y[u];
+    }
     u16* out = role == 0 ? static_cast<u16*>(p.dv) + at_row(p.dvs, b, h, key) : static_cast<u16*>(p.dk) + at_row(p.dks, b, h, key);
     *reinterpret_cast<uint2*>(out + e) = make_uint2(pack2(sum[0], sum[1]), pack2(sum[2], sum[3]));
 }
@@ -622,10 +666,11 @@ hipError_t go(const WinGrad& p, hipStream_t stream) {
     }
     if (p.nk == 0) return hipSuccess;
     const int key_tiles = (p.nk + KT - 1) / KT, sink_tiles = p.chunks ? win_sink_tiles(p.w, p.nk) : 0;
-    hipError_t e = launch_kernel(win_dkdv_kernel<D>, dim3((unsigned)groups * (key_tiles + sink_tiles * p.chunks)), dim3(KW * 64),
-                                 stream, p, c, key_tiles, sink_tiles);
-    if (e != hipSuccess || !sink_tiles) return e;
-    return launch_kernel(win_join_kernel<D>, dim3((unsigned)groups * sink_tiles * 2 * (KT * D / 4 / 256)), dim3(256), stream, p, sink_tiles);
+    const int items = key_tiles * p.parts + sink_tiles * p.chunks;
+    hipError_t e = launch_kernel(win_dkdv_kernel<D>, dim3((unsigned)groups * items), dim3(KW * 64), stream, p, c, sink_tiles);
+    const int joined = p.parts > 1 ? key_tiles : sink_tiles;
+    if (e != hipSuccess || !joined) return e;
+    return launch_kernel(win_join_kernel<D>, dim3((unsigned)groups * joined * 2 * (KT * D / 4 / 256)), dim3(256), stream, p, joined, sink_tiles);
 }
 
 }  // namespace

@@ -82,6 +82,44 @@ __device__ __forceinline__ bool sees(const Seen& s, int sinks, int key) {
 }
 __device__ __forceinline__ bool sees_any(const Seen& s, int sinks) { return s.hi > 0 && (s.lo < s.hi || sinks > 0); }
 
+// What is to be masked of 32 keys from k0 on for rows of which the first sees wl and
+// the last wh (uniform): nothing, keys behind a row's end, keys before its window,
+// or all of it.
+enum { MASK_NONE, MASK_END = 1, MASK_BEGIN = 2, MASK_ALL = 4 };
+__device__ __forceinline__ int mask_of(const Seen& wl, const Seen& wh, int sinks, int k0) {
+    const bool end = k0 + 32 > wl.hi, begin = k0 < wh.lo && k0 + 32 > sinks;
+    if (begin && k0 < sinks) return MASK_ALL;
+    return (end ? MASK_END : 0) | (begin ? MASK_BEGIN : 0);
+}
+// Whether any of these rows sees one of the 32 keys.
+__device__ __forceinline__ bool any_of(const Seen& wl, const Seen& wh, int sinks, int k0) {
+    return k0 < wh.hi && (k0 + 32 > wl.lo || k0 < sinks);
+}
+
+// Masks the scores x of a lane's row in a 32x32 accumulator: element i is key k0 +
+// 8 (i / 4) + 4 half + i % 4.  have: bit t: the t-th 16 keys have a page.
+__device__ __forceinline__ void mask_scores(f32x16& x, int how, int have, const Seen& seen, int sinks, int k0, int half) {
+    const int at = k0 + 4 * half, hi = seen.hi - at, lo = seen.lo - at;
+    if ((how & MASK_ALL) || have != 3) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int k = (i >> 2) * 8 + (i & 3);
+            if (!((have >> (i >> 3)) & 1) || !(k < hi && (k >= lo || at + k < sinks))) x[i] = kNegInf;
+        }
+        return;
+    }
+    if (how & MASK_END) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if ((i >> 2) * 8 + (i & 3) >= hi) x[i] = kNegInf;
+    }
+    if (how & MASK_BEGIN) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if ((i >> 2) * 8 + (i & 3) < lo) x[i] = kNegInf;
+    }
+}
+
 // The tiles of T keys that any of the rows from `first` to `last` (positions in
 // order) see: those of the first keys, then those of the windows.
 template <int T>

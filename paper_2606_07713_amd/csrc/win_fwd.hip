@@ -158,23 +158,17 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
         const unsigned char* ks = decltype(stage)::value == 0 ? k_st0 : k_st1;
         unsigned char* vs = decltype(stage)::value == 0 ? v_st0 : v_st1;
         const int k0 = tiles.at(v) * BN;
-        // Nothing for this wave's rows, or no row hides a key of it.
-        if (!live || k0 >= wh.hi || (k0 + BN <= wl.lo && k0 >= p.w.sinks)) return;
-        const bool need_mask = have != 15 || k0 + BN > wl.hi || (k0 < wh.lo && k0 + BN > p.w.sinks);
+        if (!live) return;
 #pragma unroll
         for (int sb = 0; sb < BN / SN; ++sb) {
+            if (!any_of(wl, wh, p.w.sinks, k0 + sb * SN)) continue;
             f32x16 s = f32x16{};
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                     *reinterpret_cast<const bf16x8*>(ks + kaddr[k] + sb * SN * RB), qf[k], s, 0, 0, 0);
-            if (need_mask) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int in_tile = sb * SN + (i >> 2) * 8 + half * 4 + (i & 3);
-                    if (!((have >> (in_tile >> 4)) & 1) || !sees(seen, p.w.sinks, k0 + in_tile)) s[i] = kNegInf;
-                }
-            }
+            const int how = mask_of(wl, wh, p.w.sinks, k0 + sb * SN), pages = (have >> (2 * sb)) & 3;
+            if (how || pages != 3) mask_scores(s, how, pages, seen, p.w.sinks, k0 + sb * SN, half);
             const auto raise = [&]() __attribute__((always_inline)) {
                 float m = kNegInf;
                 asm volatile("" : "+v"(m));   // not hoisted onto the fast path
