@@ -26,6 +26,18 @@ struct Window {
 };
 constexpr int kNoLimit = 1 << 30;
 
+// Division by n of numbers below 2^31, as a product: x / n = (2 x m) >> (32 + shift).
+struct Div {
+    uint32_t n, m;
+    int shift, unused;
+};
+inline Div div_by(long long n) {
+    Div d{(uint32_t)n, 0, 0, 0};
+    while ((1ll << d.shift) < n) ++d.shift;
+    d.m = (uint32_t)(((1ull << (31 + d.shift)) + (uint64_t)n - 1) / (uint64_t)n);
+    return d;
+}
+
 struct WinAttn {
     KeySource s;
     Window w;
@@ -36,11 +48,20 @@ struct WinAttn {
     int B, hq, hk, n, d;
     float scale;
     bool out_bf16;
+    // set by the launchers: query heads of a key/value head; workgroups of a row tile
+    Div group, per_tile, per_head, heads;
     // Key splits (1 = none) and their partial states: [B][hq][n][splits][d]
     // fp32, then [B][hq][n][splits][2] (reference in log2 units, sum).
     int splits;
     float* ws;
 };
+
+inline void set_divisions(WinAttn& p) {
+    p.group = div_by(p.hq / p.hk);
+    p.per_tile = div_by((long long)p.B * p.hk * p.splits);
+    p.per_head = div_by(p.splits);
+    p.heads = div_by(p.hk);
+}
 
 // Rows (queries times the query heads of a key/value head) that a workgroup
 // takes: 16 or 32 in the kernel of few rows, 128 in that of many.
@@ -62,6 +83,7 @@ struct WinGrad {
     int B, hq, hk, nq, nk, d;
     float scale;
     bool o_bf16;
+    Div group, per_item, heads;   // set by the launcher, as in WinAttn
     float* dsum;               // [B][hq][nq]: <dO, O> of every row
     float* part;               // partial sums of dK and dV
     int parts;                 // of every key tile's queries (1: whole)

@@ -140,19 +140,20 @@ __global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
-    const int G = p.hq / p.hk, groups = p.B * p.hk, rt = row_tiles - 1 - blockIdx.x / groups;
-    const int bh = blockIdx.x % groups, b = bh / p.hk, h = bh - b * p.hk;
+    const int G = (int)p.group.n, up = over(p.per_item, blockIdx.x), rt = row_tiles - 1 - up;
+    const int bh = blockIdx.x - up * (int)p.per_item.n, b = over(p.heads, bh), h = bh - b * p.hk;
     const int rows = p.nq * G, row0 = rt * QROWS;
     const auto uniform = [](Seen s) {
         return Seen{__builtin_amdgcn_readfirstlane(s.lo), __builtin_amdgcn_readfirstlane(s.hi)};
     };
-    const Tiles<BN> tiles(uniform(seen_by(p, row0 / G)), uniform(seen_by(p, (min(row0 + QROWS, rows) - 1) / G)), p.w.sinks);
+    const Tiles<BN> tiles(uniform(seen_by(p, over(p.group, row0))), uniform(seen_by(p, over(p.group, min(row0 + QROWS, rows) - 1))), p.w.sinks);
 
     // This wave's rows; this lane's row, its Q and dO fragments, LSE and D.
     const int w0 = row0 + wave * 32, row = w0 + col;
     const bool live = w0 < rows, in = row < rows;
-    const Seen wl = uniform(seen_by(p, min(w0, rows - 1) / G)), wh = uniform(seen_by(p, (min(w0 + 32, rows) - 1) / G));
-    const int qi = min(row, rows - 1) / G, hh = h * G + min(row, rows - 1) - qi * G;
+    const int sinks = p.w.sinks;
+    const Seen wl = uniform(seen_by(p, over(p.group, min(w0, rows - 1)))), wh = uniform(seen_by(p, over(p.group, min(w0 + 32, rows) - 1)));
+    const int qi = over(p.group, min(row, rows - 1)), hh = h * G + min(row, rows - 1) - qi * G;
     const Seen seen = seen_by(p, qi);
     const u16* qr = static_cast<const u16*>(p.q) + at_row(p.qs, b, hh, qi);
     const u16* gr = static_cast<const u16*>(p.dout) + at_row(p.gs, b, hh, qi);
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, 
         if (!live) return;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            if (!any_of(wl, wh, p.w.sinks, k0 + 32 * u)) continue;
+            if (!any_sees(wl, wh, sinks, k0 + 32 * u)) continue;
             f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
@@ -238,8 +239,7 @@ __global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, 
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], c, -lse2);
-            const int how = mask_of(wl, wh, p.w.sinks, k0 + 32 * u);
-            if (how) mask_scores(s, how, 3, seen, p.w.sinks, k0 + 32 * u, half);
+            if (!all_see(wl, wh, sinks, k0 + 32 * u)) keep(s, seen_bits(seen, sinks, k0 + 32 * u), half);
             float ds[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) ds[i] = exp2_hw(s[i]) * (dp[i] - dsum);
@@ -267,25 +267,28 @@ __global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, 
         }
     }
     if (!live) return;
+    const WinGrad late = arguments_again<WinGrad>();
     const bool odd = not_finite<D>(acc) && in;
-    if (in) store_row16<D>(static_cast<u16*>(p.dq) + at_row(p.dqs, b, hh, qi), half, acc, p.scale);
+    if (in) store_row16<D>(static_cast<u16*>(late.dq) + at_row(late.dqs, b, hh, qi), half, acc, late.scale);
+    const u16* Kl = static_cast<const u16*>(late.k) + at_row(late.ks, b, h, 0);
+    const u16* Vl = static_cast<const u16*>(late.v) + at_row(late.vs, b, h, 0);
     for (uint32_t left = (uint32_t)__ballot(odd); left; left &= left - 1) {
-        const int r = __builtin_ctz(left), i = (w0 + r) / G, head = h * G + (w0 + r) - i * G;
-        const Seen see = seen_by(p, i);
-        const u16* q = static_cast<const u16*>(p.q) + at_row(p.qs, b, head, i);
-        const u16* g = static_cast<const u16*>(p.dout) + at_row(p.gs, b, head, i);
+        const int r = __builtin_ctz(left), i = over(late.group, w0 + r), head = h * (int)late.group.n + (w0 + r) - i * (int)late.group.n;
+        const Seen see = seen_by(late, i);
+        const u16* q = static_cast<const u16*>(late.q) + at_row(late.qs, b, head, i);
+        const u16* g = static_cast<const u16*>(late.dout) + at_row(late.gs, b, head, i);
         const float l = __shfl(lse2, r), dd = __shfl(dsum, r);
         float o[D / 64] = {};
         for (int v = 0; v < tiles.count; ++v) {
             const int key = tiles.at(v) * BN + lane;
-            const bool mine = sees(see, p.w.sinks, key);
+            const bool mine = sees(see, late.w.sinks, key);
             float w = 0.0f, ds = 0.0f;
-            if (mine) pair_by_definition<D>(q, Kh + key * p.ks[2], g, Vh + key * p.vs[2], (double)p.scale * 1.4426950408889634, l, dd, w, ds);
+            if (mine) pair_by_definition<D>(q, Kl + key * late.ks[2], g, Vl + key * late.vs[2], (double)late.scale * 1.4426950408889634, l, dd, w, ds);
             const uint64_t all = __ballot(mine);
             for (int j = 0; j < 64; ++j)
-                if ((all >> j) & 1) add_row<D>(o, __shfl(ds, j), Kh + (long long)(key - lane + j) * p.ks[2]);
+                if ((all >> j) & 1) add_row<D>(o, __shfl(ds, j), Kl + (long long)(key - lane + j) * late.ks[2]);
         }
-        store_lane<D>(static_cast<u16*>(p.dq) + at_row(p.dqs, b, head, i), o, p.scale);
+        store_lane<D>(static_cast<u16*>(late.dq) + at_row(late.dqs, b, head, i), o, late.scale);
     }
 }
 
@@ -353,12 +356,12 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int role = wave >> 2, pair = wave & 3;   // role 0: P and dV; role 1: dS and dK
     const int col = lane & 31, half = lane >> 5;
-    const int G = p.hq / p.hk, groups = p.B * p.hk;
-    const int bh = blockIdx.x % groups, b = bh / p.hk, h = bh - b * p.hk;
+    const int G = (int)p.group.n, item = over(p.per_item, blockIdx.x);
+    const int bh = blockIdx.x - item * (int)p.per_item.n, b = over(p.heads, bh), h = bh - b * p.hk;
     // Items of a head: the parts of every tile's queries whose windows reach it, then
     // the chunks of the far queries of the first keys' tiles, short ones that fill up
     // the last round.
-    const int item = blockIdx.x / groups, near_items = (p.nk + KT - 1) / KT * p.parts;
+    const int near_items = (p.nk + KT - 1) / KT * p.parts;
     const bool far = item >= near_items;
     const int kt = far ? (item - near_items) / p.chunks : item / p.parts;
     const int cuts = far ? p.chunks : p.parts, cut = far ? (item - near_items) % p.chunks : item % p.parts;
@@ -441,13 +444,7 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[4 * g + r] = __builtin_fmaf(s[4 * g + r], c, -lv[r]);
         }
-        if (q0 < all_lo || q0 + 31 > all_hi) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int qi = q0 + (i >> 2) * 8 + 4 * half + (i & 3);
-                if (qi < mine.lo || qi > mine.hi) s[i] = kNegInf;
-            }
-        }
+        if (q0 < all_lo || q0 + 31 > all_hi) keep(s, ones(mine.hi + 1 - q0) & ~ones(mine.lo - q0), half);
         float w[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) w[i] = exp2_hw(s[i]);
@@ -585,40 +582,41 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
     }
     if (!live) return;
 
+    const WinGrad late = arguments_again<WinGrad>();
     // Where this wave's rows go: the gradient, or the sums [2][KT][D] (dV first) of a
     // part or chunk.
-    const bool partial = p.parts > 1 || split;
+    const bool partial = late.parts > 1 || split;
     float* part = nullptr;
-    if (partial) part = p.part + ((first_part(p, sink_tiles, bh, kt) + (far ? p.parts : 0) + cut) * 2 + role) * KT * D;
-    u16* out = role == 0 ? static_cast<u16*>(p.dv) + at_row(p.dvs, b, h, 0) : static_cast<u16*>(p.dk) + at_row(p.dks, b, h, 0);
-    const long long out_row = role == 0 ? p.dvs[2] : p.dks[2];
-    const float mul = role == 0 ? 1.0f : p.scale;
-    const bool odd = not_finite<D>(acc) && key < p.nk;
-    if (key < p.nk) {
+    if (partial) part = late.part + ((first_part(late, sink_tiles, bh, kt) + (far ? late.parts : 0) + cut) * 2 + role) * KT * D;
+    u16* out = role == 0 ? static_cast<u16*>(late.dv) + at_row(late.dvs, b, h, 0) : static_cast<u16*>(late.dk) + at_row(late.dks, b, h, 0);
+    const long long out_row = role == 0 ? late.dvs[2] : late.dks[2];
+    const float mul = role == 0 ? 1.0f : late.scale;
+    const bool odd = not_finite<D>(acc) && key < late.nk;
+    if (key < late.nk) {
         if (partial) store_row16<D>(part + (size_t)(key - k0) * D, half, acc, mul);
         else store_row16<D>(out + key * out_row, half, acc, mul);
     }
     for (uint32_t left = (uint32_t)__ballot(odd); left; left &= left - 1) {
         const int at = w0 + __builtin_ctz(left);
-        const Span span = seen_of_key(p, at);
-        const u16* k = static_cast<const u16*>(p.k) + at_row(p.ks, b, h, at);
-        const u16* v = static_cast<const u16*>(p.v) + at_row(p.vs, b, h, at);
+        const Span span = seen_of_key(late, at);
+        const u16* k = static_cast<const u16*>(late.k) + at_row(late.ks, b, h, at);
+        const u16* v = static_cast<const u16*>(late.v) + at_row(late.vs, b, h, at);
         float o[D / 64] = {};
         Cursor x = start();
         for (int j = 0; j < n_stages; ++j, next(x)) {
             const int qi = x.at * SR + lane;
-            const bool seen = qi < p.nq && qi >= span.lo && qi <= span.hi;
-            const u16* q0 = static_cast<const u16*>(p.q) + at_row(p.qs, b, x.hh, x.at * SR);
-            const u16* g0 = static_cast<const u16*>(p.dout) + at_row(p.gs, b, x.hh, x.at * SR);
+            const bool seen = qi < late.nq && qi >= span.lo && qi <= span.hi;
+            const u16* q0 = static_cast<const u16*>(late.q) + at_row(late.qs, b, x.hh, x.at * SR);
+            const u16* g0 = static_cast<const u16*>(late.dout) + at_row(late.gs, b, x.hh, x.at * SR);
             float w = 0.0f, ds = 0.0f;
             if (seen) {
-                const size_t stat = ((size_t)b * p.hq + x.hh) * p.nq + qi;
-                pair_by_definition<D>(q0 + lane * p.qs[2], k, g0 + lane * p.gs[2], v, (double)p.scale * 1.4426950408889634,
-                                      p.lse[stat] * kLog2e, p.dsum[stat], w, ds);
+                const size_t stat = ((size_t)b * late.hq + x.hh) * late.nq + qi;
+                pair_by_definition<D>(q0 + lane * late.qs[2], k, g0 + lane * late.gs[2], v, (double)late.scale * 1.4426950408889634,
+                                      late.lse[stat] * kLog2e, late.dsum[stat], w, ds);
             }
             const uint64_t all = __ballot(seen);
             for (int i = 0; i < 64; ++i)
-                if ((all >> i) & 1) add_row<D>(o, __shfl(role == 0 ? w : ds, i), role == 0 ? g0 + i * p.gs[2] : q0 + i * p.qs[2]);
+                if ((all >> i) & 1) add_row<D>(o, __shfl(role == 0 ? w : ds, i), role == 0 ? g0 + i * late.gs[2] : q0 + i * late.qs[2]);
         }
         if (partial) {
             for (int e = 0; e < D / 64; ++e) part[(size_t)(at - k0) * D + (D / 64) * lane + e] = o[e] * mul;
@@ -655,8 +653,11 @@ __global__ __launch_bounds__(256) void win_join_kernel(WinGrad p, int tiles, int
 }
 
 template <int D>
-hipError_t go(const WinGrad& p, hipStream_t stream) {
+hipError_t go(WinGrad p, hipStream_t stream) {
     const int groups = p.B * p.hk;
+    p.per_item = div_by(groups);
+    p.heads = div_by(p.hk);
+    if (p.hq > 0) p.group = div_by(p.hq / p.hk);   // else 0: no queries
     const float c = p.scale * kLog2e;
     if (p.nq > 0 && p.hq > 0) {
         const long long rows = (long long)p.nq * (p.hq / p.hk);

@@ -40,6 +40,8 @@ __device__ __forceinline__ void bf16_terms(float a, float b, uint32_t (&w)[TERMS
     }
 }
 
+__device__ __forceinline__ int over(const Div& d, int x) { return (int)(__umulhi((uint32_t)x << 1, d.m) >> d.shift); }
+
 // New tokens of sequence b, its length, and the tokens that the pages have room
 // for at most.
 __device__ __forceinline__ int new_tokens(const int* new_lens, int b, int n) {
@@ -82,42 +84,48 @@ __device__ __forceinline__ bool sees(const Seen& s, int sinks, int key) {
 }
 __device__ __forceinline__ bool sees_any(const Seen& s, int sinks) { return s.hi > 0 && (s.lo < s.hi || sinks > 0); }
 
-// What is to be masked of 32 keys from k0 on for rows of which the first sees wl and
-// the last wh (uniform): nothing, keys behind a row's end, keys before its window,
-// or all of it.
-enum { MASK_NONE, MASK_END = 1, MASK_BEGIN = 2, MASK_ALL = 4 };
-__device__ __forceinline__ int mask_of(const Seen& wl, const Seen& wh, int sinks, int k0) {
-    const bool end = k0 + 32 > wl.hi, begin = k0 < wh.lo && k0 + 32 > sinks;
-    if (begin && k0 < sinks) return MASK_ALL;
-    return (end ? MASK_END : 0) | (begin ? MASK_BEGIN : 0);
+// Bits 0 .. n - 1.
+__device__ __forceinline__ uint32_t ones(int n) { return (uint32_t)(0xffffffffull >> (32 - min(max(n, 0), 32))); }
+
+// Bit k: the row sees key k0 + k.
+__device__ __forceinline__ uint32_t seen_bits(const Seen& s, int sinks, int k0) {
+    return ones(s.hi - k0) & (~ones(s.lo - k0) | ones(sinks - k0));
 }
-// Whether any of these rows sees one of the 32 keys.
-__device__ __forceinline__ bool any_of(const Seen& wl, const Seen& wh, int sinks, int k0) {
+
+// Of rows the first of which sees wl and the last wh (uniform): whether all of them see
+// all of the 32 keys from k0 on, and whether any of them sees one.
+__device__ __forceinline__ bool all_see(const Seen& wl, const Seen& wh, int sinks, int k0) {
+    return k0 + 32 <= wl.hi && (k0 >= wh.lo || k0 + 32 <= sinks);
+}
+__device__ __forceinline__ bool any_sees(const Seen& wl, const Seen& wh, int sinks, int k0) {
     return k0 < wh.hi && (k0 + 32 > wl.lo || k0 < sinks);
 }
 
-// Masks the scores x of a lane's row in a 32x32 accumulator: element i is key k0 +
-// 8 (i / 4) + 4 half + i % 4.  have: bit t: the t-th 16 keys have a page.
-__device__ __forceinline__ void mask_scores(f32x16& x, int how, int have, const Seen& seen, int sinks, int k0, int half) {
-    const int at = k0 + 4 * half, hi = seen.hi - at, lo = seen.lo - at;
-    if ((how & MASK_ALL) || have != 3) {
+// Makes -inf of the scores in a 32x32 accumulator whose bit is not set; element i is
+// bit 8 (i / 4) + 4 half + i % 4.  Two instructions each, whatever is masked.  (Written
+// as comparisons they became a branch per element: a causal window of 512 over 4096
+// tokens 120.3 us, so 118.8.)
+__device__ __forceinline__ void keep(f32x16& x, uint32_t bits, int half) {
+    bits >>= 4 * half;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int k = (i >> 2) * 8 + (i & 3);
-            if (!((have >> (i >> 3)) & 1) || !(k < hi && (k >= lo || at + k < sinks))) x[i] = kNegInf;
-        }
-        return;
+    for (int i = 0; i < 16; ++i) {
+        const uint32_t all = (uint32_t)((int)(bits << (31 - 8 * (i >> 2) - (i & 3))) >> 31);
+        x[i] = __uint_as_float((__float_as_uint(x[i]) & all) | (0xff800000u & ~all));
     }
-    if (how & MASK_END) {
+}
+
+// The launch's arguments once more, from where they came: what is used behind a loop
+// then need not be kept in scalar registers during it.  T: the kernel's first argument.
+template <typename T>
+__device__ __forceinline__ T arguments_again() {
+    static_assert(sizeof(T) % 8 == 0, "read as words");
+    typedef const __attribute__((address_space(4))) unsigned long long* words;
+    words w = (words)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(w));
+    struct { unsigned long long x[sizeof(T) / 8]; } raw;
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if ((i >> 2) * 8 + (i & 3) >= hi) x[i] = kNegInf;
-    }
-    if (how & MASK_BEGIN) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if ((i >> 2) * 8 + (i & 3) < lo) x[i] = kNegInf;
-    }
+    for (unsigned i = 0; i < sizeof(T) / 8; ++i) raw.x[i] = w[i];
+    return __builtin_bit_cast(T, raw);
 }
 
 // The tiles of T keys that any of the rows from `first` to `last` (positions in

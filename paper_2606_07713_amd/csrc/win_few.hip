@@ -69,19 +69,16 @@ __global__ __launch_bounds__(WAVES * 64, RT == 1 ? 2 : 1) void win_few_kernel(Wi
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
     const KeySource& src = p.s;
-    const int G = p.hq / p.hk;
+    const int G = (int)p.group.n;
     // Row tiles last, those of the highest positions first.
-    int blk = blockIdx.x;
-    const int groups = p.B * p.hk * p.splits, rt = row_tiles - 1 - blk / groups;
-    blk %= groups;
-    const int sp = blk % p.splits; blk /= p.splits;
-    const int h = blk % p.hk, b = blk / p.hk;
+    const int up = over(p.per_tile, blockIdx.x), rt = row_tiles - 1 - up, in_tile = blockIdx.x - up * (int)p.per_tile.n;
+    const int bh = over(p.per_head, in_tile), sp = in_tile - bh * p.splits, b = over(p.heads, bh), h = bh - b * p.hk;
 
     const int count = new_tokens(src.new_lens, b, p.n), rows = count * G, row0 = rt * ROWS;
     if (row0 >= rows) return;
     const int len = length(src, b), end = max(0, min(len, capacity(src)));
     const long long first = (long long)len - count;   // position of query 0
-    const auto seen_of = [&](int row) { return seen_from(p.w, first + row / G, end); };
+    const auto seen_of = [&](int row) { return seen_from(p.w, first + over(p.group, row), end); };
     // Rows behind the last one are computed as it is, with queries of zero, and not stored.
     Seen seen[RT];
 #pragma unroll
@@ -97,7 +94,7 @@ __global__ __launch_bounds__(WAVES * 64, RT == 1 ? 2 : 1) void win_few_kernel(Wi
     for (int i = 0; i < RT; ++i) {
         const int row = row0 + 16 * i + n;
         const bool in = row < rows;
-        const int qi = in ? row / G : 0, hh = h * G + (in ? row - qi * G : 0);
+        const int qi = in ? over(p.group, row) : 0, hh = h * G + (in ? row - qi * G : 0);
         const u16* at = static_cast<const u16*>(p.q) + b * p.qs[0] + hh * p.qs[1] + qi * p.qs[2] + g * 8;
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
@@ -287,7 +284,7 @@ __global__ __launch_bounds__(WAVES * 64, RT == 1 ? 2 : 1) void win_few_kernel(Wi
             f[0] += u.x; f[1] += u.y; f[2] += u.z; f[3] += u.w;
             f[4] += v.x; f[5] += v.y; f[6] += v.z; f[7] += v.w;
         }
-        const int qi = row / G, hh = h * G + row - qi * G;
+        const int qi = over(p.group, row), hh = h * G + row - qi * G;
         // Sums that are not finite, or none at all in a row that sees keys: by the definition.
         float zero = 0.0f * L;
 #pragma unroll
@@ -321,7 +318,7 @@ __global__ __launch_bounds__(WAVES * 64, RT == 1 ? 2 : 1) void win_few_kernel(Wi
     __syncthreads();
     for (int r = wave; r < ROWS; r += WAVES) {
         if (!again[r]) continue;
-        const int row = row0 + r, qi = row / G, hh = h * G + row - qi * G;
+        const int row = row0 + r, qi = over(p.group, row), hh = h * G + row - qi * G;
         float f[D / 64], M, L;
         row_by_definition<D, T>(p, b, h, static_cast<const u16*>(p.q) + b * p.qs[0] + hh * p.qs[1] + qi * p.qs[2],
                                 seen_of(row), steps, begin, stop, p.splits > 1, f, M, L);
@@ -330,7 +327,8 @@ __global__ __launch_bounds__(WAVES * 64, RT == 1 ? 2 : 1) void win_few_kernel(Wi
 }
 
 template <int D, int RT>
-hipError_t go(const WinAttn& p, hipStream_t stream) {
+hipError_t go(WinAttn p, hipStream_t stream) {
+    set_divisions(p);
     const int rows = p.n * (p.hq / p.hk), tiles = (rows + 16 * RT - 1) / (16 * RT);
     // A negative scale goes into the queries' signs; a factor of zero becomes the
     // smallest one there is (kernels here keep subnormal numbers), whose weights

@@ -56,20 +56,17 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const KeySource& src = p.s;
-    const int G = p.hq / p.hk;
+    const int G = (int)p.group.n;
     // Row tiles last, those of the highest positions first; the heads next to each
     // other, so that the row tiles of a head mostly go to one XCD.
-    int blk = blockIdx.x;
-    const int groups = p.B * p.hk * p.splits, rt = row_tiles - 1 - blk / groups;
-    blk %= groups;
-    const int sp = blk % p.splits; blk /= p.splits;
-    const int h = blk % p.hk, b = blk / p.hk;
+    const int up = over(p.per_tile, blockIdx.x), rt = row_tiles - 1 - up, in_tile = blockIdx.x - up * (int)p.per_tile.n;
+    const int bh = over(p.per_head, in_tile), sp = in_tile - bh * p.splits, b = over(p.heads, bh), h = bh - b * p.hk;
 
     const int count = new_tokens(src.new_lens, b, p.n), rows = count * G, row0 = rt * MROWS;
     if (row0 >= rows) return;
     const int len = length(src, b), end = max(0, min(len, capacity(src)));
     const long long first = (long long)len - count;   // position of query 0
-    const auto seen_of = [&](int row) { return seen_from(p.w, first + row / G, end); };
+    const auto seen_of = [&](int row) { return seen_from(p.w, first + over(p.group, row), end); };
     const auto uniform = [](Seen s) {
         return Seen{__builtin_amdgcn_readfirstlane(s.lo), __builtin_amdgcn_readfirstlane(s.hi)};
     };
@@ -80,12 +77,13 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
     // This wave's rows.
     const int w0 = row0 + wave * 32, row = w0 + col;
     const bool live = w0 < rows, in = row < rows;
+    const int sinks = p.w.sinks;
     const Seen wl = uniform(seen_of(min(w0, rows - 1))), wh = uniform(seen_of(min(w0 + 32, rows) - 1));
     const Seen seen = seen_of(min(row, rows - 1));
 
     bf16x8 qf[D / 16];
     {
-        const int qi = in ? row / G : 0, hh = h * G + (in ? row - qi * G : 0);
+        const int qi = in ? over(p.group, row) : 0, hh = h * G + (in ? row - qi * G : 0);
         const u16* at = static_cast<const u16*>(p.q) + b * p.qs[0] + hh * p.qs[1] + qi * p.qs[2] + half * 8;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
@@ -161,14 +159,18 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
         if (!live) return;
 #pragma unroll
         for (int sb = 0; sb < BN / SN; ++sb) {
-            if (!any_of(wl, wh, p.w.sinks, k0 + sb * SN)) continue;
+            if (!any_sees(wl, wh, sinks, k0 + sb * SN)) continue;
             f32x16 s = f32x16{};
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                     *reinterpret_cast<const bf16x8*>(ks + kaddr[k] + sb * SN * RB), qf[k], s, 0, 0, 0);
-            const int how = mask_of(wl, wh, p.w.sinks, k0 + sb * SN), pages = (have >> (2 * sb)) & 3;
-            if (how || pages != 3) mask_scores(s, how, pages, seen, p.w.sinks, k0 + sb * SN, half);
+            const int paged = (have >> (2 * sb)) & 3;
+            if (paged != 3 || !all_see(wl, wh, sinks, k0 + sb * SN)) {
+                uint32_t bits = seen_bits(seen, sinks, k0 + sb * SN);
+                if (paged != 3) bits &= (paged & 1 ? 0x0000ffffu : 0u) | (paged & 2 ? 0xffff0000u : 0u);
+                keep(s, bits, half);
+            }
             const auto raise = [&]() __attribute__((always_inline)) {
                 float m = kNegInf;
                 asm volatile("" : "+v"(m));   // not hoisted onto the fast path
@@ -243,6 +245,7 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
     }
     __syncthreads();   // every wave is done with the stages
     if (!live) return;
+    const WinAttn late = arguments_again<WinAttn>();
 
     // O = acc / l (or the sums as they are) through a 32-row slice of the stages,
     // whole rows per store.
@@ -257,14 +260,14 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
 #pragma unroll
         for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(oacc[d][i], 0.0f, zero);
     zero = half_sum(zero);
-    const bool odd = in && (!(zero == 0.0f) || (total == 0.0f && begin < stop && sees_any(seen, p.w.sinks)));
+    const bool odd = in && (!(zero == 0.0f) || (total == 0.0f && begin < stop && sees_any(seen, sinks)));
     int ln = lane;
     asm volatile("" : "+v"(ln));   // staging addresses are formed here, not above the loop
     const int cl = ln & 31, hf = ln >> 5;
     // Row r of this wave's 32: its query head and query.
     const auto place = [&](int r, int& hh, int& qi) {
-        qi = (w0 + r) / G;
-        hh = h * G + (w0 + r) - qi * G;
+        qi = over(late.group, w0 + r);
+        hh = h * (int)late.group.n + (w0 + r) - qi * (int)late.group.n;
     };
     if constexpr (OUT == TO_BF16) {
         constexpr int CHK = C::CHUNKS, RPI = 64 / CHK;
@@ -286,7 +289,7 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
             if (w0 + r >= rows) continue;
             int hh, qi;
             place(r, hh, qi);
-            *reinterpret_cast<uint4*>(static_cast<u16*>(p.o) + b * p.os[0] + hh * p.os[1] + qi * p.os[2] + ch * 8) = x;
+            *reinterpret_cast<uint4*>(static_cast<u16*>(late.o) + b * late.os[0] + hh * late.os[1] + qi * late.os[2] + ch * 8) = x;
         }
     } else {
         // fp32 rows in two passes of D / 2 columns
@@ -312,8 +315,8 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
                 int hh, qi;
                 place(r, hh, qi);
                 float* to;
-                if constexpr (OUT == TO_STATE) to = p.ws + ((((size_t)b * p.hq + hh) * p.n + qi) * p.splits + sp) * D;
-                else to = static_cast<float*>(p.o) + b * p.os[0] + hh * p.os[1] + qi * p.os[2];
+                if constexpr (OUT == TO_STATE) to = late.ws + ((((size_t)b * late.hq + hh) * late.n + qi) * late.splits + sp) * D;
+                else to = static_cast<float*>(late.o) + b * late.os[0] + hh * late.os[1] + qi * late.os[2];
                 *reinterpret_cast<float4*>(to + u * (D / 2) + ch * 4) = x;
             }
             pf::wait_lgkmcnt0();
@@ -322,13 +325,13 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
     if (half == 0 && in) {
         int hh, qi;
         place(col, hh, qi);
-        const size_t at = ((size_t)b * p.hq + hh) * p.n + qi;
+        const size_t at = ((size_t)b * late.hq + hh) * late.n + qi;
         if constexpr (OUT == TO_STATE) {
-            float* ml = p.ws + (size_t)p.B * p.hq * p.n * p.splits * D + (at * p.splits + sp) * 2;
+            float* ml = late.ws + (size_t)late.B * late.hq * late.n * late.splits * D + (at * late.splits + sp) * 2;
             ml[0] = ref;
             ml[1] = total;
         } else {
-            if (p.lse) p.lse[at] = none ? kNegInf : (ref + __log2f(total)) * kLn2;
+            if (late.lse) late.lse[at] = none ? kNegInf : (ref + __log2f(total)) * kLn2;
         }
     }
     // Rows that have to be done by their definition.
@@ -337,14 +340,15 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
         const int r = __builtin_ctz(left);
         place(r, hh, qi);
         float f[D / 64], M, L;
-        row_by_definition<D, BN>(p, b, h, static_cast<const u16*>(p.q) + b * p.qs[0] + hh * p.qs[1] + qi * p.qs[2],
+        row_by_definition<D, BN>(late, b, h, static_cast<const u16*>(late.q) + b * late.qs[0] + hh * late.qs[1] + qi * late.qs[2],
                                  seen_of(w0 + r), tiles, begin, stop, OUT == TO_STATE, f, M, L);
-        store_row<D>(p, b, hh, qi, sp, f, M, L);
+        store_row<D>(late, b, hh, qi, sp, f, M, L);
     }
 }
 
 template <int D>
-hipError_t go(const WinAttn& p, hipStream_t stream) {
+hipError_t go(WinAttn p, hipStream_t stream) {
+    set_divisions(p);
     const long long rows = (long long)p.n * (p.hq / p.hk);
     const int tiles = (int)((rows + MROWS - 1) / MROWS);
     // As in the kernel of few rows.
