@@ -9,9 +9,13 @@
 // rows, which lie in one page whatever its size.  Only tiles that a row of the
 // workgroup sees are walked: those of the first visible keys, then the windows'.
 //
-// Softmax: a running reference per row, the maximum of the first tile that it
-// sees; later ones are weighed against it as they come, and it is raised where a
-// lane's sum of 32 keys exceeds 2^20.  The sums are of the fp32 weights.  A weight
+// Softmax: one reference per row, the largest score of the first 32 keys of which it
+// sees any; all others are weighed against it as they come.  fp32 and bf16 hold
+// weights up to 2^127 as well as small ones, so the reference need not follow the
+// maximum: only a row whose scores rise by more than 127 log2 units (88 of the
+// exponent) above it comes out infinite, and is done by the definition.  (Raised in
+// the loop where sums grew, the rarely taken branch cost a copy of all sums in every
+// step: 4096 tokens in a window of 512, 114 us.)  The sums are of the fp32 weights.  A weight
 // meets V as one bf16 number for a bf16 output (2^-9 each, which leaves the error
 // of a bf16 output at 1.4 times its own rounding's), as three for an fp32 output
 // (two left it at 2.3e-6, nine times what fp32 sums alone make).
@@ -171,45 +175,32 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
                 if (paged != 3) bits &= (paged & 1 ? 0x0000ffffu : 0u) | (paged & 2 ? 0xffff0000u : 0u);
                 keep(s, bits, half);
             }
-            const auto raise = [&]() __attribute__((always_inline)) {
+            // Rows that see their first keys here take their reference from them.
+            if (wave_any(ref == kNegInf)) {
                 float m = kNegInf;
-                asm volatile("" : "+v"(m));   // not hoisted onto the fast path
 #pragma unroll
                 for (int i = 0; i < 16; ++i) m = fmaxf(m, s[i]);
-                m = fmaxf(ref, half_max(m) * c);
-                const float a = ref == kNegInf ? 0.0f : exp2_hw(ref - m);
-                l *= a;
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d) oacc[d] *= a;
-                ref = m;
-                neg = m == kNegInf ? 0.0f : -m;
-            };
-            u32x4 pt[SN / 16][TERMS];
-            const auto weights = [&]() __attribute__((always_inline)) {
-                float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-                for (int g = 0; g < SN / 16; ++g) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int i = g * 8 + 2 * j;
-                        const float a = exp2_hw(__builtin_fmaf(s[i], c, neg)), d = exp2_hw(__builtin_fmaf(s[i + 1], c, neg));
-                        sum[0] += a;
-                        sum[1] += d;
-                        uint32_t x[TERMS];
-                        bf16_terms<TERMS>(a, d, x);
-#pragma unroll
-                        for (int k = 0; k < TERMS; ++k) pt[g][k][j] = x[k];
-                    }
-                }
-                return sum[0] + sum[1];
-            };
-            if (wave_any(ref == kNegInf)) raise();
-            float part = weights();
-            if (wave_any(!(part <= pf::kFastSumLimit))) {
-                raise();
-                part = weights();
+                m = half_max(m) * c;
+                ref = ref == kNegInf ? m : ref;
+                neg = ref == kNegInf ? 0.0f : -ref;
             }
-            l += part;
+            u32x4 pt[SN / 16][TERMS];
+            float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int g = 0; g < SN / 16; ++g) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = g * 8 + 2 * j;
+                    const float a = exp2_hw(__builtin_fmaf(s[i], c, neg)), d = exp2_hw(__builtin_fmaf(s[i + 1], c, neg));
+                    sum[0] += a;
+                    sum[1] += d;
+                    uint32_t x[TERMS];
+                    bf16_terms<TERMS>(a, d, x);
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) pt[g][k][j] = x[k];
+                }
+            }
+            l += sum[0] + sum[1];
 #pragma unroll
             for (int cc = 0; cc < SN / 16; ++cc)
 #pragma unroll
