@@ -4,9 +4,9 @@
 // one of the G = Hq/Hk heads that share it, query by query: keys and values are
 // read once for all of them, and 128 rows are only 128/G positions wide, so that
 // a window's ragged ends cost little.  K and V stream through a two-stage LDS ring
-// in 64-key tiles, one barrier per tile, in the layout and with the products of
-// the prefill kernels (prefill_bf16_common.h).  Each wave loads 16 of a tile's
-// rows, which lie in one page whatever its size.  Only tiles that a row of the
+// in tiles of 64 or 32 keys, one barrier per tile, in the layout and with the products of
+// the prefill kernels (prefill_bf16_common.h).  Each wave loads 16 or 8 of a
+// tile's rows, which lie in one page whatever its size.  Only tiles that a row of the
 // workgroup sees are walked: those of the first visible keys, then the windows'.
 //
 // Softmax: one reference per row, the largest score of the first 32 keys of which it
@@ -29,7 +29,6 @@ namespace moa {
 namespace {
 
 using namespace win;
-using pf::BN;
 using pf::Cfg;
 using pf::dv_of;
 using pf::lds_v4s;
@@ -42,17 +41,20 @@ constexpr int MROWS = MW * 32;   // rows per workgroup
 // How O leaves: bf16, fp32, or the fp32 state of a split.
 enum { TO_BF16, TO_F32, TO_STATE };
 
-template <int D, int OUT, int TERMS>
-__global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(WinAttn p, float c, uint32_t qflip, int row_tiles) {
+template <int D, int OUT, int TERMS, int BN>
+__global__ __launch_bounds__(MW * 64, D == 64 || BN == 32 ? 3 : 2) void win_many_kernel(WinAttn p, float c, uint32_t qflip, int row_tiles) {
     using C = Cfg<D>;
     constexpr uint32_t RB = C::ROW_BYTES;
     constexpr int SN = 32;                                // keys per step
-    constexpr int LPW = C::TILE_BYTES / (MW * 1024);      // 16-byte loads per lane per tile
+    constexpr int TILE = BN * C::ROW_BYTES;
+    constexpr int LPW = TILE / (MW * 1024);               // 16-byte loads per lane per tile
+    constexpr int RPW = BN / MW, GROUPS = BN / 16;        // rows that a wave loads, page groups of a tile
+    constexpr int ALL = (1 << GROUPS) - 1;
     // One array per ring stage: the compiler tracks direct-to-LDS loads per object.
-    __shared__ __attribute__((aligned(1024))) unsigned char k_st0[C::TILE_BYTES];
-    __shared__ __attribute__((aligned(1024))) unsigned char k_st1[C::TILE_BYTES];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_st0[C::TILE_BYTES];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_st1[C::TILE_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char k_st0[TILE];
+    __shared__ __attribute__((aligned(1024))) unsigned char k_st1[TILE];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_st0[TILE];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_st1[TILE];
     using S0 = std::integral_constant<int, 0>;
     using S1 = std::integral_constant<int, 1>;
 
@@ -104,13 +106,13 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
         const int slot = (wave * LPW + i) * 64 + lane;
         const int r = slot / C::CHUNKS, ch = slot % C::CHUNKS;
         const uint32_t chunk = (uint32_t)((ch ^ swz<D>(r)) * 16);
-        ld_koff[i] = (uint32_t)(r & 15) * krb + chunk;   // this wave's 16 rows of the tile
-        ld_voff[i] = (uint32_t)(r & 15) * vrb + chunk;
+        ld_koff[i] = (uint32_t)(r % RPW) * krb + chunk;   // this wave's rows of the tile
+        ld_voff[i] = (uint32_t)(r % RPW) * vrb + chunk;
     }
-    // Lane 4 i + t holds the page of 16-key group t of the i-th tile from `known` on.
+    // Lane GROUPS i + t holds the page of 16-key group t of the i-th tile from `known` on.
     int pages = 0, known = begin;
     const auto look = [&]() {
-        const int v = known + (lane >> 2), key = tiles.at(v) * BN + 16 * (lane & 3);
+        const int v = known + lane / GROUPS, key = tiles.at(v) * BN + 16 * (lane % GROUPS);
         pages = v < stop && key < end ? page_of(src, b, key) : -1;
     };
     // Starts the loads of the v-th tile; bit t of the result: group t has a page.
@@ -118,13 +120,13 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
     auto issue = [&](int v, auto stage) __attribute__((always_inline)) -> int {
         unsigned char* ks = decltype(stage)::value == 0 ? k_st0 : k_st1;
         unsigned char* vs = decltype(stage)::value == 0 ? v_st0 : v_st1;
-        if (v - known == 16) {
+        if (v - known == 64 / GROUPS) {
             known = v;
             look();
         }
-        const int i = v - known, key = tiles.at(v) * BN + 16 * wave;
-        const int page = __builtin_amdgcn_readlane(pages, 4 * i + wave);
-        const int n = page >= 0 ? max(0, min(16, end - key)) : 0;
+        const int i = v - known, key = tiles.at(v) * BN + RPW * wave;
+        const int page = __builtin_amdgcn_readlane(pages, GROUPS * i + wave * RPW / 16);
+        const int n = page >= 0 ? max(0, min(RPW, end - key)) : 0;
         const u16* kb = static_cast<const u16*>(src.k) + (n ? key_offset(src.ks, src.shift, page, h, key) : 0);
         const u16* vb = static_cast<const u16*>(src.v) + (n ? key_offset(src.vs, src.shift, page, h, key) : 0);
         const auto rk = make_rsrc(kb, rows_extent(n, krb, RB)), rv = make_rsrc(vb, rows_extent(n, vrb, RB));
@@ -132,7 +134,7 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
         for (int j = 0; j < LPW; ++j) buffer_load16_to_lds(rk, ks + (wave * LPW + j) * 1024, ld_koff[j]);
 #pragma unroll
         for (int j = 0; j < LPW; ++j) buffer_load16_to_lds(rv, vs + (wave * LPW + j) * 1024, ld_voff[j]);
-        return (int)(__ballot(pages >= 0) >> (4 * i)) & 15;
+        return (int)(__ballot(pages >= 0) >> (GROUPS * i)) & ALL;
     };
     uint32_t kaddr[D / 16], vaddr[D / 32][2];
 #pragma unroll
@@ -240,7 +242,8 @@ __global__ __launch_bounds__(MW * 64, (D == 64 ? 3 : 2)) void win_many_kernel(Wi
 
     // O = acc / l (or the sums as they are) through a 32-row slice of the stages,
     // whole rows per store.
-    unsigned char* stg = (wave < 2 ? k_st0 : k_st1) + (wave & 1) * 32 * RB;
+    constexpr int SLICES = BN / 32;   // of one stage
+    unsigned char* stg = (wave / SLICES == 0 ? k_st0 : wave / SLICES == 1 ? k_st1 : wave / SLICES == 2 ? v_st0 : v_st1) + wave % SLICES * 32 * RB;
     const float total = half_sum(l);
     const bool none = ref == kNegInf;   // no visible key
     const float inv = OUT == TO_STATE ? 1.0f : none ? 0.0f : 1.0f / total;
@@ -351,8 +354,14 @@ hipError_t go(WinAttn p, hipStream_t stream) {
     const auto run = [&](auto kernel) {
         return launch_kernel(kernel, dim3((unsigned)blocks), dim3(MW * 64), stream, p, c, flip, tiles);
     };
-    if (p.splits == 1) return p.out_bf16 ? run(win_many_kernel<D, TO_BF16, 1>) : run(win_many_kernel<D, TO_F32, 3>);
-    const hipError_t e = p.out_bf16 ? run(win_many_kernel<D, TO_STATE, 1>) : run(win_many_kernel<D, TO_STATE, 3>);
+    // At d = 128 two workgroups with 64-key tiles fit a compute unit, and three with
+    // tiles of 32, which wait for each other less but have twice the barriers: for more
+    // workgroups than two for every unit (4096 tokens in a window of 512, 2048 of them
+    // 100 -> 94 us, 8192 in 1024 176 -> 166; 504 of 200 queries on 20011 keys 85 -> 90).
+    if constexpr (D == 128)
+        if (p.splits == 1 && blocks > 512) return p.out_bf16 ? run(win_many_kernel<D, TO_BF16, 1, 32>) : run(win_many_kernel<D, TO_F32, 3, 32>);
+    if (p.splits == 1) return p.out_bf16 ? run(win_many_kernel<D, TO_BF16, 1, 64>) : run(win_many_kernel<D, TO_F32, 3, 64>);
+    const hipError_t e = p.out_bf16 ? run(win_many_kernel<D, TO_STATE, 1, 64>) : run(win_many_kernel<D, TO_STATE, 3, 64>);
     if (e != hipSuccess) return e;
     const SplitJoin j{p.ws, p.o, p.lse, p.s.new_lens, {p.os[0], p.os[1], p.os[2]}, p.B, p.hq, p.n, p.splits, p.out_bf16};
     return launch_split_join<D>(j, stream);
