@@ -54,14 +54,16 @@ int64_t span(const Sizes& s) {
 // Key splits, by an estimate of the call's microseconds.  A workgroup walks over
 // `steps` tiles (of 64 keys with many rows; of 128, four waves' 32, with few), and
 // beginning and ending cost it two more.  A tile takes the longer the more workgroups
-// share a compute unit; more than `most` run one after the other.  Few rows also wait
-// for the memory.  The join reads what the splits wrote, a latency more beyond 32 of
-// them.  (Measured, splits:us.  Many rows: 32 heads on 8, 200 of 20011 keys, d = 128
-// 1:694 4:195 8:126 9:116 12:153; 8 on 2, 4 x 1000, d = 64 1:27 2:33 4:32; 8 heads, 500
-// of 4096, d = 128 4:51 8:36 12:39; 12 on 4, 2 x 700 of 5000, d = 64 1:113 3:60 5:52
-// 6:61.  Few: 32 on 8, one query of 4097, d = 128 1:41 8:17 17:12 32:11 64:14; of 16384
-// 1:193 16:24 32:17 43:23; 8 on 1, 32 x 3 of 9000 4:47 8:35 15:44; 12 on 4, 16 x 4 in
-// a window of 1024, d = 64 1:12.7 4:11.3 5:13.3 16:15.)
+// share a compute unit; more than `most` run one after the other.  With many rows and
+// one workgroup for a unit its two key streams take a tile each at a time.  Few rows
+// also wait for the memory.  The join reads what the splits wrote, a latency more
+// beyond 32 of them.  (Measured, splits:us.  Many rows: 32 heads on 8, 200 of 20011
+// keys, d = 128 1:310 4:95 8:94 9:89 12:110; 8 on 2, 4 x 1000, d = 64 1:16 2:30 4:29;
+// 8 heads, 500 of 4096, d = 128 4:31 8:25 12:33; 12 on 4, 2 x 700 of 5000, d = 64 1:58
+// 3:50 5:46 8:51; 32 on 8, 300 in a window of 1024 1:25 3:27 5:26.  Few: 32 on 8, one
+// query of 4097, d = 128 1:42 8:16 16:13 32:11 64:13; of 16384 1:195 16:24 32:17 48:21;
+// 8 on 1, 32 x 3 of 9000 4:46 8:34 16:43; 12 on 4, 16 x 4 in a window of 1024, d = 64
+// 1:11.3 4:10.6 6:12.7 16:14.)
 int pick_splits(const Sizes& s, int requested) {
     if (!s.any()) return 1;
     if (requested > 0) return requested;
@@ -73,10 +75,13 @@ int pick_splits(const Sizes& s, int requested) {
     const auto tile = [&](int64_t at_once) { return at_once ? one * (1 + more * (double)(at_once - 1)) : 0.0; };
     int best = 1;
     double least = 0;
-    for (int64_t k = 1; k <= kMaxSplits && k <= all && (k == 1 || k * blocks <= 2048); ++k) {
+    for (int64_t k = 1; k <= 128 && k <= all && (k == 1 || k * blocks <= 1024); ++k) {
         const int64_t each = (k * blocks + 255) / 256;   // workgroups of a compute unit
         const double walk = (double)(each / most) * tile(most) + tile(each % most);
-        double cost = few ? walk * ((double)all / (double)k + 2.5) + memory : walk * (double)((all + k - 1) / k + 2);
+        const int64_t steps = (all + k - 1) / k;
+        double cost = few ? walk * ((double)all / (double)k + 2.5) + memory
+                    : each == 1 ? tile(2) * (double)((steps + 1) / 2 + 2)   // two key streams
+                                : walk * (double)(steps + 2);
         if (k > 1) cost += 3 + rows * ((double)k * (double)(s.d + 2) * 8 / 5e6 + 1.0 / 8000) + 3 * (double)((k - 1) / 32);
         if (k == 1 || cost < least) {
             best = (int)k;

@@ -125,20 +125,22 @@ __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[D / 32]) {
 constexpr int QW = 4;            // waves
 constexpr int QROWS = QW * 32;   // rows per workgroup
 
-template <int D>
-__global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, int row_tiles) {
+template <int D, int KS>
+__global__ __launch_bounds__(KS * QW * 64, 2) void win_dq_kernel(WinGrad p, float c, int row_tiles) {
     using C = Cfg<D>;
     constexpr uint32_t RB = C::ROW_BYTES;
     constexpr int LPW = C::TILE_BYTES / (QW * 1024);
-    __shared__ __attribute__((aligned(1024))) unsigned char k_st0[C::TILE_BYTES];
-    __shared__ __attribute__((aligned(1024))) unsigned char k_st1[C::TILE_BYTES];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_st0[C::TILE_BYTES];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_st1[C::TILE_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char k_st0[KS][C::TILE_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char k_st1[KS][C::TILE_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_st0[KS][C::TILE_BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_st1[KS][C::TILE_BYTES];
     using S0 = std::integral_constant<int, 0>;
     using S1 = std::integral_constant<int, 1>;
 
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Waves QW .. of two key streams hold the rows of waves 0 .. and take every second tile.
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % QW;
+    const int stream = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / QW;
     const int col = lane & 31, half = lane >> 5;
     const int G = (int)p.group.n, up = over(p.per_item, blockIdx.x), rt = row_tiles - 1 - up;
     const int bh = blockIdx.x - up * (int)p.per_item.n, b = over(p.heads, bh), h = bh - b * p.hk;
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, 
         }
     }
     dsum = half_sum(dsum);
-    if (in && half == 0) p.dsum[stat] = dsum;
+    if (in && half == 0 && stream == 0) p.dsum[stat] = dsum;
 
     const u16* Kh = static_cast<const u16*>(p.k) + at_row(p.ks, b, h, 0);
     const u16* Vh = static_cast<const u16*>(p.v) + at_row(p.vs, b, h, 0);
@@ -209,8 +211,8 @@ __global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, 
         voff[i] = (uint32_t)(r & 15) * vrb + chunk;
     }
     auto issue = [&](int v, auto stage) __attribute__((always_inline)) {
-        unsigned char* ks = decltype(stage)::value == 0 ? k_st0 : k_st1;
-        unsigned char* vs = decltype(stage)::value == 0 ? v_st0 : v_st1;
+        unsigned char* ks = decltype(stage)::value == 0 ? k_st0[stream] : k_st1[stream];
+        unsigned char* vs = decltype(stage)::value == 0 ? v_st0[stream] : v_st1[stream];
         const int key = tiles.at(v) * BN + 16 * wave, n = max(0, min(16, p.nk - key));
         const auto rk = make_rsrc(Kh + (n ? key * p.ks[2] : 0), rows_extent(n, krb, RB));
         const auto rv = make_rsrc(Vh + (n ? key * p.vs[2] : 0), rows_extent(n, vrb, RB));
@@ -224,8 +226,8 @@ __global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, 
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
     auto tile = [&](int v, auto stage) __attribute__((always_inline)) {
-        const unsigned char* ks = decltype(stage)::value == 0 ? k_st0 : k_st1;
-        const unsigned char* vs = decltype(stage)::value == 0 ? v_st0 : v_st1;
+        const unsigned char* ks = decltype(stage)::value == 0 ? k_st0[stream] : k_st1[stream];
+        const unsigned char* vs = decltype(stage)::value == 0 ? v_st0[stream] : v_st1[stream];
         const int k0 = tiles.at(v) * BN;
         if (!live) return;
 #pragma unroll
@@ -252,19 +254,33 @@ __global__ __launch_bounds__(QW * 64, 2) void win_dq_kernel(WinGrad p, float c, 
                     acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_tr<D>(ks, ta, d, 2 * u + c2), dsb[c2], acc[d], 0, 0, 0);
         }
     };
-    if (tiles.count > 0) {
-        issue(0, S0{});
-        for (int v = 0; v < tiles.count; v += 2) {
-            pf::wait_vmcnt<0>();
-            __syncthreads();
-            if (v + 1 < tiles.count) issue(v + 1, S1{});
-            tile(v, S0{});
-            if (v + 1 >= tiles.count) break;
-            pf::wait_vmcnt<0>();
-            __syncthreads();
-            if (v + 2 < tiles.count) issue(v + 2, S0{});
-            tile(v + 1, S1{});
+    auto turn = [&](int v, auto stage, auto other) __attribute__((always_inline)) {
+        pf::wait_vmcnt<0>();
+        __syncthreads();
+        if (v + KS < tiles.count) issue(v + KS, other);
+        if (KS == 1 || v < tiles.count) tile(v, stage);
+    };
+    if (stream < tiles.count) issue(stream, S0{});
+    for (int v = 0; v < tiles.count; v += 2 * KS) {
+        turn(v + stream, S0{}, S1{});
+        if (v + KS >= tiles.count) break;
+        turn(v + KS + stream, S1{}, S0{});
+    }
+    if constexpr (KS == 2) {   // the second stream's sums, through LDS
+        __syncthreads();
+        float* x = reinterpret_cast<float*>(wave < 2 ? &k_st0[0][0] : &k_st1[0][0]) + (wave & 1) * (D / 2) * 64;
+        if (stream == 1) {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[(d * 16 + i) * 64 + lane] = acc[d][i];
         }
+        __syncthreads();
+        if (stream == 1) return;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] += x[(d * 16 + i) * 64 + lane];
     }
     if (!live) return;
     const WinGrad late = arguments_again<WinGrad>();
@@ -662,7 +678,10 @@ hipError_t go(WinGrad p, hipStream_t stream) {
     if (p.nq > 0 && p.hq > 0) {
         const long long rows = (long long)p.nq * (p.hq / p.hk);
         const int tiles = (int)((rows + QROWS - 1) / QROWS);
-        const hipError_t e = launch_kernel(win_dq_kernel<D>, dim3((unsigned)groups * tiles), dim3(QW * 64), stream, p, c, tiles);
+        const unsigned blocks = (unsigned)groups * tiles;
+        const hipError_t e = blocks <= 256
+            ? launch_kernel(win_dq_kernel<D, 2>, dim3(blocks), dim3(2 * QW * 64), stream, p, c, tiles)
+            : launch_kernel(win_dq_kernel<D, 1>, dim3(blocks), dim3(QW * 64), stream, p, c, tiles);
         if (e != hipSuccess) return e;
     }
     if (p.nk == 0) return hipSuccess;

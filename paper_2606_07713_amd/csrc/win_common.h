@@ -101,17 +101,18 @@ __device__ __forceinline__ bool any_sees(const Seen& wl, const Seen& wh, int sin
     return k0 < wh.hi && (k0 + 32 > wl.lo || k0 < sinks);
 }
 
-// Makes -inf of the scores in a 32x32 accumulator whose bit is not set; element i is
-// bit 8 (i / 4) + 4 half + i % 4.  Two instructions each, whatever is masked.  (Written
-// as comparisons they became a branch per element: a causal window of 512 over 4096
-// tokens 120.3 us, so 118.8.)
+// x, or -inf where bit n is not set: two instructions.  (Written as comparisons these
+// became a branch per element.)
+__device__ __forceinline__ float keep_bit(float x, uint32_t bits, int n) {
+    const uint32_t all = (uint32_t)((int)(bits << (31 - n)) >> 31);
+    return __uint_as_float((__float_as_uint(x) & all) | (0xff800000u & ~all));
+}
+
+// The scores in a 32x32 accumulator; element i is bit 8 (i / 4) + 4 half + i % 4.
 __device__ __forceinline__ void keep(f32x16& x, uint32_t bits, int half) {
     bits >>= 4 * half;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const uint32_t all = (uint32_t)((int)(bits << (31 - 8 * (i >> 2) - (i & 3))) >> 31);
-        x[i] = __uint_as_float((__float_as_uint(x[i]) & all) | (0xff800000u & ~all));
-    }
+    for (int i = 0; i < 16; ++i) x[i] = keep_bit(x[i], bits, 8 * (i >> 2) + (i & 3));
 }
 
 // The launch's arguments once more, from where they came: what is used behind a loop

@@ -160,15 +160,18 @@ __global__ __launch_bounds__(WAVES * 64, RT == 1 ? 2 : 1) void win_few_kernel(Wi
                     a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[t][k]), q[i][k], a, 0, 0, 0);
                 s[i][t] = a;
             }
-        const bool masked = have != 3 || k0 + T > low.hi || (k0 < high.lo && k0 + T > p.w.sinks);
+        const bool masked = have != 3 || !all_see(low, high, p.w.sinks, k0);
         if (masked) {
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
+            for (int i = 0; i < RT; ++i) {
+                uint32_t bits = seen_bits(seen[i], p.w.sinks, k0);
+                if (have != 3) bits &= (have & 1 ? 0x0000ffffu : 0u) | (have & 2 ? 0xffff0000u : 0u);
+                bits >>= 4 * g;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (!((have >> t) & 1) || !sees(seen[i], p.w.sinks, k0 + 16 * t + 4 * g + j)) s[i][t][j] = kNegInf;
+                    for (int j = 0; j < 4; ++j) s[i][t][j] = keep_bit(s[i][t][j], bits, 16 * t + j);
+            }
         }
         // The weights 2^(s c - ref), each as TERMS bf16 numbers, and their sums.
         u32x4 pt[RT][TERMS];

@@ -41,8 +41,8 @@ constexpr int MROWS = MW * 32;   // rows per workgroup
 // How O leaves: bf16, fp32, or the fp32 state of a split.
 enum { TO_BF16, TO_F32, TO_STATE };
 
-template <int D, int OUT, int TERMS, int BN>
-__global__ __launch_bounds__(MW * 64, D == 64 || BN == 32 ? 3 : 2) void win_many_kernel(WinAttn p, float c, uint32_t qflip, int row_tiles) {
+template <int D, int OUT, int TERMS, int BN, int KS>
+__global__ __launch_bounds__(KS * MW * 64, KS == 1 && (D == 64 || BN == 32) ? 3 : 2) void win_many_kernel(WinAttn p, float c, uint32_t qflip, int row_tiles) {
     using C = Cfg<D>;
     constexpr uint32_t RB = C::ROW_BYTES;
     constexpr int SN = 32;                                // keys per step
@@ -51,15 +51,18 @@ __global__ __launch_bounds__(MW * 64, D == 64 || BN == 32 ? 3 : 2) void win_many
     constexpr int RPW = BN / MW, GROUPS = BN / 16;        // rows that a wave loads, page groups of a tile
     constexpr int ALL = (1 << GROUPS) - 1;
     // One array per ring stage: the compiler tracks direct-to-LDS loads per object.
-    __shared__ __attribute__((aligned(1024))) unsigned char k_st0[TILE];
-    __shared__ __attribute__((aligned(1024))) unsigned char k_st1[TILE];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_st0[TILE];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_st1[TILE];
+    __shared__ __attribute__((aligned(1024))) unsigned char k_st0[KS][TILE];
+    __shared__ __attribute__((aligned(1024))) unsigned char k_st1[KS][TILE];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_st0[KS][TILE];
+    __shared__ __attribute__((aligned(1024))) unsigned char v_st1[KS][TILE];
+    __shared__ float state[KS == 2 ? MW : 1][2][64];
     using S0 = std::integral_constant<int, 0>;
     using S1 = std::integral_constant<int, 1>;
 
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Waves MW .. of two key streams hold the rows of waves 0 .. and take every second tile.
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % MW;
+    const int stream = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / MW;
     const int col = lane & 31, half = lane >> 5;
     const KeySource& src = p.s;
     const int G = (int)p.group.n;
@@ -109,22 +112,23 @@ __global__ __launch_bounds__(MW * 64, D == 64 || BN == 32 ? 3 : 2) void win_many
         ld_koff[i] = (uint32_t)(r % RPW) * krb + chunk;   // this wave's rows of the tile
         ld_voff[i] = (uint32_t)(r % RPW) * vrb + chunk;
     }
-    // Lane GROUPS i + t holds the page of 16-key group t of the i-th tile from `known` on.
-    int pages = 0, known = begin;
+    // Lane GROUPS i + t holds the page of 16-key group t of this stream's i-th tile from
+    // `known` on.
+    int pages = 0, known = begin + stream;
     const auto look = [&]() {
-        const int v = known + lane / GROUPS, key = tiles.at(v) * BN + 16 * (lane % GROUPS);
+        const int v = known + lane / GROUPS * KS, key = tiles.at(v) * BN + 16 * (lane % GROUPS);
         pages = v < stop && key < end ? page_of(src, b, key) : -1;
     };
     // Starts the loads of the v-th tile; bit t of the result: group t has a page.
     // Tokens behind the last, and those without a page, become zeros.
     auto issue = [&](int v, auto stage) __attribute__((always_inline)) -> int {
-        unsigned char* ks = decltype(stage)::value == 0 ? k_st0 : k_st1;
-        unsigned char* vs = decltype(stage)::value == 0 ? v_st0 : v_st1;
-        if (v - known == 64 / GROUPS) {
+        unsigned char* ks = decltype(stage)::value == 0 ? k_st0[stream] : k_st1[stream];
+        unsigned char* vs = decltype(stage)::value == 0 ? v_st0[stream] : v_st1[stream];
+        if (v - known == 64 / GROUPS * KS) {
             known = v;
             look();
         }
-        const int i = v - known, key = tiles.at(v) * BN + RPW * wave;
+        const int i = (v - known) / KS, key = tiles.at(v) * BN + RPW * wave;
         const int page = __builtin_amdgcn_readlane(pages, GROUPS * i + wave * RPW / 16);
         const int n = page >= 0 ? max(0, min(RPW, end - key)) : 0;
         const u16* kb = static_cast<const u16*>(src.k) + (n ? key_offset(src.ks, src.shift, page, h, key) : 0);
@@ -159,8 +163,8 @@ __global__ __launch_bounds__(MW * 64, D == 64 || BN == 32 ? 3 : 2) void win_many
     float l = 0.0f;          // sum over this half-wave's keys
 
     auto tile = [&](int v, int have, auto stage) __attribute__((always_inline)) {
-        const unsigned char* ks = decltype(stage)::value == 0 ? k_st0 : k_st1;
-        unsigned char* vs = decltype(stage)::value == 0 ? v_st0 : v_st1;
+        const unsigned char* ks = decltype(stage)::value == 0 ? k_st0[stream] : k_st1[stream];
+        unsigned char* vs = decltype(stage)::value == 0 ? v_st0[stream] : v_st1[stream];
         const int k0 = tiles.at(v) * BN;
         if (!live) return;
 #pragma unroll
@@ -218,32 +222,63 @@ __global__ __launch_bounds__(MW * 64, D == 64 || BN == 32 ? 3 : 2) void win_many
         }
     };
 
-    // The v-th tile sits in stage v - begin & 1.  After the barrier at its start
-    // every wave has its part of it in LDS and is done with the tile before, into
+    // A stream's tiles alternate between the two stages.  After the barrier at a tile's
+    // start every wave has its part of it in LDS and is done with the tile before, into
     // whose stage the next one is loaded while this one is worked on.
+    auto turn = [&](int v, int have, auto stage, int& later, auto other) __attribute__((always_inline)) {
+        pf::wait_vmcnt<0>();
+        __syncthreads();
+        if (v + KS < stop) later = issue(v + KS, other);
+        if (KS == 1 || v < stop) tile(v, have, stage);
+    };
     if (begin < stop) {
         look();
-        int have0 = issue(begin, S0{}), have1 = 0;
-        for (int v = begin; v < stop; v += 2) {
-            pf::wait_vmcnt<0>();
-            __syncthreads();
-            if (v + 1 < stop) have1 = issue(v + 1, S1{});
-            tile(v, have0, S0{});
-            if (v + 1 >= stop) break;
-            pf::wait_vmcnt<0>();
-            __syncthreads();
-            if (v + 2 < stop) have0 = issue(v + 2, S0{});
-            tile(v + 1, have1, S1{});
+        int have0 = 0, have1 = 0;
+        if (begin + stream < stop) have0 = issue(begin + stream, S0{});
+        for (int v = begin; v < stop; v += 2 * KS) {
+            turn(v + stream, have0, S0{}, have1, S1{});
+            if (v + KS >= stop) break;
+            turn(v + KS + stream, have1, S1{}, have0, S0{});
         }
     }
     __syncthreads();   // every wave is done with the stages
+    if constexpr (KS == 2) {
+        // The second stream's sums, through LDS, against a common reference.
+        float* x = reinterpret_cast<float*>(wave < 2 ? &k_st0[0][0] : &k_st1[0][0]) + (wave & 1) * (D / 2) * 64;
+        if (stream == 1) {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[(d * 16 + i) * 64 + lane] = oacc[d][i];
+            state[wave][0][lane] = ref;
+            state[wave][1][lane] = l;
+        }
+        __syncthreads();
+        if (stream == 1) return;
+        const float r = state[wave][0][lane], top = fmaxf(ref, r);
+        const float a = ref == kNegInf ? 0.0f : exp2_hw(ref - top), c1 = r == kNegInf ? 0.0f : exp2_hw(r - top);
+        // (a sum without a reference is 0, or NaN of a score that is)
+        l = (ref == kNegInf ? l : l * a) + (r == kNegInf ? state[wave][1][lane] : state[wave][1][lane] * c1);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) oacc[d][i] = oacc[d][i] * a + x[(d * 16 + i) * 64 + lane] * c1;
+        ref = top;
+    }
     if (!live) return;
     const WinAttn late = arguments_again<WinAttn>();
 
     // O = acc / l (or the sums as they are) through a 32-row slice of the stages,
     // whole rows per store.
-    constexpr int SLICES = BN / 32;   // of one stage
-    unsigned char* stg = (wave / SLICES == 0 ? k_st0 : wave / SLICES == 1 ? k_st1 : wave / SLICES == 2 ? v_st0 : v_st1) + wave % SLICES * 32 * RB;
+    // (with two streams beside the sums that other waves still read)
+    unsigned char* stg;
+    if constexpr (KS == 2) {
+        static_assert(BN == 64, "two slices in each stage");
+        stg = (wave < 2 ? v_st0[0] : v_st1[0]) + (wave & 1) * 32 * RB;
+    } else {
+        constexpr int SLICES = BN / 32;   // of one stage
+        stg = (wave / SLICES == 0 ? k_st0[0] : wave / SLICES == 1 ? k_st1[0] : wave / SLICES == 2 ? v_st0[0] : v_st1[0]) + wave % SLICES * 32 * RB;
+    }
     const float total = half_sum(l);
     const bool none = ref == kNegInf;   // no visible key
     const float inv = OUT == TO_STATE ? 1.0f : none ? 0.0f : 1.0f / total;
@@ -351,17 +386,27 @@ hipError_t go(WinAttn p, hipStream_t stream) {
     c = c < 0.0f ? -c : c;
     if (c == 0.0f) c = std::numeric_limits<float>::denorm_min();
     const long long blocks = (long long)p.B * p.hk * tiles * p.splits;
-    const auto run = [&](auto kernel) {
-        return launch_kernel(kernel, dim3((unsigned)blocks), dim3(MW * 64), stream, p, c, flip, tiles);
+    const auto run = [&](auto kernel, int streams = 1) {
+        return launch_kernel(kernel, dim3((unsigned)blocks), dim3(streams * MW * 64), stream, p, c, flip, tiles);
     };
     // At d = 128 two workgroups with 64-key tiles fit a compute unit, and three with
     // tiles of 32, which wait for each other less but have twice the barriers: for more
     // workgroups than two for every unit (4096 tokens in a window of 512, 2048 of them
     // 100 -> 94 us, 8192 in 1024 176 -> 166; 504 of 200 queries on 20011 keys 85 -> 90).
     if constexpr (D == 128)
-        if (p.splits == 1 && blocks > 512) return p.out_bf16 ? run(win_many_kernel<D, TO_BF16, 1, 32>) : run(win_many_kernel<D, TO_F32, 3, 32>);
-    if (p.splits == 1) return p.out_bf16 ? run(win_many_kernel<D, TO_BF16, 1, 64>) : run(win_many_kernel<D, TO_F32, 3, 64>);
-    const hipError_t e = p.out_bf16 ? run(win_many_kernel<D, TO_STATE, 1, 64>) : run(win_many_kernel<D, TO_STATE, 3, 64>);
+        if (p.splits == 1 && blocks > 512) return p.out_bf16 ? run(win_many_kernel<D, TO_BF16, 1, 32, 1>) : run(win_many_kernel<D, TO_F32, 3, 32, 1>);
+    // Where a unit has one workgroup, its keys go to two streams of four waves.
+    const bool two = blocks <= 256;
+    const auto go_as = [&](auto out, auto terms) {
+        constexpr int O = decltype(out)::value, N = decltype(terms)::value;
+        return two ? run(win_many_kernel<D, O, N, 64, 2>, 2) : run(win_many_kernel<D, O, N, 64, 1>);
+    };
+    constexpr std::integral_constant<int, 1> one_term;
+    constexpr std::integral_constant<int, 3> three_terms;
+    if (p.splits == 1)
+        return p.out_bf16 ? go_as(std::integral_constant<int, TO_BF16>{}, one_term) : go_as(std::integral_constant<int, TO_F32>{}, three_terms);
+    constexpr std::integral_constant<int, TO_STATE> state;
+    const hipError_t e = p.out_bf16 ? go_as(state, one_term) : go_as(state, three_terms);
     if (e != hipSuccess) return e;
     const SplitJoin j{p.ws, p.o, p.lse, p.s.new_lens, {p.os[0], p.os[1], p.os[2]}, p.B, p.hq, p.n, p.splits, p.out_bf16};
     return launch_split_join<D>(j, stream);

@@ -98,6 +98,16 @@ def test_splits_of_ragged_lengths(splits, N):
         _check(c, _normal(9, 5, 6, N, 64), *window, num_splits=splits, max_len=1500)
 
 
+@pytest.mark.parametrize("page", [16, 64])
+def test_many_workgroups(page):
+    """More than two workgroups for every compute unit, pages that are not there among them."""
+    lens = [40 + 13 * i % 200 for i in range(80)]
+    c = Cache(lens, 8, page, 128)
+    c.table[7, 0] = -1
+    c.table[60:, 1] = -1
+    _check(c, _normal(9, 80, 16, 40, 128), 70, 0, 3, dtypes=(BF16,))
+
+
 @pytest.mark.parametrize("layout", ["pages", "tokens"])
 @pytest.mark.parametrize("N", [2, 50])
 def test_layouts_of_the_pools(layout, N):

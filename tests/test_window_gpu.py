@@ -71,6 +71,15 @@ def test_strided_views(d, Nq):
     assert bool((out[..., d:] == 7).all())
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_workgroups(d):
+    """More than two workgroups for every compute unit: other tiles are taken at d = 128."""
+    q, k, v = _normal(21, 40, 16, 70, d), _normal(22, 40, 8, 150, d), _normal(23, 40, 8, 150, d)
+    k[3, 2, 100], v[5, 1, 149, 4], v[39, 7, 81] = math.nan, math.inf, math.nan
+    for window in ((-1, 0, 0), (45, 0, 3), (20, 9, 40)):
+        _check(q, k, v, *window)
+
+
 @pytest.mark.parametrize("Nq", [3, 100])
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.0, 1e-42])
 def test_scales(Nq, scale):
@@ -108,6 +117,19 @@ def test_large_values_and_scores(Nq):
                     big[0].double() @ big[1].double().transpose(2, 3), -math.inf)
     want = v[0, 0][s.argmax(-1)].float()           # one key has all the weight
     assert torch.allclose(o, want, rtol=0, atol=0)
+
+
+@pytest.mark.parametrize("Nq", [4, 100])
+@pytest.mark.parametrize("rise", [60, 120, 200, 2000])
+def test_scores_that_rise(Nq, rise):
+    """Keys whose scores grow from the first to the last: the reference stays that of the first ones."""
+    q = _normal(24, 1, 2, Nq, 64)
+    q[..., 0] = 8
+    k, v = _normal(25, 1, 2, 400, 64), _normal(26, 1, 2, 400, 64)
+    k[..., 0] = torch.linspace(0, rise, 400, device="cuda").to(torch.bfloat16)   # scores up to `rise` higher
+    for splits in (1, 3):
+        _check(q, k, v, -1, 0, 0, num_splits=splits)
+        _check(q, k, v, 250, 0, 4, num_splits=splits)
 
 
 def test_nothing_to_do():
