@@ -68,7 +68,7 @@ size_t moa_win_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t N
  * the query heads that share it), as the sum of two (17 bits) with fewer, and of
  * three (25 bits) where O is fp32.  Keys and values that a row does not see
  * have no part in it, whatever they hold: rows whose sums do not come out finite
- * are done again by the definition, with scores in fp64.  One kernel, or two when
+ * are done again by the definition, one by one.  One kernel, or two when
  * the keys are split; no atomics, deterministic.
  */
 int moa_win_attn_fwd(const void* Q, const void* K, const void* V, void* O, float* LSE, int64_t B,

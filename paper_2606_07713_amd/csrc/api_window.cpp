@@ -201,7 +201,10 @@ int check_bwd(const Sizes& s) {
     if (s.B * s.Hk > 0 && s.Nk >= (kMaxRows + s.B * s.Hk - 1) / (s.B * s.Hk)) return MOA_ERR_UNSUPPORTED;
     const int64_t tiles = (s.Nk + kWinKeyTile - 1) / kWinKeyTile;
     const int64_t more = s.left < 0 ? 0 : 64 + tiles;   // chunks, of one tile or of many with one each
-    if (s.B * s.Hk * (tiles * near_parts(s) + more) > kMaxBlocks / 2) return MOA_ERR_UNSUPPORTED;   // of 512 threads
+    const int parts = near_parts(s);
+    if (s.B * s.Hk * (tiles * parts + more) > kMaxBlocks / 2) return MOA_ERR_UNSUPPORTED;   // of 512 threads
+    const int64_t joined = parts > 1 ? tiles : far_chunks(s) ? win_sink_tiles(window_of(s), (int)s.Nk) : 0;
+    if (s.B * s.Hk * joined > kMaxBlocks / (s.d / 4)) return MOA_ERR_UNSUPPORTED;   // d/4 of them for a tile's two sums
     return MOA_OK;
 }
 

@@ -56,28 +56,13 @@ __device__ __forceinline__ Seen seen_by(const WinGrad& p, int i) {
     return seen_from(p.w, (long long)i + p.nk - p.nq, p.nk);
 }
 
-// What of a row's gradient one pair gives: P and dS.
+// What one pair gives to a gradient: P and dS.  s0, s1: the rows of the score, t0, t1:
+// those of dP; s0 and t0 are the same in all lanes.
 template <int D>
-__device__ __forceinline__ void pair_by_definition(const u16* q, const u16* k, const u16* g, const u16* v, double c, float lse2,
+__device__ __forceinline__ void pair_by_definition(const u16* s0, const u16* s1, const u16* t0, const u16* t1, double c, float lse2,
                                                    float dsum, float& w, float& ds) {
-    double s = 0.0, t = 0.0;
-    for (int e = 0; e < D; e += 2) {
-        const auto two = [&](const u16* x) { return *reinterpret_cast<const uint32_t*>(x + e); };
-        const uint32_t a = two(q), y = two(k), m = two(g), z = two(v);
-        s += (double)bf16lo_to_f32(a) * (double)bf16lo_to_f32(y) + (double)bf16hi_to_f32(a) * (double)bf16hi_to_f32(y);
-        t += (double)bf16lo_to_f32(m) * (double)bf16lo_to_f32(z) + (double)bf16hi_to_f32(m) * (double)bf16hi_to_f32(z);
-    }
-    w = (float)exp2(s * c - (double)lse2);
-    ds = w * (float)(t - (double)dsum);
-}
-
-// Adds w * row to o, this lane's D/64 elements.
-template <int D>
-__device__ __forceinline__ void add_row(float (&o)[D / 64], float w, const u16* row) {
-    constexpr int E = D / 64;
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(w, __uint_as_float((uint32_t)row[E * lane + e] << 16), o[e]);
+    w = exp2_hw((float)(dot<D>(s0, s1) * c - (double)lse2));
+    ds = w * (float)(dot<D>(t0, t1) - (double)dsum);
 }
 
 template <int D>
@@ -300,9 +285,7 @@ __global__ __launch_bounds__(KS * QW * 64, 2) void win_dq_kernel(WinGrad p, floa
             const bool mine = sees(see, late.w.sinks, key);
             float w = 0.0f, ds = 0.0f;
             if (mine) pair_by_definition<D>(q, Kl + key * late.ks[2], g, Vl + key * late.vs[2], (double)late.scale * 1.4426950408889634, l, dd, w, ds);
-            const uint64_t all = __ballot(mine);
-            for (int j = 0; j < 64; ++j)
-                if ((all >> j) & 1) add_row<D>(o, __shfl(ds, j), Kl + (long long)(key - lane + j) * late.ks[2]);
+            add_rows<D>(o, __ballot(mine), ds, [&](int j) { return Kl + (long long)(tiles.at(v) * BN + j) * late.ks[2]; });
         }
         store_lane<D>(static_cast<u16*>(late.dq) + at_row(late.dqs, b, head, i), o, late.scale);
     }
@@ -627,12 +610,10 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
             float w = 0.0f, ds = 0.0f;
             if (seen) {
                 const size_t stat = ((size_t)b * late.hq + x.hh) * late.nq + qi;
-                pair_by_definition<D>(q0 + lane * late.qs[2], k, g0 + lane * late.gs[2], v, (double)late.scale * 1.4426950408889634,
+                pair_by_definition<D>(k, q0 + lane * late.qs[2], v, g0 + lane * late.gs[2], (double)late.scale * 1.4426950408889634,
                                       late.lse[stat] * kLog2e, late.dsum[stat], w, ds);
             }
-            const uint64_t all = __ballot(seen);
-            for (int i = 0; i < 64; ++i)
-                if ((all >> i) & 1) add_row<D>(o, __shfl(role == 0 ? w : ds, i), role == 0 ? g0 + i * late.gs[2] : q0 + i * late.qs[2]);
+            add_rows<D>(o, __ballot(seen), role == 0 ? w : ds, [&](int i) { return role == 0 ? g0 + i * late.gs[2] : q0 + i * late.qs[2]; });
         }
         if (partial) {
             for (int e = 0; e < D / 64; ++e) part[(size_t)(at - k0) * D + (D / 64) * lane + e] = o[e] * mul;

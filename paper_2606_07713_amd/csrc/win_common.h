@@ -144,8 +144,74 @@ struct Tiles {
     __device__ __forceinline__ int at(int v) const { return v < head ? v : v + skip; }
 };
 
+// <a, b> of two rows of D elements as T sums it, in one order; a is the same row in all
+// lanes.  (The loads of eight pieces are in flight together.)
+template <int D, typename T>
+__device__ __forceinline__ T dot_as(const u16* a, const u16* b) {
+#pragma clang fp contract(off)
+    T x = 0;
+    const uint64_t at = reinterpret_cast<uint64_t>(a);
+    const uint64_t uniform = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
+    const u32x4* q = reinterpret_cast<const u32x4*>(uniform);
+#pragma unroll 1
+    for (int e = 0; e < D; e += 64) {
+        u32x4 u[8], v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            u[i] = q[e / 8 + i];
+            v[i] = *reinterpret_cast<const u32x4*>(b + e + 8 * i);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x = __builtin_elementwise_fma((T)bf16lo_to_f32(u[i][j]), (T)bf16lo_to_f32(v[i][j]), x);
+                x = __builtin_elementwise_fma((T)bf16hi_to_f32(u[i][j]), (T)bf16hi_to_f32(v[i][j]), x);
+            }
+    }
+    return x;
+}
+// In fp32, or in fp64 what that does not hold.
+template <int D>
+__device__ __forceinline__ double dot(const u16* a, const u16* b) {
+    const float x = dot_as<D, float>(a, b);
+    return __builtin_isfinite(x) ? (double)x : dot_as<D, double>(a, b);
+}
+
+// Adds the lanes' w times their rows to o, this lane's elements D/64 lane ..; row(j):
+// lane j's row, only taken where its bit of `which` is set.  Eight at a time are in
+// flight.
+template <int D, typename F>
+__device__ __forceinline__ void add_rows(float (&o)[D / 64], uint64_t which, float w, F row) {
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+#pragma unroll 1
+    while (which) {
+        uint32_t bits[8];
+        float f[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const bool one = which != 0;
+            const int j = one ? __builtin_ctzll(which) : 0;
+            f[u] = one ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j)) : 0.0f;
+            bits[u] = 0;
+            if (one) {
+                const u16* at = row(j);
+                if constexpr (E == 2) bits[u] = *reinterpret_cast<const uint32_t*>(at + 2 * lane);
+                else bits[u] = at[lane];
+            }
+            which &= which - 1;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            o[0] = __builtin_fmaf(f[u], bf16lo_to_f32(bits[u]), o[0]);
+            if constexpr (E == 2) o[1] = __builtin_fmaf(f[u], bf16hi_to_f32(bits[u]), o[1]);
+        }
+    }
+}
+
 // One row by its definition, by one wave, over the keys of tiles begin .. end - 1:
-// scores in fp64, weights of at most 1, nothing of a key that the row does not
+// scores of any size, weights of at most 1, nothing of a key that the row does not
 // see.  For the rows whose sums in the tile kernels did not come out finite: a
 // value that is infinite or NaN (which a product with a weight of 0 spreads to
 // rows that do not see it), or a score or a sum beyond fp32.  o: this lane's
@@ -161,38 +227,30 @@ __device__ void row_by_definition(const WinAttn& p, int b, int h, const u16* q, 
     const int lane = threadIdx.x & 63;
     const double c = (double)p.scale * 1.4426950408889634;
     const auto score = [&](int key, int page) {
-#pragma clang fp contract(off)
-        const u16* k = static_cast<const u16*>(p.s.k) + key_offset(p.s.ks, p.s.shift, page, h, key);
-        double x = 0.0;
-        for (int e = 0; e < D; e += 2) {
-            const uint32_t a = *reinterpret_cast<const uint32_t*>(q + e), y = *reinterpret_cast<const uint32_t*>(k + e);
-            x += (double)bf16lo_to_f32(a) * (double)bf16lo_to_f32(y) + (double)bf16hi_to_f32(a) * (double)bf16hi_to_f32(y);
-        }
-        return x * c;
+        return dot<D>(q, static_cast<const u16*>(p.s.k) + key_offset(p.s.ks, p.s.shift, page, h, key)) * c;
     };
     const auto walk = [&](auto f) {
-        for (int v = begin; v < end; ++v)
-            for (int k0 = tiles.at(v) * T; k0 < (tiles.at(v) + 1) * T; k0 += 64) {
-                const int key = k0 + lane;
-                const bool in = lane < T && sees(seen, p.w.sinks, key);
-                const int page = in ? page_of(p.s, b, key) : -1;
-                if (wave_any(page >= 0)) f(k0, key, page);
-            }
+#pragma unroll 1
+        for (int v = begin; v < end; ++v) {
+            const int k0 = tiles.at(v) * T, key = k0 + lane;
+            const int page = lane < T && sees(seen, p.w.sinks, key) ? page_of(p.s, b, key) : -1;
+            if (wave_any(page >= 0)) f(k0, key, page);
+        }
     };
     double M = -__builtin_inf(), L = 0.0;
     bool any = false;
     walk([&](int, int key, int page) {
 #pragma clang fp contract(off)
-        double x = page >= 0 ? score(key, page) : -__builtin_inf();
+        const double x = page >= 0 ? score(key, page) : -__builtin_inf();
         double m = x;
 #pragma unroll
         for (int s = 1; s < 64; s <<= 1) m = fmax(m, __shfl_xor(m, s));
         any = true;
         const double top = fmax(M, m);
-        double w = page >= 0 ? exp2(x - top) : 0.0;
+        double w = page >= 0 ? (double)exp2_hw((float)(x - top)) : 0.0;
 #pragma unroll
         for (int s = 1; s < 64; s <<= 1) w += __shfl_xor(w, s);
-        L = (M == -__builtin_inf() ? 0.0 : L * exp2(M - top)) + w;
+        L = (M == -__builtin_inf() ? 0.0 : L * (double)exp2_hw((float)(M - top))) + w;
         M = top;
     });
 #pragma unroll
@@ -203,15 +261,10 @@ __device__ void row_by_definition(const WinAttn& p, int b, int h, const u16* q, 
     const double inv = partial ? 1.0 : 1.0 / L;
     walk([&](int k0, int key, int page) {
 #pragma clang fp contract(off)
-        const float w = page >= 0 ? (float)(exp2(score(key, page) - M) * inv) : 0.0f;
-        for (int j = 0; j < 64; ++j) {
-            const int pj = __shfl(page, j);
-            if (pj < 0) continue;
-            const float wj = __shfl(w, j);
-            const u16* v = static_cast<const u16*>(p.s.v) + key_offset(p.s.vs, p.s.shift, pj, h, k0 + j) + E * lane;
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(wj, __uint_as_float((uint32_t)v[e] << 16), o[e]);
-        }
+        const float w = page >= 0 ? (float)((double)exp2_hw((float)(score(key, page) - M)) * inv) : 0.0f;
+        add_rows<D>(o, __ballot(page >= 0), w, [&](int j) {
+            return static_cast<const u16*>(p.s.v) + key_offset(p.s.vs, p.s.shift, __builtin_amdgcn_readlane(page, j), h, k0 + j);
+        });
     });
     // A reference that is not finite would drop out of a join.
     const bool finite = M > -3e38 && M < 3e38;

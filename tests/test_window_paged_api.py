@@ -103,6 +103,8 @@ BWD_BAD = [
     (dict(gs=[1 << 28, 1 << 27, (1 << 23) + 8]), 2), (dict(dks=[1024, 64, 64]), 1), (dict(dqs=[2048, 512, -64]), 1),
     (dict(dQ=P), 1), (dict(dQ=5 * P), 1), (dict(dK=8 * P, dV=8 * P), 1), (dict(dV=3 * P), 1), (dict(dK=6 * P), 1),
     (dict(ws=7 * P), 1), (dict(ws=6 * P), 1), (dict(ws=None), 3), (dict(wsn=100), 3),
+    # more workgroups of the join than one launch takes
+    (dict(B=1 << 20, Hq=1, Hk=1, Nq=40, Nk=40, left=3, sinks=4, **{k: i * P << 16 for i, k in enumerate(("Q", "K", "V", "O", "dO", "LSE", "dQ", "dK", "dV", "ws"), 1)}), 2),
 ]
 
 
