@@ -12,7 +12,8 @@
 // * win_dq: one workgroup = 4 waves x 32 rows of one key/value head, a row being a
 //   query and one of the G = Hq/Hk heads that share it; K and V tiles of 64 keys
 //   stream through LDS as in the forward, only those that a row sees.  D_i of its
-//   rows comes first, for the other kernel too.
+//   rows comes first, for the other kernel too: from O, or where a row sees few keys
+//   and O is bf16, from the keys.
 // * win_dkdv: one workgroup = 128 keys; Q and dO of the queries that see one of them
 //   stream through LDS, 64 queries of one head at a time, head after head, so that
 //   shared heads meet in the same sums.  A pair of waves on one SIMD owns 32 keys:
@@ -109,6 +110,12 @@ __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[D / 32]) {
 
 constexpr int QW = 4;            // waves
 constexpr int QROWS = QW * 32;   // rows per workgroup
+// Row tiles with a row that sees fewer keys take D_i from the keys.
+constexpr int kFewKeys = 64;
+
+// How many keys a row sees; fewest at a tile's first or last row, since both limits
+// rise with the position and the keys' ends cut them.
+__device__ __forceinline__ int keys_seen(Seen s, int sinks) { return s.hi - s.lo + min(sinks, s.lo); }
 
 template <int D, int KS>
 __global__ __launch_bounds__(KS * QW * 64, 2) void win_dq_kernel(WinGrad p, float c, int row_tiles) {
@@ -133,7 +140,8 @@ __global__ __launch_bounds__(KS * QW * 64, 2) void win_dq_kernel(WinGrad p, floa
     const auto uniform = [](Seen s) {
         return Seen{__builtin_amdgcn_readfirstlane(s.lo), __builtin_amdgcn_readfirstlane(s.hi)};
     };
-    const Tiles<BN> tiles(uniform(seen_by(p, over(p.group, row0))), uniform(seen_by(p, over(p.group, min(row0 + QROWS, rows) - 1))), p.w.sinks);
+    const Seen tl = uniform(seen_by(p, over(p.group, row0))), th = uniform(seen_by(p, over(p.group, min(row0 + QROWS, rows) - 1)));
+    const Tiles<BN> tiles(tl, th, p.w.sinks);
 
     // This wave's rows; this lane's row, its Q and dO fragments, LSE and D.
     const int w0 = row0 + wave * 32, row = w0 + col;
@@ -182,7 +190,6 @@ __global__ __launch_bounds__(KS * QW * 64, 2) void win_dq_kernel(WinGrad p, floa
         }
     }
     dsum = half_sum(dsum);
-    if (in && half == 0 && stream == 0) p.dsum[stat] = dsum;
 
     const u16* Kh = static_cast<const u16*>(p.k) + at_row(p.ks, b, h, 0);
     const u16* Vh = static_cast<const u16*>(p.v) + at_row(p.vs, b, h, 0);
@@ -207,10 +214,71 @@ __global__ __launch_bounds__(KS * QW * 64, 2) void win_dq_kernel(WinGrad p, floa
         for (int j = 0; j < LPW; ++j) buffer_load16_to_lds(rv, vs + (wave * LPW + j) * 1024, voff[j]);
     };
     const TileAddr<D> ta(lane);
+    // S and dP of 32 keys, S as the exponent of the weights.
+    auto scores = [&](const unsigned char* ks, const unsigned char* vs, int u, int key, f32x16& s, f32x16& dp) __attribute__((always_inline)) {
+        s = f32x16{};
+        dp = f32x16{};
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_rows<D>(ks, ta, u, k), qf[k], s, 0, 0, 0);
+            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_rows<D>(vs, ta, u, k), gf[k], dp, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], c, -lse2);
+        if (!all_see(wl, wh, sinks, key)) keep(s, seen_bits(seen, sinks, key), half);
+    };
+    // The tiles, with `tile` for each: pairs of turns on the ring's two stages.
+    auto walk = [&](auto tile) __attribute__((always_inline)) {
+        auto turn = [&](int v, auto stage, auto other) __attribute__((always_inline)) {
+            pf::wait_vmcnt<0>();
+            __syncthreads();
+            if (v + KS < tiles.count) issue(v + KS, other);
+            if (KS == 1 || v < tiles.count) tile(v, stage);
+        };
+        if (stream < tiles.count) issue(stream, S0{});
+        for (int v = 0; v < tiles.count; v += 2 * KS) {
+            turn(v + stream, S0{}, S1{});
+            if (v + KS >= tiles.count) break;
+            turn(v + KS + stream, S1{}, S0{});
+        }
+    };
+    // D_i from O has the error of its bf16 numbers, |dO| |O| 2^-8 at most, and O is large and
+    // dS small where a row sees few keys.  There D_i is taken from them: sum_j P_ij dP_ij,
+    // exact to fp32, one more walk over one or two tiles.  (4 x 1000 causal tokens, d = 64:
+    // error of dQ and dK 2.4e-3 for 2.6e-3, at the same time.  One key to a row: exact for
+    // an error as large as the gradients of others.)
+    if (p.o_bf16 && min(keys_seen(tl, sinks), keys_seen(th, sinks)) < kFewKeys) {
+        float sum = 0.0f;
+        walk([&](int v, auto stage) __attribute__((always_inline)) {
+            if (!live) return;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int key = tiles.at(v) * BN + 32 * u;
+                if (!any_sees(wl, wh, sinks, key)) continue;
+                f32x16 s, dp;
+                scores(decltype(stage)::value == 0 ? k_st0[stream] : k_st1[stream], decltype(stage)::value == 0 ? v_st0[stream] : v_st1[stream], u, key, s, dp);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum = __builtin_fmaf(exp2_hw(s[i]), dp[i], sum);
+            }
+        });
+        sum = half_sum(sum);
+        __syncthreads();   // every wave is through with the stages
+        if constexpr (KS == 2) {
+            float* x = reinterpret_cast<float*>(&k_st0[0][0]) + wave * 64 + lane;
+            x[stream * QW * 64] = sum;
+            __syncthreads();
+            sum += x[(1 - stream) * QW * 64];
+            __syncthreads();
+        }
+        // (Not finite: a key that the row does not see may be the cause, so O stays.)
+        if (__builtin_fabsf(sum) < -kNegInf) dsum = sum;
+    }
+    if (in && half == 0 && stream == 0) p.dsum[stat] = dsum;
+
     f32x16 acc[D / 32];
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
-    auto tile = [&](int v, auto stage) __attribute__((always_inline)) {
+    walk([&](int v, auto stage) __attribute__((always_inline)) {
         const unsigned char* ks = decltype(stage)::value == 0 ? k_st0[stream] : k_st1[stream];
         const unsigned char* vs = decltype(stage)::value == 0 ? v_st0[stream] : v_st1[stream];
         const int k0 = tiles.at(v) * BN;
@@ -218,15 +286,8 @@ __global__ __launch_bounds__(KS * QW * 64, 2) void win_dq_kernel(WinGrad p, floa
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             if (!any_sees(wl, wh, sinks, k0 + 32 * u)) continue;
-            f32x16 s = f32x16{}, dp = f32x16{};
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_rows<D>(ks, ta, u, k), qf[k], s, 0, 0, 0);
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_rows<D>(vs, ta, u, k), gf[k], dp, 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], c, -lse2);
-            if (!all_see(wl, wh, sinks, k0 + 32 * u)) keep(s, seen_bits(seen, sinks, k0 + 32 * u), half);
+            f32x16 s, dp;
+            scores(ks, vs, u, k0 + 32 * u, s, dp);
             float ds[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) ds[i] = exp2_hw(s[i]) * (dp[i] - dsum);
@@ -238,19 +299,7 @@ __global__ __launch_bounds__(KS * QW * 64, 2) void win_dq_kernel(WinGrad p, floa
                 for (int d = 0; d < D / 32; ++d)
                     acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stage_tr<D>(ks, ta, d, 2 * u + c2), dsb[c2], acc[d], 0, 0, 0);
         }
-    };
-    auto turn = [&](int v, auto stage, auto other) __attribute__((always_inline)) {
-        pf::wait_vmcnt<0>();
-        __syncthreads();
-        if (v + KS < tiles.count) issue(v + KS, other);
-        if (KS == 1 || v < tiles.count) tile(v, stage);
-    };
-    if (stream < tiles.count) issue(stream, S0{});
-    for (int v = 0; v < tiles.count; v += 2 * KS) {
-        turn(v + stream, S0{}, S1{});
-        if (v + KS >= tiles.count) break;
-        turn(v + KS + stream, S1{}, S0{});
-    }
+    });
     if constexpr (KS == 2) {   // the second stream's sums, through LDS
         __syncthreads();
         float* x = reinterpret_cast<float*>(wave < 2 ? &k_st0[0][0] : &k_st1[0][0]) + (wave & 1) * (D / 2) * 64;

@@ -138,6 +138,24 @@ def test_what_does_not_see_each_other_has_no_part(d, what):
                 close(g[:, :, 3:far], want[:, :, 3:far], bound[:, :, 3:far])
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hk,N,left,right,sinks", [(2, 2, 300, 0, 0, 0), (8, 2, 333, 1, 0, 0), (4, 4, 700, 7, 0, 1), (6, 2, 200, 5, 20, 2),
+                                                      (64, 4, 600, 40, 0, 3), (4, 1, 60, -1, 0, 0)])
+def test_few_keys(Hq, Hk, N, left, right, sinks, d):
+    """Where a row sees a handful of keys, dP - D is a difference of near numbers: with a row's only key it
+    is 0.  O as a bf16 number would leave 2^-8 of |dO| |O| there; the sum over the keys leaves fp32's."""
+    import paper_2606_07713_amd as moa
+    q, k, v, do = (_normal(40 + i, 2, h, N, d) for i, h in enumerate((Hq, Hk, Hk, Hq)))
+    x = _exact(q, k, v, left, right, sinks, None, do)
+    o, lse = moa.win_attn_fwd(q, k, v, left, right, sinks, return_lse=True)
+    got = moa.win_attn_bwd(q, k, v, o, do, lse, left, right, sinks)
+    for name, g, (want, bound) in zip("qkv", got, x.grad_bounds(torch.bfloat16, Hk, few_keys=True)):
+        try:
+            close(g, want, bound)
+        except AssertionError as e:
+            raise AssertionError(f"d{name}: {e}") from None
+
+
 def test_nothing_to_do():
     import paper_2606_07713_amd as moa
     for B, Hq, Nq, Nk in ((0, 2, 3, 4), (1, 0, 3, 4), (1, 2, 0, 4), (2, 2, 3, 0)):

@@ -66,14 +66,18 @@ class Exact:
     def lse_bound(self):
         return self.weight_error()[..., 0] + 2.0 ** -21 * self.lse.abs().nan_to_num(0, posinf=0) + 2.0 ** -22
 
-    def grad_bounds(self, o_dtype, heads_k):
-        """Of dq, dk, dv in bf16: P and dS as one bf16 number each, D from O as it is stored."""
+    def grad_bounds(self, o_dtype, heads_k, few_keys=False):
+        """Of dq, dk, dv in bf16: P and dS as one bf16 number each, D from O as it is stored, or with few
+        keys as the sum of P dP over them, with a weight's error on each and one for every addition."""
         e = self.weight_error()
         r = 2.0 ** -8
         sd = (self.d + 6) * 2.0 ** -24
         terms = torch.where(self.see, self.do.abs() @ self.v.abs().transpose(2, 3), 0.0)
         o_off = (self.do.abs() * (self.o.abs() * EPS[o_dtype] + self.bound * (r + e))).sum(-1, keepdim=True)
         sum_off = sd * (self.do.abs() * self.o.abs()).sum(-1, keepdim=True)
+        if few_keys:
+            o_off = (self.p * (e + self.M * 2.0 ** -24) * self.dp.abs()).sum(-1, keepdim=True)
+            sum_off = (self.p * sd * terms).sum(-1, keepdim=True)
         ds_off = self.p * ((2 * r + r * r + e) * (self.dp - self.delta).abs() + (1 + 2 * r) * (o_off + sum_off + sd * terms))
         s = abs(self.scale)
         dq = s * (ds_off @ self.k.abs()) + self.dq.abs() * r * (1 + r)
