@@ -80,8 +80,9 @@ int moa_win_attn_fwd(const void* Q, const void* K, const void* V, void* O, float
 
 /*
  * moa_win_attn_bwd_workspace_bytes -- device workspace of a moa_win_attn_bwd call, in
- * bytes (0 for invalid dimensions): a sum for every query row, and, where first keys
- * stay visible behind a window, partial sums of their gradients.
+ * bytes (0 for dimensions that are invalid or not supported): a sum for every query
+ * row, and partial sums of dK and dV where first keys stay visible behind a window, or
+ * where the key tiles alone would leave compute units idle.
  */
 size_t moa_win_attn_bwd_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t Nq, int64_t Nk,
                                         int64_t d, int64_t left, int64_t right, int64_t sinks);
@@ -105,17 +106,20 @@ size_t moa_win_attn_bwd_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64
  * *_strides as for the forward; here rows of all tensors are at most 2^23 elements
  *           apart.
  * B, Hq, Hk, Nq, Nk, d, left, right, sinks, scale
- *           the forward's; supported besides: B * Hk * Nk < 2^26 and fewer than 2^23
- *           workgroups of 512 threads (of 128 keys of one key/value head).
+ *           the forward's; supported besides: B * Hk * Nk < 2^26, at most 2^23
+ *           workgroups of 512 threads (of 128 keys of one key/value head), and at most
+ *           2^24 of 256 where partial sums are joined (d/4 for 128 keys).
  * workspace, workspace_bytes
  *           at least moa_win_attn_bwd_workspace_bytes(...) bytes, 16-byte aligned,
  *           overlapping nothing.
  *
  * Computation: bf16 matrix products with fp32 accumulation; P and dS enter them as one
- * bf16 number each, one rounding at the end.  Rows and keys that do not see each
+ * bf16 number each, one rounding at the end.  D comes from O and dO, or, where O is
+ * bf16 and rows of a tile of 128 see fewer than 64 keys, from the keys: sum_j P_ij
+ * <dO_i, V_j>, which has no part of O's rounding.  Rows and keys that do not see each
  * other have no part in each other's gradients, whatever they hold: sums that do not
  * come out finite are done again by the definition.  Two kernels, or three with
- * first keys behind a window; no atomics, deterministic.
+ * partial sums; no atomics, deterministic.
  */
 int moa_win_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO,
                      const float* LSE, void* dQ, void* dK, void* dV, int64_t B, int64_t Hq,

@@ -7,6 +7,11 @@
 // per element that it keeps in registers, the next rows on their way while it
 // works on the present ones; the angles are taken once per token, into LDS.  What
 // a key or value row adds is its page, looked up once per token.
+//
+// What bounds it: memory.  2 x 4096 tokens, 16 + 16 + 16 heads, d = 128: 34 us alone,
+// 5.9 TB/s, waiting for rows 0.68 of its time; 44 among other work (4.6 TB/s, a copy of
+// that size 5.1).  (All three tensors mixed in a group's rows, each row's addresses
+// formed anew: 87.)  One token: 5 us, latencies.
 #include "rope_common.h"
 #include "paged.h"
 #include "win_common.h"

@@ -28,6 +28,11 @@
 //   win_join adds in a fixed order.
 // No atomics; deterministic.  P and dS are rounded to bf16 for the matrix products.
 // Rows whose sums do not come out finite are done again by the definition.
+//
+// What bounds them: matrix instructions with an operand from LDS in each (matrix cores
+// 0.50 of a unit's cycles in dQ, 0.44 in dK/dV, two waves to a SIMD, which is what d = 128
+// has registers for).  8192 tokens, 32 heads on 8, d = 128, a window of 1024: dQ 226 us,
+// dK/dV 345 us, the join of the first keys' sums 6 us.
 #include <algorithm>
 #include <type_traits>
 

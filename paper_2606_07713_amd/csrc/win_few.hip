@@ -14,6 +14,10 @@
 // operand when the values are taken in the same order: no weight crosses a lane.
 // A weight meets V as two bf16 numbers, 17 bits together, or as three for an fp32
 // output, whose rounding is far below two; the sums are of the fp32 weights.
+//
+// What bounds it: HBM.  64 sequences of 8192 tokens, 32 heads on 8, d = 128: 316 us,
+// 6.8 TB/s, the matrix cores 0.06 busy.  One sequence of 4097: 8 us in 256 workgroups and
+// 4 for the join, latencies.
 #include <limits>
 
 #include "split_join.h"

@@ -19,6 +19,11 @@
 // meets V as one bf16 number for a bf16 output (2^-9 each, which leaves the error
 // of a bf16 output at 1.4 times its own rounding's), as three for an fp32 output
 // (two left it at 2.3e-6, nine times what fp32 sums alone make).
+//
+// What bounds it: matrix and vector instructions, which overlap in part (matrix cores
+// 0.43 to 0.48 of a unit's cycles, 6 to 8 vector instructions for each matrix
+// instruction).  d = 128, 32 heads on 8: 2 x 4096 tokens in a window of 512 93 us, 8192 in
+// one of 1024 160 us (0.81 PFLOP/s of visible pairs), 8192 causal of 32 heads 544 us.
 #include <limits>
 
 #include "prefill_bf16_common.h"

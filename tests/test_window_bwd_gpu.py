@@ -108,7 +108,10 @@ def test_differences(d):
             ends.append((moa.win_attn_fwd(*moved, *how, out_dtype=torch.float32).double() * do.double()).sum())
         slope = (ends[0] - ends[1]) / 2
         want = (g.double() * way.double() / 64).sum()
-        # elements of 2 and more do not take the whole step; the third derivative, and the gradient's roundings
+        # Elements of 2 and more do not take the whole step.  The gradient's roundings: at most three halves of
+        # bf16 steps an element, 1.2e-2 of it (P, dS, dK), of random signs under a random direction, so 1.2e-2 of
+        # the norm; the third derivative, with scores that move by 2^-6 |q| and less: (2^-6 sqrt(d) / sqrt(d))^2
+        # of the slope, 2.5e-4.  Four times the two.
         off = (g.double().abs() * (way.double() / 64 - way_got.double()).abs()).sum()
         noise = (g.double().square().sum().sqrt() / 64) * 0.05
         assert abs(float(slope - want)) <= float(off + noise) + 1e-4
