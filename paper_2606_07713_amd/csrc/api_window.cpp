@@ -21,9 +21,13 @@ constexpr float kMaxScale = 0x1p127f;           // times log2(e) is still finite
 // Workgroups of 256 threads in one launch: its threads are counted in 32 bits.
 constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;
 
-// The sizes of an attention call; Nk: keys of a sequence, at most.
+// The sizes of an attention call; Nk: keys of a sequence, at most; left, right: -1
+// where there is no limit, below kMost else, so that sums of them hold.
 struct Sizes {
     int64_t B, Hq, Hk, N, Nk, d, left, right, sinks;
+    Sizes(int64_t B_, int64_t Hq_, int64_t Hk_, int64_t N_, int64_t Nk_, int64_t d_, int64_t left_, int64_t right_, int64_t sinks_)
+        : B(B_), Hq(Hq_), Hk(Hk_), N(N_), Nk(Nk_), d(d_), left(limit(left_)), right(limit(right_)), sinks(std::min(sinks_, kMost)) {}
+    static int64_t limit(int64_t x) { return x < 0 || x >= kMost ? -1 : x; }
     int64_t rows() const { return N * (Hq / Hk); }
     int64_t per() const { return win_rows_per_block(rows()); }
     int64_t tiles() const { return (rows() + per() - 1) / per(); }
@@ -97,9 +101,9 @@ size_t states_bytes(const Sizes& s, int splits) {
     return align256((size_t)(s.B * s.Hq * s.N) * (size_t)splits * (size_t)(s.d + 2) * sizeof(float));
 }
 
-int limit(int64_t x) { return x < 0 || x >= kMost ? kNoLimit : (int)x; }
+int limit(int64_t x) { return x < 0 ? kNoLimit : (int)x; }
 
-Window window_of(const Sizes& s) { return {limit(s.left), limit(s.right), (int)std::min(s.sinks, kMost)}; }
+Window window_of(const Sizes& s) { return {limit(s.left), limit(s.right), (int)s.sinks}; }
 
 // What both entry points check and do once their keys are known.  `keys`: the
 // ranges that the call reads besides Q.

@@ -200,6 +200,20 @@ def test_splits_and_workspaces():
                 assert b(1, 4, 2, N, 5000, 64, left, 0, sinks) < 1 << 30
 
 
+@pytest.mark.parametrize("far", [1 << 30, 1 << 62, (1 << 63) - 1])
+def test_windows_longer_than_any_sequence(far):
+    """They are no limit, however long: the same choices as without one, and no sum of them overflows."""
+    for N, Nk, sinks in ((1, 5000, 0), (300, 9000, 4), (4096, 4096, 200)):
+        for left, right in ((far, 0), (far, far), (-1, far), (100, far)):
+            plain = [-1 if x == far else x for x in (left, right)]
+            for f, more in ((moa.moa_win_attn_num_splits, [0]), (moa.moa_win_attn_workspace_bytes, [0]),
+                            (moa.moa_win_attn_bwd_workspace_bytes, [])):
+                assert f(1, 8, 2, N, Nk, 64, left, right, sinks, *more) == f(1, 8, 2, N, Nk, 64, *plain, sinks, *more)
+                assert f(1, 8, 2, N, Nk, 64, left, right, far, *more) == f(1, 8, 2, N, Nk, 64, *plain, 1 << 30, *more)
+            a = [moa.moa_paged_attn_num_splits(1, 8, 2, N, 64, 16, 1000, 0, *w, s, 0) for w, s in (((left, right), sinks), (plain, sinks))]
+            assert a[0] == a[1]
+
+
 def test_wrappers_refuse():
     torch = pytest.importorskip("torch")
     q = torch.zeros(1, 2, 3, 64, dtype=torch.bfloat16)
