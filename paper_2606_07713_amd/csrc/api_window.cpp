@@ -16,7 +16,6 @@ using namespace moa;
 
 constexpr int64_t kMaxRows = int64_t(1) << 26;  // B * Hq * N: four rows a workgroup when splits are joined
 constexpr int64_t kMaxStageStride = int64_t(1) << 23;   // 64 rows' bytes stay in 32 bits
-constexpr int kMaxSplits = 256;
 constexpr float kMaxScale = 0x1p127f;           // times log2(e) is still finite
 // Workgroups of 256 threads in one launch: its threads are counted in 32 bits.
 constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;

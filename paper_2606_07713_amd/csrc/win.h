@@ -63,6 +63,12 @@ inline void set_divisions(WinAttn& p) {
     p.heads = div_by(p.hk);
 }
 
+// The states of up to kMaxSplits splits are added: none of them is larger than the
+// largest number over that, or it is done by the definition, whose states are 2^-40 of
+// the sums (of weights of at most 1).
+constexpr int kMaxSplits = 256;
+constexpr float kStateShift = 40.0f;
+
 // Rows (queries times the query heads of a key/value head) that a workgroup
 // takes: 16 or 32 in the kernel of few rows, 128 in that of many.
 inline int win_rows_per_block(long long rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 128; }

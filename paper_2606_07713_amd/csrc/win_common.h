@@ -258,7 +258,8 @@ __device__ void row_by_definition(const WinAttn& p, int b, int h, const u16* q, 
     ref = kNegInf;
     sum = 0.0f;
     if (!any) return;
-    const double inv = partial ? 1.0 : 1.0 / L;
+    const double inv = partial ? 0x1p-40 : 1.0 / L;
+    static_assert(kStateShift == 40.0f);
     walk([&](int k0, int key, int page) {
 #pragma clang fp contract(off)
         const float w = page >= 0 ? (float)((double)exp2_hw((float)(score(key, page) - M)) * inv) : 0.0f;
@@ -268,8 +269,8 @@ __device__ void row_by_definition(const WinAttn& p, int b, int h, const u16* q, 
     });
     // A reference that is not finite would drop out of a join.
     const bool finite = M > -3e38 && M < 3e38;
-    ref = finite || !partial ? (float)M : 0.0f;
-    sum = finite ? (float)L : __builtin_nanf("");
+    ref = !partial ? (float)M : finite ? (float)(M + (double)kStateShift) : 0.0f;
+    sum = finite ? (float)(partial ? L * inv : L) : __builtin_nanf("");
     if (!finite && partial)
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] = __builtin_nanf("");

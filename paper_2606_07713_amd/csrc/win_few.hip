@@ -293,9 +293,10 @@ __global__ __launch_bounds__(WAVES * 64, RT == 1 ? 2 : 1) void win_few_kernel(Wi
         }
         const int qi = over(p.group, row), hh = h * G + row - qi * G;
         // Sums that are not finite, or none at all in a row that sees keys: by the definition.
-        float zero = 0.0f * L;
+        const float most = p.splits > 1 ? (float)kMaxSplits : 1.0f;
+        float zero = 0.0f * (L * most);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) zero = __builtin_fmaf(f[e], 0.0f, zero);
+        for (int e = 0; e < 8; ++e) zero = __builtin_fmaf(f[e] * most, 0.0f, zero);
         if (!(zero == 0.0f) || (L == 0.0f && begin < stop && sees_any(seen_of(row), p.w.sinks))) again[r] = 1;
         const size_t to_row = ((size_t)b * p.hq + hh) * p.n + qi;
         if (p.splits > 1) {

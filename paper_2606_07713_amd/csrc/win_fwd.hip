@@ -288,11 +288,12 @@ __global__ __launch_bounds__(KS * MW * 64, KS == 1 && (D == 64 || BN == 32) ? 3 
     const bool none = ref == kNegInf;   // no visible key
     const float inv = OUT == TO_STATE ? 1.0f : none ? 0.0f : 1.0f / total;
     // Sums that are not finite, or none at all in a row that sees keys.
-    float zero = 0.0f * total;
+    constexpr float most = OUT == TO_STATE ? (float)kMaxSplits : 1.0f;
+    float zero = 0.0f * (total * most);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(oacc[d][i], 0.0f, zero);
+        for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(oacc[d][i] * most, 0.0f, zero);
     zero = half_sum(zero);
     const bool odd = in && (!(zero == 0.0f) || (total == 0.0f && begin < stop && sees_any(seen, sinks)));
     int ln = lane;

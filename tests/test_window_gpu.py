@@ -72,6 +72,31 @@ def test_strided_views(d, Nq):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("splits", [1, 2, 16])
+@pytest.mark.parametrize("Nq,G", [(1, 2), (20, 1), (90, 2)])
+def test_values_near_the_largest(Nq, G, splits, d):
+    """Sums of such values leave fp32 before they are divided, in a split and in the join of splits."""
+    v = _normal(50, 1, 2, 1024, d)
+    v = (torch.where(v < 0, -1.0, 1.0) * 3e38 - v.float() * 1e36).to(torch.bfloat16)
+    v[..., d // 2:] = 3e38
+    _check(_normal(51, 1, 2 * G, Nq, d), _normal(52, 1, 2, 1024, d), v, -1, -1, 0, num_splits=splits)
+    _check(_normal(51, 1, 2 * G, Nq, d), _normal(52, 1, 2, 1024, d), v, 300, 0, 0, num_splits=splits)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rise", [100.0, 119.5, 126.0, 127.5, 140.0])
+@pytest.mark.parametrize("Nq,G", [(1, 2), (20, 1), (90, 2)])
+def test_scores_that_rise_in_every_split(Nq, G, rise, d):
+    """One key of every 64 stands so many log2 units above the others: a split's sum is the largest
+    number or near it, and 16 of them are added."""
+    q, k, v = _normal(53, 1, 2 * G, Nq, d), _normal(54, 1, 2, 1024, d), _normal(55, 1, 2, 1024, d)
+    q[..., 0], k[..., 0] = 1.0, 0.0
+    q[..., 1:], k[:, :, 60::64, 0] = 0.0, 1.0
+    _check(q, k, v, -1, -1, 0, scale=rise * math.log(2), num_splits=16)
+    _check(q, k, v, -1, -1, 0, scale=rise * math.log(2), num_splits=1)
+
+
+@pytest.mark.parametrize("d", [64, 128])
 def test_many_workgroups(d):
     """More than two workgroups for every compute unit: other tiles are taken at d = 128."""
     q, k, v = _normal(21, 40, 16, 70, d), _normal(22, 40, 8, 150, d), _normal(23, 40, 8, 150, d)
