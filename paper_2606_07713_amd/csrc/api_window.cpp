@@ -168,23 +168,40 @@ int far_chunks(const Sizes& s) {
     return (int)std::clamp<int64_t>(std::min(fill, behind / 6), 1, std::max<int64_t>(1, 64 / tiles));
 }
 
-// Parts of the queries of every key tile, where the tiles alone do not fill the GPU: a
-// workgroup takes a stage of 64 queries in about 1.5 us (256 run at a time), starting
-// and ending it costs about four of these, joining about two and one for every 12 MB
-// of partial sums.
-int near_parts(const Sizes& s) {
-    if (!s.any() || s.Nk == 0) return 1;
-    const int64_t tiles = (s.Nk + kWinKeyTile - 1) / kWinKeyTile, items = s.B * s.Hk * tiles, G = s.Hq / s.Hk;
-    const int64_t reach = s.left < 0 || s.right < 0 ? s.N : std::min(s.N, s.left + s.right + kWinKeyTile);
-    const int64_t all = ((reach + kWinStage - 1) / kWinStage) * G;
-    const double sums = (double)items * kWinKeyTile * (double)s.d * 8 / 12e6;
-    int best = 1;
+// Parts of the queries of the key tiles, where the tiles alone do not fill the GPU: so
+// many for the tile with most of them, and as long ones for the others.  A workgroup
+// takes a stage of 64 queries in about 1.5 us (256 run at a time), starting and ending
+// it costs about four of these, joining about two and one for every 12 MB of partial
+// sums.  (Where tiles differ, parts of one length are 7 for the first tile of 4 x 1000
+// causal tokens, 8 heads on 2, d = 64, and 1 for the last: 25 us where 4 for each take 31.)
+struct Parts {
+    int most, stages;
+};
+Parts near_parts(const Sizes& s) {
+    if (!s.any() || s.Nk == 0) return {1, 0};
+    const int64_t tiles = (s.Nk + kWinKeyTile - 1) / kWinKeyTile, heads = s.B * s.Hk, G = s.Hq / s.Hk;
+    if (heads * tiles > 512) return {1, 0};
+    const Window w = window_of(s);
+    const bool chunks = far_chunks(s) > 0;
+    int64_t each[512], longest = 0, all = 0;
+    for (int64_t t = 0; t < tiles; ++t) {
+        each[t] = near_stages(w, (int)s.N, (int)s.Nk, chunks, (int)t).each * G;
+        longest = std::max(longest, each[t]);
+        all += each[t];
+    }
+    Parts best{1, 0};
     double least = 0;
-    for (int64_t k = 1; k <= 16 && k <= all; ++k) {
-        const int64_t rounds = (k * items + 255) / 256;
-        const double cost = (double)(rounds * ((all + k - 1) / k + 4)) + (k > 1 ? 2 + (double)k * sums : 0);
+    for (int64_t k = 1; k <= 16 && k <= longest; ++k) {
+        const int64_t stages = (longest + k - 1) / k;   // at most, in a part
+        int64_t count = 0;
+        for (int64_t t = 0; t < tiles; ++t) count += parts_of((int)k, (int)each[t], (int)stages);
+        count *= heads;
+        const int64_t rounds = (count + 255) / 256;
+        const double mean = (double)(all * heads) / (double)count, last = (double)stages;
+        double cost = rounds == 1 ? last + 4 : (double)rounds * (mean + 4) + (last - mean) / 2;
+        if (k > 1) cost += 2 + (double)count * kWinKeyTile * (double)s.d * 8 / 12e6;
         if (k == 1 || cost < least) {
-            best = (int)k;
+            best = {(int)k, (int)stages};
             least = cost;
         }
     }
@@ -204,7 +221,7 @@ int check_bwd(const Sizes& s) {
     if (s.B * s.Hk > 0 && s.Nk >= (kMaxRows + s.B * s.Hk - 1) / (s.B * s.Hk)) return MOA_ERR_UNSUPPORTED;
     const int64_t tiles = (s.Nk + kWinKeyTile - 1) / kWinKeyTile;
     const int64_t more = s.left < 0 ? 0 : 64 + tiles;   // chunks, of one tile or of many with one each
-    const int parts = near_parts(s);
+    const int parts = near_parts(s).most;
     if (s.B * s.Hk * (tiles * parts + more) > kMaxBlocks / 2) return MOA_ERR_UNSUPPORTED;   // of 512 threads
     const int64_t joined = parts > 1 ? tiles : far_chunks(s) ? win_sink_tiles(window_of(s), (int)s.Nk) : 0;
     if (s.B * s.Hk * joined > kMaxBlocks / (s.d / 4)) return MOA_ERR_UNSUPPORTED;   // d/4 of them for a tile's two sums
@@ -260,7 +277,7 @@ int moa_win_attn_fwd(const void* Q, const void* K, const void* V, void* O, float
 size_t moa_win_attn_bwd_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t Nq, int64_t Nk,
                                         int64_t d, int64_t left, int64_t right, int64_t sinks) {
     const Sizes s{B, Hq, Hk, Nq, Nk, d, left, right, sinks};
-    return check_bwd(s) ? 0 : align256((size_t)(B * Hq * Nq) * 4) + part_bytes(s, near_parts(s), far_chunks(s));
+    return check_bwd(s) ? 0 : align256((size_t)(B * Hq * Nq) * 4) + part_bytes(s, near_parts(s).most, far_chunks(s));
 }
 
 int moa_win_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO,
@@ -296,8 +313,9 @@ int moa_win_attn_bwd(const void* Q, const void* K, const void* V, const void* O,
     if (s.any() && !LSE) return MOA_ERR_INVALID_ARG;
     if (B == 0 || (!s.any() && Nk == 0)) return MOA_OK;
     const size_t stats = (size_t)(B * Hq * Nq) * 4;
-    const int parts = near_parts(s), chunks = far_chunks(s);
-    const size_t need = align256(stats) + part_bytes(s, parts, chunks);
+    const Parts parts = near_parts(s);
+    const int chunks = far_chunks(s);
+    const size_t need = align256(stats) + part_bytes(s, parts.most, chunks);
     if (need && (!workspace || workspace_bytes < need)) return MOA_ERR_WORKSPACE;
     Buf all[10];
     for (int i = 0; i < 8; ++i) all[i] = {t[i].p, extent_bytes(t[i].s, B, t[i].H, t[i].N, d, t[i].es)};
@@ -317,7 +335,8 @@ int moa_win_attn_bwd(const void* Q, const void* K, const void* V, const void* O,
     p.o_bf16 = o_dtype == MOA_BF16;
     p.dsum = static_cast<float*>(workspace);
     p.part = need > align256(stats) ? reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(stats)) : nullptr;
-    p.parts = parts;
+    p.parts = parts.most;
+    p.part_stages = parts.stages;
     p.chunks = chunks;
     return hip_status(launch_win_bwd(p, static_cast<hipStream_t>(stream)));
 }

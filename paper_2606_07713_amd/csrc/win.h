@@ -92,7 +92,9 @@ struct WinGrad {
     Div group, per_item, heads;   // set by the launcher, as in WinAttn
     float* dsum;               // [B][hq][nq]: <dO, O> of every row
     float* part;               // partial sums of dK and dV
-    int parts;                 // of every key tile's queries (1: whole)
+    int parts;                 // of a key tile's queries at most (1: whole)
+    int part_stages;           // stages that a part has at most
+    int near_items;            // set by the launcher: parts of all tiles
     int chunks;                // of the queries behind the first keys' windows (0: none)
 };
 
@@ -103,6 +105,29 @@ constexpr int kWinKeyTile = 128, kWinStage = 64;
 inline int win_sink_tiles(const Window& w, int nk) {
     const int sinks = w.sinks < nk ? w.sinks : nk;
     return w.left == kNoLimit ? 0 : (sinks + kWinKeyTile - 1) / kWinKeyTile;
+}
+
+// The stages of one head whose queries see a key of tile kt, but for those that see
+// only first keys of it and have chunks of their own; near_hi: the last query of those
+// whose windows reach the tile.
+struct Near {
+    int first, each, near_hi;
+};
+constexpr Near near_stages(const Window& w, int nq, int nk, bool chunks, int kt) {
+    const long long off = (long long)nk - nq, last = nq - 1;
+    const int k0 = kt * kWinKeyTile, k1 = (k0 + kWinKeyTile < nk ? k0 + kWinKeyTile : nk) - 1;
+    const long long from = w.right == kNoLimit ? 0 : k0 - off - w.right, to = w.left == kNoLimit ? last : k1 - off + w.left;
+    const int lo = (int)(from < 0 ? 0 : from > nq ? nq : from);
+    const int near_hi = (int)(to < -1 ? -1 : to > last ? last : to);
+    const int hi = k0 < w.sinks && !chunks ? (int)last : near_hi, first = lo / kWinStage;
+    return {first, hi < lo ? 0 : hi / kWinStage + 1 - first, near_hi};
+}
+// Into how many parts these stages of all heads are cut: long lists into more, so that
+// all workgroups take about as long.
+constexpr int parts_of(int most, int stages, int part_stages) {
+    if (most == 1) return 1;
+    const int n = (stages + part_stages - 1) / part_stages;
+    return n < 1 ? 1 : n > most ? most : n;
 }
 
 hipError_t launch_win_bwd(const WinGrad& p, hipStream_t stream);

@@ -24,8 +24,8 @@
 // * The first keys stay visible to all later queries, so their sums would be as long
 //   as the sequence where all others are as long as the window.  The queries behind
 //   their windows are cut into chunks with workgroups of their own, and where there
-//   are few key tiles the queries of every tile into parts; they leave fp32 sums that
-//   win_join adds in a fixed order.
+//   are few key tiles the tiles' queries into parts, about as long as each other; they
+//   leave fp32 sums that win_join adds in a fixed order.
 // No atomics; deterministic.  P and dS are rounded to bf16 for the matrix products.
 // Rows whose sums do not come out finite are done again by the definition.
 //
@@ -383,7 +383,10 @@ struct Stages {
     int first, each, begin, count;
 };
 
-// Partial sums: of every tile those of its parts, of the first keys' tiles those of
+__device__ __forceinline__ Near near_of(const WinGrad& p, int kt) { return near_stages(p.w, p.nq, p.nk, p.chunks > 0, kt); }
+__device__ __forceinline__ int parts_of(const WinGrad& p, const Near& x) { return moa::parts_of(p.parts, x.each * (int)p.group.n, p.part_stages); }
+
+// Partial sums: of every tile room for all parts, of the first keys' tiles those of
 // their chunks behind them; none of a tile with one part and no chunks.  The first
 // ones of tile kt of key/value head bh.
 __device__ __forceinline__ size_t first_part(const WinGrad& p, int sink_tiles, int bh, int kt) {
@@ -414,28 +417,48 @@ __global__ __launch_bounds__(KW * 64, 1) void win_dkdv_kernel(WinGrad p, float c
     // Items of a head: the parts of every tile's queries whose windows reach it, then
     // the chunks of the far queries of the first keys' tiles, short ones that fill up
     // the last round.
-    const int near_items = (p.nk + KT - 1) / KT * p.parts;
-    const bool far = item >= near_items;
-    const int kt = far ? (item - near_items) / p.chunks : item / p.parts;
-    const int cuts = far ? p.chunks : p.parts, cut = far ? (item - near_items) % p.chunks : item % p.parts;
-    const int k0 = kt * KT, k1 = min(k0 + KT, p.nk) - 1;
+    const bool far = item >= p.near_items;
+    int kt = item, cut = 0;
+    if (far) {
+        kt = (item - p.near_items) / p.chunks;
+        cut = (item - p.near_items) % p.chunks;
+    } else if (p.parts > 1) {
+        // The tile among whose parts the item is: a tile a lane.  (A part's number beyond
+        // its tile's, with room for all parts in the grid, left whole shader engines idle:
+        // 31 -> 36 us for the parts that take 25 without gaps.)
+        const int key_tiles = (p.nk + KT - 1) / KT;
+        for (int t0 = 0, before = 0;; t0 += 64) {
+            if (t0 >= key_tiles) return;
+            const int t = t0 + lane, n = t < key_tiles ? parts_of(p, near_of(p, t)) : 0;
+            int sum = n;
+#pragma unroll
+            for (int s = 1; s < 64; s <<= 1) {
+                const int below = __shfl_up(sum, s);
+                if (lane >= s) sum += below;
+            }
+            const uint64_t past = __ballot(before + sum > item);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                kt = t0 + l;
+                cut = item - before - __builtin_amdgcn_readlane(sum - n, l);
+                break;
+            }
+            before += __builtin_amdgcn_readlane(sum, 63);
+        }
+    }
+    const int k0 = kt * KT;
     const bool split = kt < sink_tiles && p.chunks > 0;
 
     Stages st;
     {
-        // Windows alone decide of the near queries where the far ones have chunks.
-        const long long off = (long long)p.nk - p.nq;
-        const int lo = seen_of_key(p, k0).lo;
-        int hi = seen_of_key(p, k1).hi;
-        const int near_hi = (int)max(-1ll, min((long long)p.nq - 1, k1 - off + (long long)p.w.left));
-        if (k0 < p.w.sinks) hi = split ? near_hi : p.nq - 1;
-        int first = lo / SR, end = hi < lo ? first : hi / SR + 1;
+        const Near x = near_of(p, kt);
+        st.first = x.first;
+        st.each = x.each;
         if (far) {
-            first = max(lo / SR, (near_hi + SR) / SR);   // the stage behind near_hi's
-            end = max(first, (p.nq + SR - 1) / SR);
+            st.first = max(x.first, (x.near_hi + SR) / SR);   // the stage behind near_hi's
+            st.each = max(0, (p.nq + SR - 1) / SR - st.first);
         }
-        st.first = first;
-        st.each = end - first;
+        const int cuts = far ? p.chunks : parts_of(p, x);
         const int all = st.each * G, per = (all + cuts - 1) / cuts;
         st.begin = min(all, cut * per);
         st.count = min(per, all - st.begin);
@@ -688,13 +711,17 @@ __global__ __launch_bounds__(256) void win_join_kernel(WinGrad p, int tiles, int
     const int key = kt * KT + e4 / (D / 4), e = e4 % (D / 4) * 4;
     if (key >= p.nk) return;
     // chunks hold sums of the first keys alone
-    const int n = p.parts + (kt < sink_tiles && key < p.w.sinks ? p.chunks : 0);
+    const int near = parts_of(p, near_of(p, kt));
+    const int n = near + (kt < sink_tiles && key < p.w.sinks ? p.chunks : 0), over = p.parts - near;
     const float* at = p.part + (first_part(p, sink_tiles, bh, kt) * 2 + role) * KT * D + (size_t)e4 * 4;
     f32x4 sum = {0, 0, 0, 0};
     for (int i = 0; i < n; i += 4) {
         f32x4 y[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const f32x4*>(at + (size_t)min(i + u, n - 1) * 2 * KT * D);
+        for (int u = 0; u < 4; ++u) {
+            const int x = min(i + u, n - 1);
+            y[u] = *reinterpret_cast<const f32x4*>(at + (size_t)(x < near ? x : x + over) * 2 * KT * D);
+        }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
             if (i + u < n) sum += y[u];
@@ -721,7 +748,13 @@ hipError_t go(WinGrad p, hipStream_t stream) {
     }
     if (p.nk == 0) return hipSuccess;
     const int key_tiles = (p.nk + KT - 1) / KT, sink_tiles = p.chunks ? win_sink_tiles(p.w, p.nk) : 0;
-    const int items = key_tiles * p.parts + sink_tiles * p.chunks;
+    p.near_items = key_tiles;
+    if (p.parts > 1) {
+        p.near_items = 0;
+        for (int t = 0; t < key_tiles; ++t)
+            p.near_items += moa::parts_of(p.parts, near_stages(p.w, p.nq, p.nk, p.chunks > 0, t).each * (p.hq / p.hk), p.part_stages);
+    }
+    const int items = p.near_items + sink_tiles * p.chunks;
     hipError_t e = launch_kernel(win_dkdv_kernel<D>, dim3((unsigned)groups * items), dim3(KW * 64), stream, p, c, sink_tiles);
     const int joined = p.parts > 1 ? key_tiles : sink_tiles;
     if (e != hipSuccess || !joined) return e;

@@ -141,6 +141,17 @@ def test_what_does_not_see_each_other_has_no_part(d, what):
                 close(g[:, :, 3:far], want[:, :, 3:far], bound[:, :, 3:far])
 
 
+@pytest.mark.parametrize("Nq,Nk,left,right,sinks", [(300, 9000, -1, -1, 0), (1500, 8300, 700, 0, 5), (4300, 8400, -1, 0, 0),
+                                                     (2000, 1000, -1, 300, 0), (1000, 3000, 100, 900, 300), (3000, 2900, 2000, 0, 130)])
+def test_tiles_of_different_length(Nq, Nk, left, right, sinks):
+    """Few key tiles, or many of a single head, seen by many queries or by few: their parts are as long as
+    each other, so tiles have different numbers of them."""
+    import paper_2606_07713_amd as moa
+    assert moa.moa_win_attn_bwd_workspace_bytes(1, 2, 1, Nq, Nk, 64, left, right, sinks) > 4 * 2 * Nq + (1 << 16)   # some
+    q, k, v = _normal(60, 1, 2, Nq, 64), _normal(61, 1, 1, Nk, 64), _normal(62, 1, 1, Nk, 64)
+    _check(q, k, v, _normal(63, 1, 2, Nq, 64), left, right, sinks)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("Hq,Hk,N,left,right,sinks", [(2, 2, 300, 0, 0, 0), (8, 2, 333, 1, 0, 0), (4, 4, 700, 7, 0, 1), (6, 2, 200, 5, 20, 2),
                                                       (64, 4, 600, 40, 0, 3), (4, 1, 60, -1, 0, 0)])
