@@ -21,6 +21,20 @@ constexpr float kLn2 = 0.6931471805599453f;
 // 2^x on the hardware transcendental unit (v_exp_f32).
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// 2^x, x <= 0, as a product: v_exp_f32 gives 0 below -126, and a factor between two
+// references that far apart may meet a sum of 2^127 against the lower one.  From -252 on
+// every such sum counts; above -126 `rest` is 1, and the product the plain factor.
+struct TwoFactors {
+    float a, rest;
+    __device__ __forceinline__ explicit TwoFactors(float x) {
+        const float near = fmaxf(x, -126.0f);
+        a = exp2_hw(near);
+        rest = exp2_hw(x - near);   // (of a NaN: NaN)
+    }
+    template <typename V>
+    __device__ __forceinline__ V of(V y) const { return y * rest * a; }
+};
+
 // bf16 bit pattern -> fp32 (exact).
 __device__ __forceinline__ float bf16lo_to_f32(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16hi_to_f32(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }

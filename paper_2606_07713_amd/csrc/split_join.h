@@ -17,9 +17,12 @@ struct SplitJoin {
     bool out_bf16;
 };
 
-// Splits without a visible key have a reference of -inf and sums of 0.  With few
-// rows the pass is a chain of load latencies, so W = 4 waves share a row of more
-// than 4 splits, each takes U of its splits at a time, and all of these loads are
+// Splits without a visible key have a reference of -inf and sums of 0.  Sums of others
+// need not be near their references: one of 2^120 against the lowest reference counts
+// beside one of 2^-40 against the highest, so references are met in two factors.
+//
+// With few rows the pass is a chain of load latencies, so W = 4 waves share a row of
+// more than 4 splits, each takes U of its splits at a time, and all of these loads are
 // in flight together: up to 32 splits cost one latency.  From 2048 rows on there
 // are enough waves with one for each (us by one wave a row and by four, d = 128:
 // 512 rows of 16 splits 4.8 and 3.9, 1024 of 16 5.4 and 4.8, 1024 of 5 4.0 and 4.3;
@@ -55,16 +58,18 @@ __global__ __launch_bounds__(256) void split_join_kernel(SplitJoin p) {
             if (s0 + u * W >= p.splits) ms[u] = kNegInf;
             top = fmaxf(top, ms[u]);
         }
-        const float alpha = M == kNegInf ? 0.0f : exp2_hw(M - top);
+        if (M != kNegInf) {   // (else nothing yet)
+            const TwoFactors alpha(M - top);
+            L = alpha.of(L);
+            o = alpha.of(o);
+        }
         M = top;
-        L *= alpha;
-        o *= alpha;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (ms[u] == kNegInf) continue;
-            const float w = exp2_hw(ms[u] - M);
-            L += w * ls[u];
-            o += w * a[u];
+            const TwoFactors w(ms[u] - M);
+            L += w.of(ls[u]);
+            o += w.of(a[u]);
         }
     }
     // nothing was written for rows behind the new tokens, and nothing is
@@ -80,9 +85,9 @@ __global__ __launch_bounds__(256) void split_join_kernel(SplitJoin p) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             if (part_m[w] == kNegInf) continue;
-            const float f = exp2_hw(part_m[w] - top);
-            L += f * part_l[w];
-            o += f * part[w][lane];
+            const TwoFactors f(part_m[w] - top);
+            L += f.of(part_l[w]);
+            o += f.of(part[w][lane]);
         }
         M = top;
     }

@@ -13,7 +13,9 @@
 // sees any; all others are weighed against it as they come.  fp32 and bf16 hold
 // weights up to 2^127 as well as small ones, so the reference need not follow the
 // maximum: only a row whose scores rise by more than 127 log2 units (88 of the
-// exponent) above it comes out infinite, and is done by the definition.  (Raised in
+// exponent) above it comes out infinite, and is done by the definition.  A state's sums
+// may then be 2^127 against its reference, so where states meet, of two key streams or
+// of splits, the one with the lower reference is never left out for that.  (Raised in
 // the loop where sums grew, the rarely taken branch cost a copy of all sums in every
 // step: 4096 tokens in a window of 512, 114 us.)  The sums are of the fp32 weights.  A weight
 // meets V as one bf16 number for a bf16 output (2^-9 each, which leaves the error
@@ -261,13 +263,16 @@ __global__ __launch_bounds__(KS * MW * 64, KS == 1 && (D == 64 || BN == 32) ? 3 
         __syncthreads();
         if (stream == 1) return;
         const float r = state[wave][0][lane], top = fmaxf(ref, r);
-        const float a = ref == kNegInf ? 0.0f : exp2_hw(ref - top), c1 = r == kNegInf ? 0.0f : exp2_hw(r - top);
-        // (a sum without a reference is 0, or NaN of a score that is)
-        l = (ref == kNegInf ? l : l * a) + (r == kNegInf ? state[wave][1][lane] : state[wave][1][lane] * c1);
+        // (sums without a reference are 0, or NaN of a score that is)
+        const TwoFactors mine(ref == kNegInf ? 0.0f : ref - top), its(r == kNegInf ? 0.0f : r - top);
+        {
+#pragma clang fp contract(off)   // a row's sum is the same from either stream
+            l = mine.of(l) + its.of(state[wave][1][lane]);
+        }
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) oacc[d][i] = oacc[d][i] * a + x[(d * 16 + i) * 64 + lane] * c1;
+            for (int i = 0; i < 16; ++i) oacc[d][i] = __builtin_fmaf(oacc[d][i] * mine.rest, mine.a, its.of(x[(d * 16 + i) * 64 + lane]));
         ref = top;
     }
     if (!live) return;
