@@ -247,10 +247,12 @@ __device__ void row_by_definition(const WinAttn& p, int b, int h, const u16* q, 
         for (int s = 1; s < 64; s <<= 1) m = fmax(m, __shfl_xor(m, s));
         any = true;
         const double top = fmax(M, m);
-        double w = page >= 0 ? (double)exp2_hw((float)(x - top)) : 0.0;
+        // A score that is NaN is not in M, but makes L one; one of -inf counts nothing,
+        // also where there is no other yet.
+        double w = x == -__builtin_inf() ? 0.0 : (double)exp2_hw((float)(x - top));
 #pragma unroll
         for (int s = 1; s < 64; s <<= 1) w += __shfl_xor(w, s);
-        L = (M == -__builtin_inf() ? 0.0 : L * (double)exp2_hw((float)(M - top))) + w;
+        L = (M == -__builtin_inf() ? L : L * (double)exp2_hw((float)(M - top))) + w;
         M = top;
     });
 #pragma unroll
@@ -299,7 +301,8 @@ __device__ __forceinline__ void store_row(const WinAttn& p, int b, int hh, int q
         if (p.out_bf16) static_cast<__bf16*>(p.o)[to + e] = (__bf16)o[e];
         else static_cast<float*>(p.o)[to + e] = o[e];
     }
-    if (p.lse && lane == 0) p.lse[at] = ref == kNegInf ? kNegInf : (ref + __log2f(sum)) * kLn2;
+    // (a sum of 0 without a reference: -inf; NaN: NaN)
+    if (p.lse && lane == 0) p.lse[at] = (ref + __log2f(sum)) * kLn2;
 }
 
 }  // namespace win
