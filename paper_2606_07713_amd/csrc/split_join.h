@@ -17,6 +17,12 @@ struct SplitJoin {
     bool out_bf16;
 };
 
+// States that ask for their row to be done another way have a reference of NaN; no state
+// of these kernels does.
+struct NoRows {
+    static constexpr bool any = false;
+};
+
 // Splits without a visible key have a reference of -inf and sums of 0.  Sums of others
 // need not be near their references: one of 2^120 against the lowest reference counts
 // beside one of 2^-40 against the highest, so references are met in two factors.
@@ -27,8 +33,8 @@ struct SplitJoin {
 // are enough waves with one for each (us by one wave a row and by four, d = 128:
 // 512 rows of 16 splits 4.8 and 3.9, 1024 of 16 5.4 and 4.8, 1024 of 5 4.0 and 4.3;
 // 2048 of 16 5.9 and 6.7, 8192 of 8 7.4 and 17.3; 512 of 4 3.3 and 3.9).
-template <int D, int W>
-__global__ __launch_bounds__(256) void split_join_kernel(SplitJoin p) {
+template <int D, int W, typename Again>
+__global__ __launch_bounds__(256) void split_join_kernel(SplitJoin p, Again again) {
     constexpr int PER = D / 64, U = W == 1 ? 4 : 8;
     typedef float vec __attribute__((ext_vector_type(PER)));
     __shared__ vec part[4][64];
@@ -43,6 +49,7 @@ __global__ __launch_bounds__(256) void split_join_kernel(SplitJoin p) {
     const float* ml = p.ws + (size_t)p.B * p.hq * p.n * p.splits * D + (size_t)row * p.splits * 2;
     float M = kNegInf, L = 0.0f;
     vec o = 0.0f;
+    bool asks = false;
     for (int s0 = W == 1 ? 0 : wave; s0 < p.splits; s0 += U * W) {
         float ms[U], ls[U], top = M;
         vec a[U];
@@ -55,6 +62,7 @@ __global__ __launch_bounds__(256) void split_join_kernel(SplitJoin p) {
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            if constexpr (Again::any) asks |= ms[u] != ms[u];
             if (s0 + u * W >= p.splits) ms[u] = kNegInf;
             top = fmaxf(top, ms[u]);
         }
@@ -76,9 +84,12 @@ __global__ __launch_bounds__(256) void split_join_kernel(SplitJoin p) {
     if (p.new_lens && i >= min(max(p.new_lens[b], 0), p.n)) return;
     if constexpr (W > 1) {
         part[wave][lane] = o;
-        if (lane == 0) { part_m[wave] = M; part_l[wave] = L; }
+        if (lane == 0) { part_m[wave] = asks ? __builtin_nanf("") : M; part_l[wave] = L; }
         __syncthreads();
         if (wave != 0) return;
+        if constexpr (Again::any)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) asks |= part_m[w] != part_m[w];
         const float top = fmaxf(fmaxf(part_m[0], part_m[1]), fmaxf(part_m[2], part_m[3]));
         L = 0.0f;
         o = 0.0f;
@@ -91,6 +102,11 @@ __global__ __launch_bounds__(256) void split_join_kernel(SplitJoin p) {
         }
         M = top;
     }
+    if constexpr (Again::any)
+        if (wave_any(asks)) {
+            again.template row<D>(b, hh, i);
+            return;
+        }
     const bool none = M == kNegInf;   // no visible key
     o *= none ? 0.0f : 1.0f / L;
     const long long to = b * p.os[0] + hh * p.os[1] + i * p.os[2] + PER * lane;
@@ -103,12 +119,12 @@ __global__ __launch_bounds__(256) void split_join_kernel(SplitJoin p) {
     if (p.lse && lane == 0) p.lse[row] = none ? kNegInf : (M + __log2f(L)) * kLn2;
 }
 
-template <int D>
-hipError_t launch_split_join(const SplitJoin& p, hipStream_t stream) {
+template <int D, typename Again = NoRows>
+hipError_t launch_split_join(const SplitJoin& p, hipStream_t stream, const Again& again = {}) {
     const long long all = (long long)p.B * p.hq * p.n;
     if (p.splits <= 4 || all >= 2048)
-        return launch_kernel(split_join_kernel<D, 1>, dim3((unsigned)((all + 3) / 4)), dim3(256), stream, p);
-    return launch_kernel(split_join_kernel<D, 4>, dim3((unsigned)all), dim3(256), stream, p);
+        return launch_kernel(split_join_kernel<D, 1, Again>, dim3((unsigned)((all + 3) / 4)), dim3(256), stream, p, again);
+    return launch_kernel(split_join_kernel<D, 4, Again>, dim3((unsigned)all), dim3(256), stream, p, again);
 }
 
 }  // namespace moa

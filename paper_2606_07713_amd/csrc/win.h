@@ -68,6 +68,8 @@ inline void set_divisions(WinAttn& p) {
 // the sums (of weights of at most 1).
 constexpr int kMaxSplits = 256;
 constexpr float kStateShift = 40.0f;
+// From here on an fp32 reference would be off by more than 8 log2 units.
+constexpr double kLargestReference = 0x1p28;
 
 // Rows (queries times the query heads of a key/value head) that a workgroup
 // takes: 16 or 32 in the kernel of few rows, 128 in that of many.

@@ -145,8 +145,8 @@ struct Tiles {
 };
 
 // <a, b> of two rows of D elements as T sums it, in one order; a is the same row in all
-// lanes.  (The loads of eight pieces are in flight together.)
-template <int D, typename T>
+// lanes.  (The loads of U pieces are in flight together.)
+template <int D, int U, typename T>
 __device__ __forceinline__ T dot_as(const u16* a, const u16* b) {
 #pragma clang fp contract(off)
     T x = 0;
@@ -154,15 +154,15 @@ __device__ __forceinline__ T dot_as(const u16* a, const u16* b) {
     const uint64_t uniform = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
     const u32x4* q = reinterpret_cast<const u32x4*>(uniform);
 #pragma unroll 1
-    for (int e = 0; e < D; e += 64) {
-        u32x4 u[8], v[8];
+    for (int e = 0; e < D; e += 8 * U) {
+        u32x4 u[U], v[U];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < U; ++i) {
             u[i] = q[e / 8 + i];
             v[i] = *reinterpret_cast<const u32x4*>(b + e + 8 * i);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < U; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 x = __builtin_elementwise_fma((T)bf16lo_to_f32(u[i][j]), (T)bf16lo_to_f32(v[i][j]), x);
@@ -172,25 +172,24 @@ __device__ __forceinline__ T dot_as(const u16* a, const u16* b) {
     return x;
 }
 // In fp32, or in fp64 what that does not hold.
-template <int D>
+template <int D, int U = 8>
 __device__ __forceinline__ double dot(const u16* a, const u16* b) {
-    const float x = dot_as<D, float>(a, b);
-    return __builtin_isfinite(x) ? (double)x : dot_as<D, double>(a, b);
+    const float x = dot_as<D, U, float>(a, b);
+    return __builtin_isfinite(x) ? (double)x : dot_as<D, U, double>(a, b);
 }
 
 // Adds the lanes' w times their rows to o, this lane's elements D/64 lane ..; row(j):
-// lane j's row, only taken where its bit of `which` is set.  Eight at a time are in
-// flight.
-template <int D, typename F>
+// lane j's row, only taken where its bit of `which` is set.  U at a time are in flight.
+template <int D, int U = 8, typename F>
 __device__ __forceinline__ void add_rows(float (&o)[D / 64], uint64_t which, float w, F row) {
     constexpr int E = D / 64;
     const int lane = threadIdx.x & 63;
 #pragma unroll 1
     while (which) {
-        uint32_t bits[8];
-        float f[8];
+        uint32_t bits[U];
+        float f[U];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
+        for (int u = 0; u < U; ++u) {
             const bool one = which != 0;
             const int j = one ? __builtin_ctzll(which) : 0;
             f[u] = one ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j)) : 0.0f;
@@ -203,7 +202,7 @@ __device__ __forceinline__ void add_rows(float (&o)[D / 64], uint64_t which, flo
             which &= which - 1;
         }
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
+        for (int u = 0; u < U; ++u) {
             o[0] = __builtin_fmaf(f[u], bf16lo_to_f32(bits[u]), o[0]);
             if constexpr (E == 2) o[1] = __builtin_fmaf(f[u], bf16hi_to_f32(bits[u]), o[1]);
         }
@@ -216,8 +215,10 @@ __device__ __forceinline__ void add_rows(float (&o)[D / 64], uint64_t which, flo
 // value that is infinite or NaN (which a product with a weight of 0 spreads to
 // rows that do not see it), or a score or a sum beyond fp32.  o: this lane's
 // elements D/64 lane ..; without `partial` divided by the sum, with it the state
-// of a split.
-template <int D, int T>
+// of a split: its weights count against the fp32 number that its reference is.  Where
+// that would leave fp32 too, or there is none, the reference is NaN, and the join does
+// the whole row (RowsAgain).
+template <int D, int T, int U = 8>
 __device__ void row_by_definition(const WinAttn& p, int b, int h, const u16* q, const Seen& seen, const Tiles<T>& tiles,
                                   int begin, int end, bool partial, float (&o)[D / 64], float& ref, float& sum) {
     // Both walks have to see the same scores, bit for bit: of one of 2^100 a single
@@ -225,9 +226,10 @@ __device__ void row_by_definition(const WinAttn& p, int b, int h, const u16* q, 
 #pragma clang fp contract(off)
     constexpr int E = D / 64;
     const int lane = threadIdx.x & 63;
-    const double c = (double)p.scale * 1.4426950408889634;
+    // (the factor of the tile kernels: states of both kinds meet)
+    const double c = p.scale * kLog2e;
     const auto score = [&](int key, int page) {
-        return dot<D>(q, static_cast<const u16*>(p.s.k) + key_offset(p.s.ks, p.s.shift, page, h, key)) * c;
+        return dot<D, U>(q, static_cast<const u16*>(p.s.k) + key_offset(p.s.ks, p.s.shift, page, h, key)) * c;
     };
     const auto walk = [&](auto f) {
 #pragma unroll 1
@@ -260,41 +262,32 @@ __device__ void row_by_definition(const WinAttn& p, int b, int h, const u16* q, 
     ref = kNegInf;
     sum = 0.0f;
     if (!any) return;
-    const double inv = partial ? 0x1p-40 : 1.0 / L;
-    static_assert(kStateShift == 40.0f);
+    double inv = 1.0 / L;
+    ref = (float)M;
+    if (partial) {
+        ref = (float)(M + (double)kStateShift);
+        if (!(__builtin_fabs(M) < kLargestReference)) {
+            ref = sum = __builtin_nanf("");
+            return;
+        }
+        const double rest = M - (double)ref, whole = __builtin_rint(rest);
+        inv = __builtin_ldexp((double)exp2_hw((float)(rest - whole)), (int)whole);
+    }
+    sum = (float)(partial ? L * inv : L);
     walk([&](int k0, int key, int page) {
 #pragma clang fp contract(off)
         const float w = page >= 0 ? (float)((double)exp2_hw((float)(score(key, page) - M)) * inv) : 0.0f;
-        add_rows<D>(o, __ballot(page >= 0), w, [&](int j) {
+        add_rows<D, U>(o, __ballot(page >= 0), w, [&](int j) {
             return static_cast<const u16*>(p.s.v) + key_offset(p.s.vs, p.s.shift, __builtin_amdgcn_readlane(page, j), h, k0 + j);
         });
     });
-    // A reference that is not finite would drop out of a join.
-    const bool finite = M > -3e38 && M < 3e38;
-    ref = !partial ? (float)M : finite ? (float)(M + (double)kStateShift) : 0.0f;
-    sum = finite ? (float)(partial ? L * inv : L) : __builtin_nanf("");
-    if (!finite && partial)
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = __builtin_nanf("");
 }
 
-// Stores such a row: O and LSE, or the state of split sp.
+// Stores such a row: O and LSE.
 template <int D>
-__device__ __forceinline__ void store_row(const WinAttn& p, int b, int hh, int qi, int sp, const float (&o)[D / 64],
-                                          float ref, float sum) {
+__device__ __forceinline__ void store_output(const WinAttn& p, int b, int hh, int qi, const float (&o)[D / 64], float ref, float sum) {
     constexpr int E = D / 64;
     const int lane = threadIdx.x & 63;
-    const size_t at = ((size_t)b * p.hq + hh) * p.n + qi;
-    if (p.splits > 1) {
-        float* ml = p.ws + (size_t)p.B * p.hq * p.n * p.splits * D + (at * p.splits + sp) * 2;
-#pragma unroll
-        for (int e = 0; e < E; ++e) p.ws[(at * p.splits + sp) * D + E * lane + e] = o[e];
-        if (lane == 0) {
-            ml[0] = ref;
-            ml[1] = sum;
-        }
-        return;
-    }
     const long long to = b * p.os[0] + hh * p.os[1] + qi * p.os[2] + E * lane;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -302,8 +295,43 @@ __device__ __forceinline__ void store_row(const WinAttn& p, int b, int hh, int q
         else static_cast<float*>(p.o)[to + e] = o[e];
     }
     // (a sum of 0 without a reference: -inf; NaN: NaN)
-    if (p.lse && lane == 0) p.lse[at] = (ref + __log2f(sum)) * kLn2;
+    if (p.lse && lane == 0) p.lse[((size_t)b * p.hq + hh) * p.n + qi] = (ref + __log2f(sum)) * kLn2;
 }
+
+// The same, or the state of split sp.
+template <int D>
+__device__ __forceinline__ void store_row(const WinAttn& p, int b, int hh, int qi, int sp, const float (&o)[D / 64],
+                                          float ref, float sum) {
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+    if (p.splits == 1) return store_output<D>(p, b, hh, qi, o, ref, sum);
+    const size_t at = ((size_t)b * p.hq + hh) * p.n + qi;
+    float* ml = p.ws + (size_t)p.B * p.hq * p.n * p.splits * D + (at * p.splits + sp) * 2;
+#pragma unroll
+    for (int e = 0; e < E; ++e) p.ws[(at * p.splits + sp) * D + E * lane + e] = o[e];
+    if (lane == 0) {
+        ml[0] = ref;
+        ml[1] = sum;
+    }
+}
+
+// The join's rows with a state that asks for it: all splits at once by the definition.
+struct RowsAgain {
+    static constexpr bool any = true;
+    WinAttn p;
+    template <int D>
+    __device__ __forceinline__ void row(int b, int hh, int qi) const {
+        const KeySource& src = p.s;
+        const int len = length(src, b);
+        const Seen seen = seen_from(p.w, (long long)len - new_tokens(src.new_lens, b, p.n) + qi, max(0, min(len, capacity(src))));
+        const Tiles<64> tiles(seen, seen, p.w.sinks);
+        float f[D / 64], M, L;
+        // (two loads in flight: the join of all others keeps its registers)
+        row_by_definition<D, 64, 2>(p, b, over(p.group, hh), static_cast<const u16*>(p.q) + b * p.qs[0] + hh * p.qs[1] + qi * p.qs[2],
+                                 seen, tiles, 0, tiles.count, false, f, M, L);
+        store_output<D>(p, b, hh, qi, f, M, L);
+    }
+};
 
 }  // namespace win
 }  // namespace moa

@@ -355,7 +355,7 @@ hipError_t go(WinAttn p, hipStream_t stream) {
     else e = tiles == 1 ? run(win_few_kernel<D, RT, F32, true>) : run(win_few_kernel<D, RT, F32, false>);
     if (e != hipSuccess || p.splits == 1) return e;
     const SplitJoin j{p.ws, p.o, p.lse, p.s.new_lens, {p.os[0], p.os[1], p.os[2]}, p.B, p.hq, p.n, p.splits, p.out_bf16};
-    return launch_split_join<D>(j, stream);
+    return launch_split_join<D>(j, stream, RowsAgain{p});
 }
 
 }  // namespace

@@ -420,7 +420,7 @@ hipError_t go(WinAttn p, hipStream_t stream) {
     const hipError_t e = p.out_bf16 ? go_as(state, one_term) : go_as(state, three_terms);
     if (e != hipSuccess) return e;
     const SplitJoin j{p.ws, p.o, p.lse, p.s.new_lens, {p.os[0], p.os[1], p.os[2]}, p.B, p.hq, p.n, p.splits, p.out_bf16};
-    return launch_split_join<D>(j, stream);
+    return launch_split_join<D>(j, stream, RowsAgain{p});
 }
 
 }  // namespace

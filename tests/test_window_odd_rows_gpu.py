@@ -66,3 +66,68 @@ def test_rows_that_see_nothing_beside_odd_ones(Nq, Nk, splits, d):
         o, lse = moa.win_attn_fwd(q, k, v, -1, 0, return_lse=True, num_splits=splits)
         assert bool((x.lse[:, :, :empty] == -math.inf).all()) and bool((lse[:, :, :empty] == -math.inf).all())
         assert bool((o[:, :, :empty] == 0).all())
+
+
+def _by_scores(q, k, v, scale, splits):
+    """Where a score's fp32 products and sum are exact, only the weights' exponentials (2^-22), their
+    arguments (fp32 numbers below 128, of scores in fp64: 2^-18 and |score| 2^-51), sums and products are off."""
+    import paper_2606_07713_amd as moa
+    s = q.double() @ k.double().repeat_interleave(q.shape[1] // k.shape[1], 1).transpose(2, 3) * scale
+    v = v.double().repeat_interleave(q.shape[1] // v.shape[1], 1)
+    p, lse = torch.softmax(s, -1), torch.logsumexp(s, -1)
+    top = float(torch.where(s.isfinite(), s, 0.0).abs().max())
+    o, got = moa.win_attn_fwd(q, k, v.to(BF16)[:, ::q.shape[1] // k.shape[1]], scale=scale, out_dtype=torch.float32, return_lse=True,
+                              num_splits=splits)
+    torch.cuda.synchronize()
+    close(o, p @ v, (p @ v.abs()) * (2.0 ** -17 + top * 2.0 ** -51) + 1e-30)
+    close(got, lse, lse.abs() * 2.0 ** -21 + 2.0 ** -17)
+
+
+def _one_score(S, sign, Nq, Nk, d, seed):
+    """Keys with scores of sign * 2 S, and q for scores of up to S and small steps beside it."""
+    q, k, v = _normal(seed, 1, 2, Nq, d), _normal(seed + 1, 1, 1, Nk, d), _normal(seed + 2, 1, 1, Nk, d)
+    q.zero_(), k.zero_()
+    q[..., 0], q[..., 1] = 2.0 ** 10, 1
+    k[..., 0] = 0 if sign > 0 else -2 * S / 2.0 ** 10
+    return q, k, v
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Nq", [2, 100])
+@pytest.mark.parametrize("splits", [1, 2, 3, 16])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("S,step", [(2.0 ** 21, 1), (2.0 ** 22, 0.5), (2.0 ** 23, 1), (2.0 ** 28, 32), (2.0 ** 30, 128), (2.0 ** 33, 1024)])
+def test_near_scores_that_are_large(S, step, sign, splits, Nq, d):
+    """Scores of S and a step or two more, in different splits, behind keys that are far below."""
+    q, k, v = _one_score(S, sign, Nq, 1024, d, 20)
+    for n, (key, steps) in enumerate(((40, 1), (500, 0), (700, 2), (990, 2))):
+        k[0, 0, key, 0], k[0, 0, key, 1] = sign * S / 2.0 ** 10, steps * step
+    _by_scores(q, k, v, 1.0, splits)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Nq", [2, 100])
+@pytest.mark.parametrize("splits", [1, 2, 3, 16])
+def test_scores_beyond_fp32(splits, Nq, d):
+    """The result of the definition, whatever the number of splits: one key has all the weight."""
+    import paper_2606_07713_amd as moa
+    q, k, v = _normal(30, 1, 2, Nq, d), _normal(31, 1, 1, 1000, d), _normal(32, 1, 1, 1000, d)
+    q, k = (q.float() * 1e25).to(BF16), (k.float() * 1e25).to(BF16)
+    for left, right in ((-1, -1), (-1, 0), (400, 0)):
+        o = moa.win_attn_fwd(q, k, v, left, right, out_dtype=torch.float32, num_splits=splits)
+        x = _exact(q, k, v, left, right, 0)
+        s = torch.where(x.see, q.double() @ k.double().transpose(2, 3), -math.inf)
+        assert torch.equal(o, v[0, 0][s.argmax(-1)].float())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Nq", [2, 100])
+@pytest.mark.parametrize("splits", [1, 2, 4])
+def test_scores_of_minus_infinity_count_nothing(splits, Nq, d):
+    """All keys of one split or stream, or all but one of the sequence, have a score of -inf."""
+    q, k, v = _normal(33, 1, 2, Nq, d), _normal(34, 1, 1, 512, d), _normal(35, 1, 1, 512, d)
+    q, k = q.abs(), k.abs()
+    for first, end in ((0, 64), (0, 256), (256, 512), (0, 511), (1, 512)):
+        x = k.clone()
+        x[:, :, first:end, 3] = -math.inf
+        _check(q, x, v, num_splits=splits)
