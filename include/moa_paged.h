@@ -102,8 +102,9 @@ size_t moa_paged_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t
  * O, LSE    as for moa_win_attn_fwd, [B][Hq][N][d] and [B][Hq][N].
  * B, Hq, Hk, N, d, page, num_pages, max_pages
  *           B, N, Hq >= 0, Hq a multiple of Hk; supported: d in {64, 128}, max_pages *
- *           page <= 2^30, B * Hq * N < 2^26, and fewer than 2^24 workgroups (of 16, 32
- *           or 128 rows of one key/value head and one split).
+ *           page <= 2^30, B * Hq * N < 2^26 (with num_splits of 2 and more 2^26 - 4 at
+ *           most), and fewer than 2^24 workgroups (of 16, 32 or 128 rows of one
+ *           key/value head and one split).
  * max_len   as above.  Any value is right; a good one is fast.
  * scale, out_dtype, workspace, workspace_bytes, num_splits
  *           as for moa_win_attn_fwd, whose computation this is.

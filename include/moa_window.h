@@ -54,8 +54,9 @@ size_t moa_win_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t N
  *           stride of a dimension of size 1 is ignored.
  * B, Hq, Hk, Nq, Nk, d
  *           All may be 0 but Hk and d; Hq a multiple of Hk; supported: d in {64,
- *           128}, Nq and Nk up to 2^30, B * Hq * Nq < 2^26, and fewer than 2^24
- *           workgroups (of 16, 32 or 128 rows of one key/value head and one split).
+ *           128}, Nq and Nk up to 2^30, B * Hq * Nq < 2^26 (with num_splits of 2 and more
+ *           2^26 - 4 at most), and fewer than 2^24 workgroups (of 16, 32 or 128 rows of
+ *           one key/value head and one split).
  * scale     finite, at most 2^127 in size; 0 and negative values are valid.
  * workspace, workspace_bytes
  *           at least moa_win_attn_workspace_bytes(...) bytes, 16-byte aligned,

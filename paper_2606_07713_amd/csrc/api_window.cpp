@@ -14,11 +14,12 @@ namespace {
 
 using namespace moa;
 
-constexpr int64_t kMaxRows = int64_t(1) << 26;  // B * Hq * N: four rows a workgroup when splits are joined
+constexpr int64_t kMaxRows = int64_t(1) << 26;          // B * Hq * N
 constexpr int64_t kMaxStageStride = int64_t(1) << 23;   // 64 rows' bytes stay in 32 bits
 constexpr float kMaxScale = 0x1p127f;           // times log2(e) is still finite
 // Workgroups of 256 threads in one launch: its threads are counted in 32 bits.
 constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;
+constexpr int64_t kMaxJoinedRows = 4 * kMaxBlocks;      // four rows a workgroup where splits are joined
 
 // The sizes of an attention call; Nk: keys of a sequence, at most; left, right: -1
 // where there is no limit, below kMost else, so that sums of them hold.
@@ -43,6 +44,7 @@ int check_sizes(const Sizes& s, int num_splits) {
     if (s.B * std::max(s.Hq, s.Hk) >= kMaxRows) return MOA_ERR_UNSUPPORTED;
     if (s.B * s.Hq > 0 && s.N >= (kMaxRows + s.B * s.Hq - 1) / (s.B * s.Hq)) return MOA_ERR_UNSUPPORTED;
     if (s.any() && s.groups() > kMaxBlocks / std::max(num_splits, 1)) return MOA_ERR_UNSUPPORTED;
+    if (num_splits > 1 && s.any() && s.B * s.Hq * s.N > kMaxJoinedRows) return MOA_ERR_UNSUPPORTED;   // (by itself none splits so many)
     return MOA_OK;
 }
 
