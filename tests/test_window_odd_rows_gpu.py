@@ -131,3 +131,28 @@ def test_scores_of_minus_infinity_count_nothing(splits, Nq, d):
         x = k.clone()
         x[:, :, first:end, 3] = -math.inf
         _check(q, x, v, num_splits=splits)
+
+
+@pytest.mark.parametrize("N", [2, 40])
+@pytest.mark.parametrize("splits", [1, 3, 7])
+def test_scores_beyond_fp32_over_a_paged_cache(splits, N):
+    """Ragged lengths, fewer new tokens than rows, a page that is not there: one key has all the weight."""
+    import paper_2606_07713_amd as moa
+    from test_paged_gpu import Cache, _i32
+    from win_util import visible
+    lens, new = [700, 90, 333], [N, 1, N - 1]
+    c = Cache(lens, 2, 16, 64)
+    c.table[0, 5] = -1
+    c.k.copy_((c.k.float() * 1e25).to(BF16))
+    q = (_normal(40, 3, 4, N, 64).float() * 1e25).to(BF16)
+    for left, right, sinks in ((-1, 0, 0), (200, 0, 20)):
+        out = torch.full((3, 4, N, 64), 7.0, device="cuda")
+        o, lse = moa.paged_attn_fwd(q, c.k, c.v, _i32(lens), page_table=c.table, new_lens=_i32(new), left=left, right=right,
+                                    sinks=sinks, out_dtype=torch.float32, num_splits=splits, out=out, return_lse=True)
+        for b, n in enumerate(lens):
+            (k, has), (v, _) = c.rows(c.k, b, n), c.rows(c.v, b, n)
+            see = visible(torch.arange(n - new[b], n, device="cuda")[None], n, torch.tensor([n], device="cuda"), left, right, sinks) & has
+            s = q[b, :, :new[b]].double() @ k.repeat_interleave(2, 0).transpose(1, 2)
+            best = torch.where(see, s, -math.inf).argmax(-1)
+            want = v.repeat_interleave(2, 0).gather(1, best[..., None].expand(-1, -1, 64))
+            assert torch.equal(o[b, :, :new[b]].double(), want) and bool((o[b, :, new[b]:] == 7).all())
