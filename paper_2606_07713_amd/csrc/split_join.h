@@ -116,7 +116,15 @@ __global__ __launch_bounds__(256) void split_join_kernel(SplitJoin p, Again agai
     } else {
         *reinterpret_cast<vec*>(static_cast<float*>(p.o) + to) = o;
     }
-    if (p.lse && lane == 0) p.lse[row] = none ? kNegInf : (M + __log2f(L)) * kLn2;
+    if (!p.lse || lane != 0) return;
+    float whole = M, of = L;
+    if constexpr (Again::any)
+        if (L < 0x1p-20f && L > 0.0f) {   // a high reference and a small sum: what they cancel is taken first
+            const int e = __builtin_amdgcn_frexp_expf(L);
+            whole += (float)e;
+            of = ldexpf(L, -e);
+        }
+    p.lse[row] = none ? kNegInf : (whole + __log2f(of)) * kLn2;
 }
 
 template <int D, typename Again = NoRows>

@@ -156,3 +156,15 @@ def test_scores_beyond_fp32_over_a_paged_cache(splits, N):
             best = torch.where(see, s, -math.inf).argmax(-1)
             want = v.repeat_interleave(2, 0).gather(1, best[..., None].expand(-1, -1, 64))
             assert torch.equal(o[b, :, :new[b]].double(), want) and bool((o[b, :, new[b]:] == 7).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Nq", [2, 50])
+def test_log_sums_near_zero_of_splits_by_definition(Nq, d):
+    """Few keys and small scores: LSE keeps the bound of fp32 near 0, whatever the state's reference is."""
+    for Nk in (1, 2, 3, 4, 7, 40):
+        q, k, v = _normal(50 + Nk, 2, 16, Nq, d, std=0.1), _normal(60 + Nk, 2, 2, Nk, d, std=0.1), _normal(70 + Nk, 2, 2, Nk, d)
+        v[0, 1, :1], v[1, 0, Nk - 1:] = math.nan, math.inf
+        for splits in (1, 2, 3, 16):
+            _check(q, k, v, num_splits=splits)
+            _check(q, k, v, -1, 0, 0, num_splits=splits)
