@@ -67,10 +67,13 @@ size_t moa_win_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64_t N
  * the sums of the unrounded weights in fp32.  A weight multiplies V as one bf16
  * number where O is bf16 and a key/value head has more than 32 rows (queries times
  * the query heads that share it), as the sum of two (17 bits) with fewer, and of
- * three (25 bits) where O is fp32.  Keys and values that a row does not see
- * have no part in it, whatever they hold: rows whose sums do not come out finite
- * are done again by the definition, one by one.  One kernel, or two when
- * the keys are split; no atomics, deterministic.
+ * three (all bits of an fp32 number) where O is fp32.  Keys and values that a row does
+ * not see have no part in it, whatever they hold: rows whose sums do not come out
+ * finite (values or scores that are infinite or NaN, values or scores that leave fp32,
+ * scores that rise by 127 log2 units above those of the row's first keys) are done
+ * again by the definition, each by one wave: a call full of such rows takes up to 300
+ * times as long.  LSE is an fp32 number: infinite for scores beyond its range.  One
+ * kernel, or two when the keys are split; no atomics, deterministic.
  */
 int moa_win_attn_fwd(const void* Q, const void* K, const void* V, void* O, float* LSE, int64_t B,
                      int64_t Hq, int64_t Hk, int64_t Nq, int64_t Nk, int64_t d,
@@ -119,7 +122,8 @@ size_t moa_win_attn_bwd_workspace_bytes(int64_t B, int64_t Hq, int64_t Hk, int64
  * bf16 and rows of a tile of 128 see fewer than 64 keys, from the keys: sum_j P_ij
  * <dO_i, V_j>, which has no part of O's rounding.  Rows and keys that do not see each
  * other have no part in each other's gradients, whatever they hold: sums that do not
- * come out finite are done again by the definition.  Two kernels, or three with
+ * come out finite are done again by the definition, each by one wave (up to 150 times as
+ * long where all are).  Two kernels, or three with
  * partial sums; no atomics, deterministic.
  */
 int moa_win_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO,

@@ -15,7 +15,7 @@
 // in a product is free, two such accumulators, packed to bf16, are the B
 // operand of the second product as they are.  That product is taken twice, with
 // the weights' nearest bf16 numbers and with those of what these leave: one
-// bf16 number per weight (2^-9) would be off by as much as a bf16 output is by
+// bf16 number per weight (2^-8) would be off by as much as a bf16 output is by
 // itself, and by far more than an fp32 output.
 //
 // Softmax: a running reference per row, the maximum of the first tile that the

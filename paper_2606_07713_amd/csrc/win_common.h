@@ -27,7 +27,8 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 
 // a and b as sums of TERMS bf16 numbers each, every one the nearest to what the ones
-// before it leave (8 bits and a sign: 2^-9, 2^-18, 2^-27 of a weight at most is lost).
+// before it leave: at most 2^-8 or 2^-17 of a weight is lost with one or two, and nothing of
+// an fp32 number with three.
 template <int TERMS>
 __device__ __forceinline__ void bf16_terms(float a, float b, uint32_t (&w)[TERMS]) {
 #pragma unroll

@@ -12,8 +12,8 @@
 // v_perm for each register.  The S^T accumulators leave a lane with the keys
 // 4 g .. 4 g + 3 of two groups of 16 for its row, which is the second product's
 // operand when the values are taken in the same order: no weight crosses a lane.
-// A weight meets V as two bf16 numbers, 17 bits together, or as three for an fp32
-// output, whose rounding is far below two; the sums are of the fp32 weights.
+// A weight meets V as two bf16 numbers, 17 bits together, or as three, all of its bits,
+// for an fp32 output, whose rounding is far below two; the sums are of the fp32 weights.
 //
 // What bounds it: HBM.  64 sequences of 8192 tokens, 32 heads on 8, d = 128: 316 us,
 // 6.8 TB/s, the matrix cores 0.06 busy.  One sequence of 4097: 8 us in 256 workgroups and

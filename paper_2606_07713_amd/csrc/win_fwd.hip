@@ -17,15 +17,20 @@
 // may then be 2^127 against its reference, so where states meet, of two key streams or
 // of splits, the one with the lower reference is never left out for that.  (Raised in
 // the loop where sums grew, the rarely taken branch cost a copy of all sums in every
-// step: 4096 tokens in a window of 512, 114 us.)  The sums are of the fp32 weights.  A weight
-// meets V as one bf16 number for a bf16 output (2^-9 each, which leaves the error
-// of a bf16 output at 1.4 times its own rounding's), as three for an fp32 output
-// (two left it at 2.3e-6, nine times what fp32 sums alone make).
+// step: 4096 tokens in a window of 512, 114 us.)  The sums are of the fp32 weights.
+//
+// A weight meets V as one bf16 number for a bf16 output, off by 2^-8 of it at most, as in
+// the prefill.  That leaves the output's error at 1.4 times its own rounding's (2.25e-3 to
+// 2.35e-3 against 64 bits for 1.65e-3); two numbers would leave the rounding's alone and
+// cost a quarter of the time in the matrix cores and the packing (4096 tokens in a
+// window of 512 95 -> 119 us, 200 queries on 20011 keys 94 -> 122, 4 x 1000 causal, d = 64,
+// 17 -> 21).  Who needs more takes an fp32 output, whose weights are three numbers, all of
+// their bits (two left it at 2.3e-6, nine times what fp32 sums alone make).
 //
 // What bounds it: matrix and vector instructions, which overlap in part (matrix cores
 // 0.43 to 0.48 of a unit's cycles, 6 to 8 vector instructions for each matrix
-// instruction).  d = 128, 32 heads on 8: 2 x 4096 tokens in a window of 512 93 us, 8192 in
-// one of 1024 160 us (0.81 PFLOP/s of visible pairs), 8192 causal of 32 heads 544 us.
+// instruction).  d = 128, 32 heads on 8: 2 x 4096 tokens in a window of 512 94 us, 8192 in
+// one of 1024 163 us (0.79 PFLOP/s of visible pairs), 8192 causal of 32 heads 544 us.
 #include <limits>
 
 #include "prefill_bf16_common.h"
